@@ -93,8 +93,8 @@ def _hidden_w(hidden, w, w_name):
 
 
 def _dlogits_arg(dlogits, logits):
-    if dlogits is True:
-        return torch.empty_like(logits)
+    if dlogits is True:  # with the logits' own row stride, also where they are a view of wider rows
+        return torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=logits.device)
     if dlogits is False or dlogits is None:
         return None
     _meta(dlogits, "dlogits", logits.dtype)
