@@ -1,6 +1,6 @@
 """MI355X (gfx950) library for the multi-step GRPO token loss of AsyncWebRL.
 
-Thin torch-facing binding of libgrpo's C ABI (include/grpo.h): every function
+Thin torch-facing binding of libgrpo's C ABI (include/grpo*.h): every function
 here marshals tensors into pointers and calls the entry point of the same
 name; all arithmetic runs in the HIP kernels.  torch provides device memory
 and the current stream only.  There is no CPU fallback: the functions raise
@@ -15,15 +15,17 @@ import torch
 
 from . import _lib
 from ._lib import (GRPO_ADV_GROUP_NORM, GRPO_ADV_SUCCESS_FILTER, GRPO_BF16, GRPO_F32,  # noqa: F401
-                   GRPO_FLAG_ACTION, GRPO_FLAG_NONFINITE, GRPO_FLAG_OFFSETS, GRPO_NOALLOC_SCRATCH_BYTES,
-                   GRPO_NORM_CONST_K, GRPO_NORM_TRAJ_STEPS, GrpoError)
+                   GRPO_FLAG_ACTION, GRPO_FLAG_NONFINITE, GRPO_FLAG_OFFSETS, GRPO_FLAG_SETTING, GRPO_GRAD_PARTIALS,
+                   GRPO_NOALLOC_SCRATCH_BYTES,
+                   GRPO_NORM_CONST_K, GRPO_NORM_TRAJ_STEPS, GRPO_SAMPLING_MAX_V, GrpoError)
 
 __all__ = ["grpo_advantages", "grpo_advantages_ex", "grpo_loss_workspace_bytes", "grpo_loss_fwd_bwd",
            "grpo_loss_fwd_bwd_noalloc", "fused_lmhead_workspace_bytes",
            "fused_lmhead_grpo", "fused_lmhead_blocked_workspace_bytes", "fused_lmhead_grpo_blocked", "grpo_token_logp", "grpo_vocab_shard_stats", "grpo_loss_fwd_bwd_vocab_shard",
            "vocab_stats_fields", "fused_lmhead_vocab_shard_stats", "fused_lmhead_grpo_vocab_shard",
            "vocab_shard_logits_buffer", "GrpoLoss", "FusedLmHeadGrpoLoss", "loss",
-           "fused_lmhead_token_logp",
+           "fused_lmhead_token_logp", "grpo_sample", "grpo_sampled_logp", "grpo_sampled_logp_bwd", "SampledLogp",
+           "GradList", "grpo_grad_sumsq", "grpo_grad_clip", "grpo_clip_grad_norm_",
            "grpo_status_str", "LossAux", "GrpoError"]
 
 
@@ -633,4 +635,6 @@ def fused_lmhead_grpo_vocab_shard(hidden: torch.Tensor, w_shard: torch.Tensor, s
     return loss_out, dhidden_partial, dw_shard
 
 
-from .autograd import FusedLmHeadGrpoLoss, GrpoLoss  # noqa: E402  (needs the entry points above)
+from .sampling import grpo_sample, grpo_sampled_logp, grpo_sampled_logp_bwd  # noqa: E402  (need the helpers above)
+from .clip import GradList, grpo_clip_grad_norm_, grpo_grad_clip, grpo_grad_sumsq  # noqa: E402
+from .autograd import FusedLmHeadGrpoLoss, GrpoLoss, SampledLogp  # noqa: E402

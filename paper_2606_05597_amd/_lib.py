@@ -1,4 +1,4 @@
-"""ctypes view of libgrpo's C ABI (include/grpo.h).  Marshalling only."""
+"""ctypes view of libgrpo's C ABI (include/grpo.h, grpo_sampling.h, grpo_clip.h).  Marshalling only."""
 from __future__ import annotations
 
 import ctypes
@@ -27,6 +27,10 @@ GRPO_NOALLOC_SCRATCH_BYTES = 24 << 20
 GRPO_FLAG_ACTION = 1
 GRPO_FLAG_OFFSETS = 2
 GRPO_FLAG_NONFINITE = 4
+GRPO_FLAG_SETTING = 8
+
+GRPO_SAMPLING_MAX_V = 4194304
+GRPO_GRAD_PARTIALS = 2048
 
 P = ctypes.c_void_p
 
@@ -45,6 +49,20 @@ class LossParams(ctypes.Structure):
 class Aux(ctypes.Structure):
     _fields_ = [("token_logp", P), ("tok_traj", P), ("traj_tok_off", P), ("gather_idx", P), ("traj_loss", P),
                 ("clip_counts", P), ("ratio_stats", P), ("error_flags", P), ("hot_begin", P), ("hot_end", P)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", P), ("top_k", P), ("top_p", P), ("min_p", P), ("temperature_all", ctypes.c_float),
+                ("top_k_all", ctypes.c_int32), ("top_p_all", ctypes.c_float), ("min_p_all", ctypes.c_float)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("data", P), ("out", P), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32)]
+
+
+class GradLayout(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("in_place", ctypes.c_int32), ("units", ctypes.c_int64)]
 
 
 class GrpoError(RuntimeError):
@@ -107,6 +125,22 @@ def load() -> ctypes.CDLL:
         lib.fused_lmhead_vocab_shard_logits_bytes.argtypes = [I64, I64]
         lib.fused_lmhead_vocab_shard_logits_bytes.restype = SZ
         lib.fused_lmhead_grpo_vocab_shard.restype = ctypes.c_int
+        lib.grpo_sampling_workspace_bytes.argtypes = [I64, I64]
+        lib.grpo_sampling_workspace_bytes.restype = SZ
+        lib.grpo_sample.argtypes = [P, I32, I64, I64, I64, ctypes.POINTER(Sampling), P, P, P, P, P, P, SZ, P]
+        lib.grpo_sample.restype = ctypes.c_int
+        lib.grpo_sampled_logp.argtypes = lib.grpo_sample.argtypes
+        lib.grpo_sampled_logp.restype = ctypes.c_int
+        lib.grpo_sampled_logp_bwd.argtypes = [P, I32, I64, I64, I64, P, P, P, P, P]
+        lib.grpo_sampled_logp_bwd.restype = ctypes.c_int
+        lib.grpo_grad_table_bytes.argtypes = [I32]
+        lib.grpo_grad_table_bytes.restype = SZ
+        lib.grpo_grad_table.argtypes = [ctypes.POINTER(Grad), I32, P, SZ, ctypes.POINTER(GradLayout)]
+        lib.grpo_grad_table.restype = ctypes.c_int
+        lib.grpo_grad_sumsq.argtypes = [ctypes.POINTER(GradLayout), P, P, P]
+        lib.grpo_grad_sumsq.restype = ctypes.c_int
+        lib.grpo_grad_clip.argtypes = [ctypes.POINTER(GradLayout), P, P, ctypes.c_double, P, P, P]
+        lib.grpo_grad_clip.restype = ctypes.c_int
         # the binding's own (autograd.py), not declared in grpo.h
         lib.grpo_binding_scale_to_bf16.argtypes = [P, P, P, I64, P]
         lib.grpo_binding_scale_to_bf16.restype = ctypes.c_int

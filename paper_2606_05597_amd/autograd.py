@@ -16,8 +16,10 @@ Neither direction synchronises with the host.  How backward treats the incoming 
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _check, _lib, _ptr, _stream, fused_lmhead_grpo, fused_lmhead_grpo_blocked, grpo_loss_fwd_bwd
+from .sampling import grpo_sampled_logp, grpo_sampled_logp_bwd
 
 _UPSTREAM = ("scale", "unit")
 
@@ -130,3 +132,31 @@ class FusedLmHeadGrpoLoss(torch.autograd.Function):
             else:
                 dW = _apply_upstream(ctx.upstream, (dw,), grad_output)[0].to(torch.bfloat16)
         return dh, dW, None, None, None, None, None, None, None
+
+
+class SampledLogp(torch.autograd.Function):
+    """``logp = SampledLogp.apply(logits, actions, opts)``
+
+    The log-probs (fp32 [T]) of given actions under the rollout's sampling distribution, for objectives of the caller's
+    own: logits [T, V] (bf16 or fp32, on the GPU), ``opts`` a dict of the keyword options of ``grpo_sampled_logp``
+    (temperature, top_k, top_p, min_p, V, error_flags, workspace).  backward reads the logits again and writes their gradient
+    (``grpo_sampled_logp_bwd``; zero in columns past V); the kept set is a constant.  An action that is not kept has
+    log-prob -inf and no gradient.
+    """
+
+    @staticmethod
+    def forward(ctx, logits, actions, opts=None):
+        opts = dict(opts or {})
+        ctx.V = opts.get("V")
+        logp, _, rows = grpo_sampled_logp(logits.detach(), actions, **opts)
+        ctx.save_for_backward(logits, actions, rows)
+        return logp
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_output):
+        logits, actions, rows = ctx.saved_tensors
+        padded = ctx.V is not None and ctx.V < logits.shape[1]
+        dlogits = torch.zeros_like(logits) if padded else True
+        d = grpo_sampled_logp_bwd(logits, actions, rows, grad_output.contiguous(), V=ctx.V, dlogits=dlogits)
+        return d, None, None

@@ -350,6 +350,28 @@ __device__ inline void merge_vocab_stats_wave(const grpo_vocab_stats* stats, int
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// The same 16 bytes at any address of a 4- or 2-byte element: the hardware takes vector accesses at any alignment.
+typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+template <typename Tin>
+struct VecAt {
+  typedef u32x4_a4 type;
+};
+template <>
+struct VecAt<uint16_t> {
+  typedef u32x4_a2 type;
+};
+
+// Element e of a 16-byte vector (8 bf16 or 4 fp32), widened to fp32.
+template <typename Tin>
+__device__ __forceinline__ float elem(const u32x4& x, int e) {
+  if constexpr (sizeof(Tin) == 2) {
+    const uint32_t w = x[e >> 1];
+    return (e & 1) ? bf16_hi(w) : bf16_lo(w);
+  } else {
+    return __uint_as_float(x[e]);
+  }
+}
 
 // max(a, b, c) in one instruction.  Written as asm because the compiler otherwise canonicalises every loaded
 // value before an fmaxf (two more instructions per dword of logits).  In IEEE mode a quiet NaN operand is

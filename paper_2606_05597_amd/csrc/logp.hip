@@ -20,8 +20,6 @@
 
 namespace grpo {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 struct LogpArgs {
   const void* logits;
   int64_t ld, V;
@@ -88,17 +86,6 @@ __device__ __forceinline__ void block_combine3(float m, float s, float t, float*
     M_out = (double)M;
     S_out = S;
     T_out = T;
-  }
-}
-
-// Element e of a 16-byte vector (8 bf16 or 4 fp32), widened to fp32.
-template <typename Tin>
-__device__ __forceinline__ float elem(const u32x4& x, int e) {
-  if constexpr (sizeof(Tin) == 2) {
-    const uint32_t w = x[e >> 1];
-    return (e & 1) ? bf16_hi(w) : bf16_lo(w);
-  } else {
-    return __uint_as_float(x[e]);
   }
 }
 
