@@ -1064,40 +1064,64 @@ __global__ __launch_bounds__(kBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8))) 
   const float c = (float)(kLog2e64 / (double)r.temperature);
   const float l = none || nan ? 0.f : (float)log2(r.sum);
   const float neg = (float)-scale;
-  auto one = [&](float z, int col) {
-    const bool in = z > r.threshold || (z == r.threshold && col <= r.tie);
-    float d = in ? neg * __builtin_amdgcn_exp2f(fmaf(z - r.max, c, -l)) : 0.f;
-    if (col == act) d = (float)(scale * (1.0 - exp(((double)z - (double)r.max) / (double)r.temperature) / r.sum));
-    return none ? 0.f : nan ? NAN : d;
+  const int c0 = b * kBwdCols;
+  // Words that equal the threshold are kept up to r.tie: all of this workgroup's, none, or (mixed) some of them.
+  const float least = r.tie < c0 ? nextafterf(r.threshold, INFINITY) : r.threshold;
+  const bool mixed = r.tie >= c0 && r.tie < c0 + kBwdCols;
+  auto one = [&](float z, int col, bool ties) {
+    const bool in = z >= least && !(ties && z == r.threshold && col > r.tie);
+    return in ? neg * __builtin_amdgcn_exp2f(fmaf(z - r.max, c, -l)) : 0.f;
   };
-  auto vec = [&](const u32x4& x, int col) {
+  auto vec = [&](const u32x4& x, int col, bool ties) {
     u32x4 o;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if constexpr (sizeof(Tin) == 2)
-        o[q] = pack_bf16(one(bf16_lo(x[q]), col + 2 * q), one(bf16_hi(x[q]), col + 2 * q + 1));
+        o[q] = pack_bf16(one(bf16_lo(x[q]), col + 2 * q, ties), one(bf16_hi(x[q]), col + 2 * q + 1, ties));
       else
-        o[q] = __float_as_uint(one(__uint_as_float(x[q]), col + q));
+        o[q] = __float_as_uint(one(__uint_as_float(x[q]), col + q, ties));
     }
     return o;
   };
-  const int c0 = b * kBwdCols;
+  // the action's own, formed in fp64; read before any store, which may be to the same place
+  const bool has_act = act >= c0 && act < min(c0 + kBwdCols, a.V);
+  float d_act = 0.f;
+  if (has_act) {
+    const float z = load_elem(row + act);
+    d_act = none ? 0.f : (float)(scale * (1.0 - exp(((double)z - (double)r.max) / (double)r.temperature) / r.sum));
+    __syncthreads();
+  }
+  const int edge = a.V / EPV * EPV;  // the row's last words, fewer than a vector holds, one to a thread
+  const int n_edge = b == a.blocks - 1 ? a.V - edge : 0;
   u32x4 x[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const int col = c0 + (i * kBwdNT + tid) * EPV;
     if (col + EPV <= a.V) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + col));
   }
+  const float ez = tid < n_edge ? load_elem(row + edge + tid) : 0.f;
+  auto store = [&](auto value) {
 #pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int col = c0 + (i * kBwdNT + tid) * EPV;
-    if (col + EPV <= a.V) {
-      __builtin_nontemporal_store(vec(x[i], col), reinterpret_cast<u32x4_any*>(drow + col));
-      asm volatile("s_nop 1" ::: "memory");  // the store has read its data before its registers are reused
-    } else {
-      for (int q = col; q < a.V; ++q) store_elem(drow + q, one(load_elem(row + q), q));
+    for (int i = 0; i < U; ++i) {
+      const int col = c0 + (i * kBwdNT + tid) * EPV;
+      if (col + EPV <= a.V) {
+        __builtin_nontemporal_store(value(x[i], col), reinterpret_cast<u32x4_any*>(drow + col));
+        asm volatile("s_nop 1" ::: "memory");  // the store has read its data before its registers are reused
+      }
     }
+  };
+  if (none || nan) {
+    const float v = none ? 0.f : NAN;
+    const uint32_t w = sizeof(Tin) == 2 ? pack_bf16(v, v) : __float_as_uint(v);
+    store([&](const u32x4&, int) { return u32x4{w, w, w, w}; });
+    if (tid < n_edge) store_elem(drow + edge + tid, v);
+    return;
   }
+  if (mixed) store([&](const u32x4& v, int col) { return vec(v, col, true); });
+  else store([&](const u32x4& v, int col) { return vec(v, col, false); });
+  if (tid < n_edge) store_elem(drow + edge + tid, one(ez, edge + tid, mixed));
+  // the thread that stored the action's place, after that store
+  if (has_act && tid == (act >= edge ? act - edge : (act - c0) / EPV % kBwdNT)) store_elem(drow + act, d_act);
 }
 
 __global__ void k_clear_sampling_flag(int32_t* f) { *f = 0; }
