@@ -9,14 +9,16 @@
 // Counts are exact; weights and their sums are fp64 (exp2_neg below), because with 150,000 words of about equal weight a
 // word's share is 7e-6 of the sum, and an error of 1e-8 in the sums would draw another word in one row of a thousand.
 //
-// A row is cut into tiles of kTile words, each reduced in a wave's registers to its maximum, its count of live words and
+// A row is cut into tiles, each reduced in a wave's registers to its maximum, its count of live words and
 // its sum of weights relative to its own maximum: one pass over memory, of any number of waves per row.  Then one
 // workgroup per row works on the tiles' records and re-reads only the tiles that it needs:
 //   nothing cut     a draw picks its tile by the tiles' sums and re-reads that one;
 //   few candidates  a lower bound of the threshold (the k-th largest of the partial maxima; for top-p, the weight below
 //                   which all live words together weigh less than (1 - p) S; min-p's own) leaves at most kCap words:
 //                   they are gathered in LDS, sorted, and the cut read off their prefix sums;
-//   many            histograms: words fall into kBins bins of a quarter of a power of two of weight, each bin's count
+//   many, bf16      a count of each value (bf16 logits below 64 in size have 5,377 that are told apart); counts times weights,
+//                   summed from the top, give the cut, and a table of the values' weights the tiles' kept sums;
+//   many, else      histograms: words fall into kBins bins of a quarter of a power of two of weight, each bin's count
 //                   and weight are summed, the bin that holds the cut is split again by the bits of its logits until at
 //                   most kCap words (gathered and sorted) or one repeated value are left.
 // Histogram weights are integers (weight relative to the bin's top, in 2^-44), so that atomics in any order give one sum.
@@ -32,21 +34,23 @@
 
 namespace grpo {
 
-constexpr int kTile = 2048;        // words of a tile: 32 per lane
-constexpr int kMaxTiles = GRPO_SAMPLING_MAX_V / kTile;
+constexpr int kTileVecs = 4;       // a tile: 4 vectors of 16 bytes per lane, 2,048 bf16 words or 1,024 of fp32
 constexpr int kSubs = 8;           // partial maxima of a tile, each over 8 lanes' words
-constexpr int kMaxSubs = 1024;     // partial maxima (or tiles' maxima) that bound the k-th largest word
+constexpr int kMaxSubs = 1280;     // partial maxima (or tiles' maxima) that bound the k-th largest word
 constexpr int kCap = 2048;         // words that are sorted in LDS
 constexpr int kBins = 128, kCols = 32;
-constexpr int kNT = 512, kNW = kNT / 64;
+constexpr int kMaxNW = 16;
+constexpr float kLimit = 64.f;     // logits that the count of values takes: below it in size
 constexpr float kLiveMin = -99999992.f;  // the smallest float above -1e8: the lowest live logit
 constexpr double kLog2e64 = 1.4426950408889634074;
 
 struct TileRec {
   double sum;
   float sub[kSubs];
+  float lo;       // the least live logit
   int32_t live;
   int32_t bad;
+  int32_t pad;
 };
 
 struct RowArgs {
@@ -104,22 +108,26 @@ __device__ __forceinline__ float min3f(float a, float b, float c) {
   return r;
 }
 
-__device__ __forceinline__ double scan_add(double v) {  // inclusive, over the wave
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double n = __shfl_up(v, o, 64);
-    if (lane >= o) v += n;
-  }
-  return v;
+// Inclusive sums over the wave, by lane moves within rows of 16 (row_shr), then from row to row (row_bcast).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_rows(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, ROWS == 0xF);
 }
-__device__ __forceinline__ int scan_add(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int n = __shfl_up(v, o, 64);
-    if (lane >= o) v += n;
-  }
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ double dpp_rows(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)dpp_rows<CTRL, ROWS>((int)(uint32_t)u);
+  const uint32_t hi = (uint32_t)dpp_rows<CTRL, ROWS>((int)(uint32_t)(u >> 32));
+  return __builtin_bit_cast(double, (uint64_t)lo | ((uint64_t)hi << 32));
+}
+template <typename T>
+__device__ __forceinline__ T scan_add(T v) {
+  v += dpp_rows<0x111, 0xF>(v);
+  v += dpp_rows<0x112, 0xF>(v);
+  v += dpp_rows<0x114, 0xF>(v);
+  v += dpp_rows<0x118, 0xF>(v);
+  v += dpp_rows<0x142, 0xA>(v);
+  v += dpp_rows<0x143, 0xC>(v);
   return v;
 }
 
@@ -143,12 +151,13 @@ __device__ __forceinline__ Settings load_settings(const grpo_sampling& g, int t)
   return s;
 }
 
-// What a tile's sum of weights is for: nothing, a cut or a draw (fp64), or a log-prob alone (fp32 terms, like the other
-// log-probs of this library).
+// How a tile's weights are summed: not at all, exactly enough for a cut or a draw (fp64), or for a log-prob alone, and for
+// a first estimate of a cut (fp32 terms, like the other log-probs of this library; off by less than kSum32Error).
 enum SumMode { kNoSum, kSum64, kSum32 };
-__device__ __forceinline__ SumMode sum_mode(const Settings& s, int V, bool draw) {
+constexpr double kSum32Error = 1e-5;
+__device__ __forceinline__ SumMode sum_mode(const Settings& s, int V, bool draw, bool fused) {
   if (!s.ok || s.greedy || (s.k > 0 && s.k < V)) return kNoSum;
-  if (s.p < 1.f) return kSum64;
+  if (s.p < 1.f) return fused ? kSum32 : kSum64;
   if (s.min_p > 0.f) return kNoSum;
   return draw ? kSum64 : kSum32;
 }
@@ -158,11 +167,11 @@ __device__ __forceinline__ SumMode sum_mode(const Settings& s, int V, bool draw)
 // at any alignment, so a row may start at any element.  Words past the row's end read as -inf.
 template <typename Tin>
 struct Tile {
-  static constexpr int EPV = 16 / (int)sizeof(Tin), NV = kTile / 64 / EPV;
+  static constexpr int EPV = 16 / (int)sizeof(Tin), NV = kTileVecs, kWords = 64 * EPV * NV;
   u32x4 v[NV];
 
   __device__ __forceinline__ static int col(int tile, int j, int e) {
-    return tile * kTile + (j * 64 + (threadIdx.x & 63)) * EPV + e;
+    return tile * kWords + (j * 64 + (threadIdx.x & 63)) * EPV + e;
   }
   // Vector j of a tile that the row's end may cut.
   __device__ __forceinline__ static u32x4 load_one(const Tin* row, int V, int tile, int j) {
@@ -184,7 +193,7 @@ struct Tile {
   }
   __device__ __forceinline__ void load(const Tin* row, int V, int tile) {
     typedef typename VecAt<Tin>::type u32x4_any;
-    if ((tile + 1) * kTile <= V) {
+    if ((tile + 1) * kWords <= V) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) v[j] = *reinterpret_cast<const u32x4_any*>(row + col(tile, j, 0));
     } else {
@@ -204,6 +213,7 @@ struct TileStats {
   double sum;   // of weights relative to max; every lane
   float sub;    // the maximum over this lane's group of 8 lanes
   float max;    // every lane
+  float lo;     // the least live logit; every lane
   int live;     // every lane
   bool bad;     // a NaN or +inf; every lane
 };
@@ -227,18 +237,25 @@ __device__ __forceinline__ TileStats tile_stats(const Tile<Tin>& x, SumMode mode
   g = fmaxf(g, dpp_f32v<0x4E>(g));
   s.sub = fmaxf(g, dpp_f32v<0x141>(g));
   s.max = wave_max_dpp(mx);
-  const float lo = -wave_max_dpp(-mn);
+  float lo = -wave_max_dpp(-mn);
   s.bad = __any(nan) || s.max == INFINITY;
   s.sum = 0.0;
-  s.live = kTile;
+  s.live = Tile<Tin>::kWords;
   const bool all_live = lo >= kLiveMin;
   if (!all_live) {
     s.live = 0;
+    mn = INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) s.live += __popcll(__ballot(x.at(j, e) >= kLiveMin));
+      for (int e = 0; e < EPV; ++e) {
+        const float z = x.at(j, e);
+        s.live += __popcll(__ballot(z >= kLiveMin));
+        if (z >= kLiveMin) mn = fminf(mn, z);
+      }
+    lo = -wave_max_dpp(-mn);
   }
+  s.lo = lo;
   if (mode == kNoSum || s.bad || s.live == 0) return s;
   if (mode == kSum64) {
     const double m = (double)s.max;
@@ -289,17 +306,39 @@ __global__ __launch_bounds__(256) void k_sample_tiles(const RowArgs a, int n_wav
   const Settings st = load_settings(a.par, t);
   Tile<Tin> x;
   x.load(static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld, a.V, tile);
-  const TileStats s = tile_stats<Tin>(x, sum_mode(st, a.V, draw), st.c);
+  const TileStats s = tile_stats<Tin>(x, sum_mode(st, a.V, draw, false), st.c);
   TileRec* r = a.recs + w;
   if ((lane & 7) == 0) r->sub[lane >> 3] = s.sub;
   if (lane == 0) {
     r->sum = s.sum;
+    r->lo = s.lo;
     r->live = s.live;
     r->bad = s.bad;
   }
 }
 
 // ---- one row --------------------------------------------------------------------
+// bf16 logits below kLimit in size, by value: `i` counts the steps from 2^-15 up, 0 is anything smaller in size, and
+// kSteps + 1 is what does not count (masked words); a word's bin is kMid + i or kMid - i by its sign.
+constexpr int kStepLo = 0x3800;                       // the bits of 2^-15
+constexpr int kSteps = 0x4280 - kStepLo;              // of kLimit, less those
+constexpr int kMid = kSteps + 1, kValues = 2 * kMid + 1;
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+// Both bins of a pair of words, less kMid; `least` is 0 where one of either half was kMid itself.
+__device__ __forceinline__ s16x2 value_bins(uint32_t w, u16x2& least) {
+  u16x2 i = __builtin_bit_cast(u16x2, w & 0x7fff7fffu);
+  i = __builtin_elementwise_sub_sat(i, (u16x2)(unsigned short)(kStepLo - 1));
+  least = __builtin_elementwise_min(least, i);
+  i = __builtin_elementwise_min(i, (u16x2)(unsigned short)kMid);
+  const s16x2 sign = __builtin_bit_cast(s16x2, w) >> (s16x2)(short)15;
+  return (__builtin_bit_cast(s16x2, i) ^ sign) - sign;
+}
+__device__ __forceinline__ float bin_value(int bin) {
+  const int i = bin - kMid, mag = (i < 0 ? -i : i) + kStepLo - 1;
+  return i == 0 ? 0.f : __uint_as_float(((uint32_t)mag << 16) | (i < 0 ? 0x80000000u : 0u));
+}
+
 struct Cut {
   float thr;    // kept: z > thr, or z == thr and index <= tie
   int tie;
@@ -316,108 +355,138 @@ struct RowShared {
       unsigned long long key[kCap];
       double cum[kCap];
     } l;
-    int tcount[kMaxTiles];
+    struct {
+      double weight[kValues];
+      uint32_t count[kValues];
+      unsigned long long mid;  // the weight of the words of bin kMid, in 2^-44 of `mid_top`'s
+    } v;
   };
-  double tsum[kMaxTiles];
-  float tmax[kMaxTiles];
   float sub[kMaxSubs];
   double bin_mass[2][kBins];
   int bin_count[2][kBins];
-  double wd[kNW];
-  int wi[kNW];
+  double wd[2][kMaxNW];
+  int wi[2][kMaxNW];
+  float wf[2][kMaxNW];
   // broadcast
   int n, bin, i0;
   uint32_t key;
   double d0;
 };
 
-// Workgroup reductions, the same value in every thread; `sh.w*` may be reused after them.
-__device__ __forceinline__ double block_sum(RowShared& sh, double v) {
-  v = wave_sum_dpp(v);
-  if ((threadIdx.x & 63) == 0) sh.wd[threadIdx.x >> 6] = v;
-  __syncthreads();
-  double r = 0.0;
-#pragma unroll
-  for (int i = 0; i < kNW; ++i) r += sh.wd[i];
-  __syncthreads();
-  return r;
-}
-template <typename F>
-__device__ __forceinline__ int block_reduce_int(RowShared& sh, int v, F f) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
-  if ((threadIdx.x & 63) == 0) sh.wi[threadIdx.x >> 6] = v;
-  __syncthreads();
-  int r = sh.wi[0];
-#pragma unroll
-  for (int i = 1; i < kNW; ++i) r = f(r, sh.wi[i]);
-  __syncthreads();
-  return r;
-}
-__device__ __forceinline__ int block_sum_int(RowShared& sh, int v) {
-  return block_reduce_int(sh, v, [](int a, int b) { return a + b; });
-}
-__device__ __forceinline__ int block_min_int(RowShared& sh, int v) {
-  return block_reduce_int(sh, v, [](int a, int b) { return min(a, b); });
-}
-__device__ __forceinline__ int block_max_int(RowShared& sh, int v) {
-  return block_reduce_int(sh, v, [](int a, int b) { return max(a, b); });
-}
-// Inclusive scan over the workgroup's threads; total in every thread.
-__device__ __forceinline__ double block_scan(RowShared& sh, double v, double& total) {
-  const int wv = threadIdx.x >> 6;
-  v = scan_add(v);
-  if ((threadIdx.x & 63) == 63) sh.wd[wv] = v;
-  __syncthreads();
-  double before = 0.0, all = 0.0;
-#pragma unroll
-  for (int i = 0; i < kNW; ++i) {
-    if (i < wv) before += sh.wd[i];
-    all += sh.wd[i];
-  }
-  __syncthreads();
-  total = all;
-  return before + v;
-}
+// A tile's record in LDS, `tiles` of each after RowShared.
+struct RowTiles {
+  double* sum;
+  float* max;
+  int* count;
+};
+__host__ __device__ constexpr size_t row_tile_bytes(int tiles) { return (size_t)tiles * 16; }
 
-// Sorts the n keys in sh.l.key, largest first, padded with zeros to a power of two.
-__device__ __forceinline__ void sort_list(RowShared& sh, int n) {
-  const int tid = threadIdx.x;
-  int P = 2;
-  while (P < n) P <<= 1;
-  for (int i = n + tid; i < P; i += kNT) sh.l.key[i] = 0ull;
-  __syncthreads();
-  for (int k = 2; k <= P; k <<= 1) {
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int q = tid; q < (P >> 1); q += kNT) {
-        const int i = ((q & ~(j - 1)) << 1) | (q & (j - 1));
-        const unsigned long long x = sh.l.key[i], y = sh.l.key[i | j];
-        if ((x < y) == ((i & k) == 0)) {
-          sh.l.key[i] = y;
-          sh.l.key[i | j] = x;
-        }
-      }
-      __syncthreads();
-    }
-  }
-}
-
-template <typename Tin>
+template <typename Tin, int NT>
 struct RowWork {
+  static constexpr int NW = NT / 64, NV = Tile<Tin>::NV, EPV = Tile<Tin>::EPV;
+  static constexpr bool kByValue = sizeof(Tin) == 2;
   RowShared& sh;
+  RowTiles rec;
   const Tin* row;
   int V, tiles;
   float m;   // the row's maximum
   double c;  // log2(e) / tau
   float x_lo;  // words below it are not looked at
 
+  // ---- over the workgroup: the same value in every thread; two barriers each, so that `sh` may be reused ----
+  __device__ __forceinline__ double block_sum(double v) const {
+    v = wave_sum_dpp(v);
+    if ((threadIdx.x & 63) == 0) sh.wd[0][threadIdx.x >> 6] = v;
+    __syncthreads();
+    double r = 0.0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) r += sh.wd[0][i];
+    __syncthreads();
+    return r;
+  }
+  template <typename F>
+  __device__ __forceinline__ int block_reduce(int v, F f) const {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
+    if ((threadIdx.x & 63) == 0) sh.wi[0][threadIdx.x >> 6] = v;
+    __syncthreads();
+    int r = sh.wi[0][0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) r = f(r, sh.wi[0][i]);
+    __syncthreads();
+    return r;
+  }
+  __device__ __forceinline__ int block_sum(int v) const {
+    return block_reduce(v, [](int a, int b) { return a + b; });
+  }
+  __device__ __forceinline__ int block_min(int v) const {
+    return block_reduce(v, [](int a, int b) { return min(a, b); });
+  }
+  __device__ __forceinline__ int block_max(int v) const {
+    return block_reduce(v, [](int a, int b) { return max(a, b); });
+  }
+  // Sums of a count and a weight over the threads up to this one.
+  __device__ __forceinline__ void block_scan(int& n, double& v, int& all_n, double& all_v) const {
+    const int wv = threadIdx.x >> 6;
+    n = scan_add(n);
+    v = scan_add(v);
+    if ((threadIdx.x & 63) == 63) {
+      sh.wi[0][wv] = n;
+      sh.wd[0][wv] = v;
+    }
+    __syncthreads();
+    double before = 0.0;
+    int n_before = 0;
+    all_n = 0;
+    all_v = 0.0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      if (i == wv) {
+        before = all_v;
+        n_before = all_n;
+      }
+      all_n += sh.wi[0][i];
+      all_v += sh.wd[0][i];
+    }
+    __syncthreads();
+    n += n_before;
+    v += before;
+  }
+  __device__ __forceinline__ double block_scan(double v, double& all) const {
+    int n = 0, all_n;
+    block_scan(n, v, all_n, all);
+    return v;
+  }
+
+  // ---- over the row ----
+
+  // f(tile's words, tile) for each of this wave's tiles that `want` names, the next one's loads in flight.
+  template <typename P, typename F>
+  __device__ __forceinline__ void each_tile(P want, F f) const {
+    auto next = [&](int t) {
+      while (t < tiles && !want(t)) t += NW;
+      return t;
+    };
+    int tile = next(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    Tile<Tin> x;
+    if (tile < tiles) x.load(row, V, tile);
+    while (tile < tiles) {
+      const int after = next(tile + NW);
+      Tile<Tin> y;
+      if (after < tiles) y.load(row, V, after);
+      f(x, tile);
+      x = y;
+      tile = after;
+    }
+  }
+
   // f(vector, j) over a tile's vectors, the next one's load in flight: for the passes whose work per word is long.
   template <typename F>
   __device__ __forceinline__ void each_vector(int tile, F f) const {
     u32x4 x = Tile<Tin>::load_one(row, V, tile, 0);
 #pragma unroll 1
-    for (int j = 0; j < Tile<Tin>::NV; ++j) {
-      const u32x4 next = Tile<Tin>::load_one(row, V, tile, min(j + 1, Tile<Tin>::NV - 1));
+    for (int j = 0; j < NV; ++j) {
+      const u32x4 next = Tile<Tin>::load_one(row, V, tile, min(j + 1, NV - 1));
       f(x, j);
       x = next;
     }
@@ -425,50 +494,77 @@ struct RowWork {
 
   __device__ __forceinline__ double t2(float z) const { return ((double)z - (double)m) * c; }
   __device__ __forceinline__ double weight(float z) const { return exp2_neg(t2(z)); }
+  __device__ __forceinline__ bool kept(float z, int col, float thr, int tie) const {
+    return z > thr || (z == thr && col <= tie);
+  }
+
+  // ---- a list of words in LDS ----
 
   // The words of [lo, hi] appended to the list while it has room; returns how many there are, or more than kCap.
-  __device__ __forceinline__ int gather(float lo, float hi) {
+  __device__ __forceinline__ int gather(float lo, float hi) const {
     const int tid = threadIdx.x, lane = tid & 63;
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    for (int tile = tid >> 6; tile < tiles; tile += kNW) {
-      if (sh.tmax[tile] < lo) continue;
-      if (__builtin_amdgcn_readfirstlane(*(volatile int*)&sh.n) > kCap) break;
-      Tile<Tin> x;
-      x.load(row, V, tile);
+    each_tile(
+        [&](int tile) {
+          return rec.max[tile] >= lo && __builtin_amdgcn_readfirstlane(*(volatile int*)&sh.n) <= kCap;
+        },
+        [&](const Tile<Tin>& x, int tile) {
 #pragma unroll
-      for (int j = 0; j < Tile<Tin>::NV; ++j) {
-        if (!__any(vec_max<Tin>(x.v[j], -INFINITY) >= lo)) continue;
+          for (int j = 0; j < NV; ++j) {
+            if (!__any(vec_max<Tin>(x.v[j], -INFINITY) >= lo)) continue;
 #pragma unroll
-        for (int e = 0; e < Tile<Tin>::EPV; ++e) {
-          const float z = x.at(j, e);
-          const bool in = z >= lo && z <= hi;
-          const uint64_t mask = __ballot(in);
-          if (mask) {
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&sh.n, __popcll(mask));
-            at = __builtin_amdgcn_readfirstlane(at) + (int)__popcll(mask & ((1ull << lane) - 1));
-            if (in && at < kCap)
-              sh.l.key[at] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~x.col(tile, j, e);
+            for (int e = 0; e < EPV; ++e) {
+              const float z = x.at(j, e);
+              const bool in = z >= lo && z <= hi;
+              const uint64_t mask = __ballot(in);
+              if (mask) {
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&sh.n, __popcll(mask));
+                at = __builtin_amdgcn_readfirstlane(at) + (int)__popcll(mask & ((1ull << lane) - 1));
+                if (in && at < kCap)
+                  sh.l.key[at] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~x.col(tile, j, e);
+              }
+            }
           }
-        }
-      }
-    }
+        });
     __syncthreads();
     const int n = sh.n;
     __syncthreads();
     return n;
   }
 
+  // Sorts the n keys in sh.l.key, largest first, padded with zeros to a power of two.
+  __device__ __forceinline__ void sort_list(int n) const {
+    const int tid = threadIdx.x;
+    int P = 2;
+    while (P < n) P <<= 1;
+    for (int i = n + tid; i < P; i += NT) sh.l.key[i] = 0ull;
+    __syncthreads();
+    for (int k = 2; k <= P; k <<= 1) {
+      for (int j = k >> 1; j > 0; j >>= 1) {
+        for (int q = tid; q < (P >> 1); q += NT) {
+          const int i = ((q & ~(j - 1)) << 1) | (q & (j - 1));
+          const unsigned long long x = sh.l.key[i], y = sh.l.key[i | j];
+          if ((x < y) == ((i & k) == 0)) {
+            sh.l.key[i] = y;
+            sh.l.key[i | j] = x;
+          }
+        }
+        __syncthreads();
+      }
+    }
+  }
+
   __device__ __forceinline__ float list_value(int i) const { return key_value((uint32_t)(sh.l.key[i] >> 32)); }
   __device__ __forceinline__ int list_index(int i) const { return (int)~(uint32_t)sh.l.key[i]; }
 
   // sh.l.cum = the prefix sums of the list's weights, from `base` on.
-  __device__ __forceinline__ void scan_list(int n, double base) {
-    for (int i0 = 0; i0 < n; i0 += kNT) {
+  __device__ __forceinline__ void scan_list(int n, double base) const {
+    for (int i0 = 0; i0 < n; i0 += NT) {
       const int i = i0 + threadIdx.x;
       double total;
-      const double v = block_scan(sh, i < n ? weight(list_value(i)) : 0.0, total);
+      const double v = block_scan(i < n ? weight(list_value(i)) : 0.0, total);
       if (i < n) sh.l.cum[i] = base + v;
       base += total;
     }
@@ -476,15 +572,87 @@ struct RowWork {
   }
 
   // The least r >= 1 with cum[r - 1] >= target, or n.
-  __device__ __forceinline__ int first_reaching(int n, double target) {
+  __device__ __forceinline__ int first_reaching(int n, double target) const {
     int r = n;
-    for (int i = threadIdx.x; i < n; i += kNT)
+    for (int i = threadIdx.x; i < n; i += NT)
       if (sh.l.cum[i] >= target) {
         r = i + 1;
         break;
       }
-    return block_min_int(sh, r);
+    return block_min(r);
   }
+
+  // ---- one value's words ----
+
+  // Wave 0: the tile's r-th word (from 1) that equals z, by index.
+  __device__ __forceinline__ int nth_equal(int tile, float z, int r) const {
+    int found = 0;
+    each_vector(tile, [&](const u32x4& x, int j) {
+      int n = 0;
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) n += elem<Tin>(x, e) == z;
+      const int incl = scan_add(n);
+      const int all = __builtin_amdgcn_readlane(incl, 63);
+      if (r >= 1 && r <= all) {
+        const int l = __ffsll((unsigned long long)__ballot(incl >= r)) - 1;
+        int left = r - (incl - n), col = 0;
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) {
+          const bool same = elem<Tin>(x, e) == z;
+          left -= same;
+          if (left == 0 && same) col = Tile<Tin>::col(tile, j, e);
+        }
+        found = __builtin_amdgcn_readlane(col, l);
+      }
+      r -= all;
+    });
+    return found;
+  }
+
+  // rec.count = each tile's words that equal z.
+  __device__ __forceinline__ void count_equal(float z) const {
+    for (int i = threadIdx.x; i < tiles; i += NT)
+      if (!(rec.max[i] >= z)) rec.count[i] = 0;
+    each_tile([&](int tile) { return rec.max[tile] >= z; },
+              [&](const Tile<Tin>& x, int tile) {
+                int n = 0;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                  for (int e = 0; e < EPV; ++e) n += __popcll(__ballot(x.at(j, e) == z));
+                if ((threadIdx.x & 63) == 0) rec.count[tile] = n;
+              });
+    __syncthreads();
+  }
+
+  // The index of the r-th word of the row that equals z, from rec.count; rec.count then holds the tiles' words among
+  // the first r.
+  __device__ __forceinline__ int tie_index(float z, int r) const {
+    const int lane = threadIdx.x;
+    if (lane < 64) {
+      int left = r, at = -1, at_left = 0;
+      for (int i0 = 0; i0 < tiles; i0 += 64) {
+        const int n = i0 + lane < tiles ? rec.count[i0 + lane] : 0;
+        const int incl = scan_add(n);
+        const uint64_t mask = __ballot(incl >= left);
+        if (at < 0 && mask) {
+          const int l = __ffsll((unsigned long long)mask) - 1;
+          at_left = left - __builtin_amdgcn_readlane(incl - n, l);
+          at = i0 + l;
+        }
+        if (i0 + lane < tiles) rec.count[i0 + lane] = max(0, min(n, left - (incl - n)));
+        left -= __builtin_amdgcn_readlane(incl, 63);
+      }
+      const int col = at < 0 ? V : nth_equal(at, z, at_left);
+      if (lane == 0) sh.i0 = col;
+    }
+    __syncthreads();
+    const int col = sh.i0;
+    __syncthreads();
+    return col;
+  }
+
+  // ---- histograms of weight ----
 
   __device__ __forceinline__ int bin_of(float z) const {
     const double q = -4.0 * t2(z);
@@ -493,19 +661,19 @@ struct RowWork {
 
   // Histogram `to`: the words of [lo, hi] by bins of a quarter power of two of weight (top = 0), or by the bits of their
   // keys below `top`, `shift` bits to a bin.  Weights relative to the bin's top, in 2^-44, then in units of the row's.
-  __device__ __forceinline__ void histogram(int to, float lo, float hi, uint32_t top, int shift) {
+  __device__ __forceinline__ void histogram(int to, float lo, float hi, uint32_t top, int shift) const {
     const int tid = threadIdx.x, colm = tid & (kCols - 1);
-    for (int i = tid; i < kBins * kCols; i += kNT) {
+    for (int i = tid; i < kBins * kCols; i += NT) {
       sh.h.mass[i] = 0ull;
       sh.h.count[i] = 0u;
     }
     __syncthreads();
     const double t_top = top ? t2(key_value(top)) : 0.0;
-    for (int tile = tid >> 6; tile < tiles; tile += kNW) {
-      if (sh.tmax[tile] < lo) continue;
+    for (int tile = tid >> 6; tile < tiles; tile += NW) {
+      if (rec.max[tile] < lo) continue;
       each_vector(tile, [&](const u32x4& x, int) {
 #pragma unroll
-        for (int e = 0; e < Tile<Tin>::EPV; ++e) {
+        for (int e = 0; e < EPV; ++e) {
           const float z = elem<Tin>(x, e);
           if (z >= lo && z <= hi) {
             const double t = t2(z);
@@ -528,23 +696,25 @@ struct RowWork {
     }
     __syncthreads();
     // four threads to a bin, eight columns each
-    static_assert(kNT == 4 * kBins && kCols == 32, "threads to bins");
+    static_assert(NT >= 4 * kBins && kCols == 32, "threads to bins");
     const int b = tid >> 2, q = (tid & 3) * (kCols / 4);
-    double mass = 0.0;
-    int count = 0;
+    if (b < kBins) {
+      double mass = 0.0;
+      int count = 0;
 #pragma unroll
-    for (int i = 0; i < kCols / 4; ++i) {
-      const int at = b * kCols + q + ((i + (tid >> 2)) & (kCols / 4 - 1));
-      mass += (double)sh.h.mass[at] * 0x1p-44;
-      count += (int)sh.h.count[at];
-    }
-    mass += __shfl_xor(mass, 1, 64);
-    mass += __shfl_xor(mass, 2, 64);
-    count += __shfl_xor(count, 1, 64);
-    count += __shfl_xor(count, 2, 64);
-    if ((tid & 3) == 0) {
-      sh.bin_mass[to][b] = mass * exp2_neg(top ? t_top : -0.25 * b);
-      sh.bin_count[to][b] = count;
+      for (int i = 0; i < kCols / 4; ++i) {
+        const int at = b * kCols + q + ((i + (tid >> 2)) & (kCols / 4 - 1));
+        mass += (double)sh.h.mass[at] * 0x1p-44;
+        count += (int)sh.h.count[at];
+      }
+      mass += __shfl_xor(mass, 1, 64);
+      mass += __shfl_xor(mass, 2, 64);
+      count += __shfl_xor(count, 1, 64);
+      count += __shfl_xor(count, 2, 64);
+      if ((tid & 3) == 0) {
+        sh.bin_mass[to][b] = mass * exp2_neg(top ? t_top : -0.25 * b);
+        sh.bin_count[to][b] = count;
+      }
     }
     __syncthreads();
   }
@@ -552,7 +722,7 @@ struct RowWork {
   // The first bin of histogram `of` up to which count0 (mass0) and the bins' counts (masses) reach the target, or the
   // last one that holds a word; count0 and mass0 then end before it.
   __device__ __forceinline__ int find_bin(int of, bool by_mass, int& count0, double& mass0, int k, double target,
-                                          int& in_bin) {
+                                          int& in_bin) const {
     const int tid = threadIdx.x, lane = tid & 63;
     if (tid < 64) {
       const int c0 = sh.bin_count[of][2 * lane], c1 = sh.bin_count[of][2 * lane + 1];
@@ -581,72 +751,8 @@ struct RowWork {
     return b;
   }
 
-  // Wave 0: the tile's r-th word (from 1) that equals z, by index.
-  __device__ __forceinline__ int nth_equal(int tile, float z, int r) {
-    int found = 0;
-    each_vector(tile, [&](const u32x4& x, int j) {
-      int n = 0;
-#pragma unroll
-      for (int e = 0; e < Tile<Tin>::EPV; ++e) n += elem<Tin>(x, e) == z;
-      const int incl = scan_add(n);
-      const int all = __builtin_amdgcn_readlane(incl, 63);
-      if (r >= 1 && r <= all) {
-        const int l = __ffsll((unsigned long long)__ballot(incl >= r)) - 1;
-        int left = r - (incl - n), col = 0;
-#pragma unroll
-        for (int e = 0; e < Tile<Tin>::EPV; ++e) {
-          const bool same = elem<Tin>(x, e) == z;
-          left -= same;
-          if (left == 0 && same) col = Tile<Tin>::col(tile, j, e);
-        }
-        found = __builtin_amdgcn_readlane(col, l);
-      }
-      r -= all;
-    });
-    return found;
-  }
-
-  // The index of the r-th word of the row that equals z.
-  __device__ __forceinline__ int tie_index(float z, int r) {
-    const int tid = threadIdx.x;
-    for (int tile = tid >> 6; tile < tiles; tile += kNW) {
-      int n = 0;
-      if (sh.tmax[tile] >= z) {
-        Tile<Tin> x;
-        x.load(row, V, tile);
-#pragma unroll
-        for (int j = 0; j < Tile<Tin>::NV; ++j)
-#pragma unroll
-          for (int e = 0; e < Tile<Tin>::EPV; ++e) n += __popcll(__ballot(x.at(j, e) == z));
-      }
-      if ((tid & 63) == 0) sh.tcount[tile] = n;
-    }
-    __syncthreads();
-    if (tid < 64) {
-      int left = r, at = -1;
-      for (int i0 = 0; i0 < tiles && at < 0; i0 += 64) {
-        const int n = i0 + tid < tiles ? sh.tcount[i0 + tid] : 0;
-        const int incl = scan_add(n);
-        const uint64_t mask = __ballot(incl >= left);
-        if (mask) {
-          const int l = __ffsll((unsigned long long)mask) - 1;
-          left -= __builtin_amdgcn_readlane(incl - n, l);
-          at = i0 + l;
-        } else {
-          left -= __builtin_amdgcn_readlane(incl, 63);
-        }
-      }
-      const int col = at < 0 ? V : nth_equal(at, z, left);
-      if (tid == 0) sh.i0 = col;
-    }
-    __syncthreads();
-    const int col = sh.i0;
-    __syncthreads();
-    return col;
-  }
-
   // The cut after the k-th word, or after the shortest prefix of weight `target`, from histogram 0.
-  __device__ __forceinline__ Cut select(bool by_mass, int k, double target) {
+  __device__ __forceinline__ Cut select(bool by_mass, int k, double target) const {
     int count0 = 0, cnt;
     double mass0 = 0.0;
     const int b = find_bin(0, by_mass, count0, mass0, k, target, cnt);
@@ -680,11 +786,15 @@ struct RowWork {
       else if (w > 0.0) r = (int)fmin(ceil((target - mass0) / w), (double)cnt);
       r = max(1, min(r, cnt));
       cut.mass = mass0 + (double)r * w;
-      cut.tie = r == cnt ? V : tie_index(cut.thr, r);
+      cut.tie = V;
+      if (r < cnt) {
+        count_equal(cut.thr);
+        cut.tie = tie_index(cut.thr, r);
+      }
       return cut;
     }
     const int n = gather(key_value(klo), key_value(khi));
-    sort_list(sh, n);
+    sort_list(n);
     scan_list(n, mass0);
     const int r = by_mass ? first_reaching(n, target) : max(1, min(k - count0, n));
     cut.thr = list_value(r - 1);
@@ -694,18 +804,236 @@ struct RowWork {
     return cut;
   }
 
-  __device__ __forceinline__ bool kept(float z, int col, float thr, int tie) const {
-    return z > thr || (z == thr && col <= tie);
+  // rec.sum = the tiles' kept weights; their sum, and the number of kept words.
+  __device__ __forceinline__ double kept_sums(float thr, int tie, int& n) const {
+    const int lane = threadIdx.x & 63;
+    int here = 0;
+    for (int tile = threadIdx.x >> 6; tile < tiles; tile += NW) {
+      double s = 0.0;
+      if (rec.max[tile] >= thr) {
+        each_vector(tile, [&](const u32x4& x, int j) {
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) {
+            const float z = elem<Tin>(x, e);
+            if (kept(z, Tile<Tin>::col(tile, j, e), thr, tie)) {
+              s += weight(z);
+              ++here;
+            }
+          }
+        });
+        s = wave_sum_dpp(s);
+      }
+      if (lane == 0) rec.sum[tile] = s;
+    }
+    __syncthreads();
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < tiles; i += NT) sum += rec.sum[i];
+    sum = block_sum(sum);
+    n = block_sum(here);
+    return sum;
   }
 
+  // ---- the count of bf16 values ----
+
+  // The row's cut from the count of each value, S and the number of kept words, and with `sums` the tiles' kept weights
+  // in rec.sum.  False where the cut falls among the words of bin kMid, which are not told apart.
+  __device__ __forceinline__ bool by_value(bool k_on, int k, bool p_on, double p, float z_min, bool sums, float& thr_out,
+                                           int& tie_out, int& n_out, double& S_out) const {
+    constexpr int kEach = (kValues + NT - 1) / NT;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const double mid_top = t2(bin_value(kMid + 1));
+    // f(word) for a tile's words of bin kMid: 1 in 80,000 of normal logits, so in a pass of its own
+    auto each_mid = [&](int tile, u16x2 least, auto f) {
+      if (!__any(least.x == 0 || least.y == 0)) return;
+      each_vector(tile, [&](const u32x4& x, int) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+          if (fabsf(elem<Tin>(x, e)) < bin_value(kMid + 1)) f(elem<Tin>(x, e));
+      });
+    };
+    for (int i = tid; i < kValues; i += NT) sh.v.count[i] = 0u;
+    if (tid == 0) sh.v.mid = 0ull;
+    __syncthreads();
+    each_tile([](int) { return true; },
+              [&](const Tile<Tin>& x, int tile) {
+                u16x2 least = (u16x2)(unsigned short)1;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                  for (int q = 0; q < 4; ++q) {
+                    const s16x2 b = value_bins(x.v[j][q], least);
+                    atomicAdd(&sh.v.count[kMid + b.x], 1u);
+                    atomicAdd(&sh.v.count[kMid + b.y], 1u);
+                  }
+                each_mid(tile, least, [&](float z) {
+                  const double y = exp2_neg(fmin(t2(z) - mid_top, 0.0)) + 256.0;
+                  atomicAdd(&sh.v.mid, __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
+                });
+              });
+    __syncthreads();
+    // each thread kEach bins, from the largest value down; the last one holds the masked words
+    const double mid = (double)sh.v.mid * 0x1p-44 * exp2_neg(mid_top);
+    auto bin_at = [&](int i) { return kValues - 1 - (tid * kEach + i); };
+    int cn = 0;
+    double cm = 0.0;
+    for (int i = 0; i < kEach; ++i) {
+      const int b = bin_at(i);
+      if (b < 1) continue;
+      const int q = (int)sh.v.count[b];
+      const double w = q > 0 && b != kMid ? weight(bin_value(b)) : 0.0;
+      sh.v.weight[b] = w;
+      cn += q;
+      cm += b == kMid ? mid : (double)q * w;
+    }
+    const int my_n = cn;
+    const double my_m = cm;
+    int all_n;
+    double all_m;
+    block_scan(cn, cm, all_n, all_m);
+    const int n0 = cn - my_n;
+    const double m0 = cm - my_m;
+    // the first bin up to which the counts (weights) reach the target
+    auto find = [&](bool by_mass, int k_, double target, int& count0, double& mass0) {
+      if (tid == 0) sh.bin = -1;
+      const int first = block_min(my_n > 0 && (by_mass ? m0 + my_m >= target : n0 + my_n >= k_) ? tid : INT_MAX);
+      if (tid == (first == INT_MAX ? 0 : first)) {
+        int a = n0;
+        double w = m0;
+        for (int i = 0; i < kEach; ++i) {
+          const int b = bin_at(i);
+          if (b < 1 || sh.v.count[b] == 0) continue;
+          const double q = b == kMid ? mid : (double)sh.v.count[b] * sh.v.weight[b];
+          sh.bin = b;  // the last one with a word, where rounding leaves the target above them
+          sh.i0 = a;
+          sh.d0 = w;
+          if (by_mass ? w + q >= target : a + (int)sh.v.count[b] >= k_) break;
+          a += (int)sh.v.count[b];
+          w += q;
+        }
+      }
+      __syncthreads();
+      const int b = first == INT_MAX ? -1 : sh.bin;
+      count0 = sh.i0;
+      mass0 = sh.d0;
+      __syncthreads();
+      return b;
+    };
+    int n = all_n;
+    double S = all_m;
+    float thr = kLiveMin;
+    int r = 0, cnt = 0;  // of the cut's value, r words of cnt are kept (0: all)
+    if (k_on && k < all_n) {
+      int count0;
+      double mass0;
+      const int b = find(false, k, 0.0, count0, mass0);
+      if (b <= 0 || b == kMid) return false;
+      thr = bin_value(b);
+      cnt = (int)sh.v.count[b];
+      r = k - count0;
+      n = k;
+      S = mass0 + (double)r * sh.v.weight[b];
+    }
+    if (p_on) {
+      const double target = p * S;
+      int count0;
+      double mass0;
+      const int b = find(true, 0, target, count0, mass0);
+      if (b == kMid) return false;
+      if (b > 0) {
+        const double w = sh.v.weight[b];
+        const int have = (int)sh.v.count[b];
+        const int need = w > 0.0 ? max(1, (int)fmin(ceil((target - mass0) / w), (double)have)) : have;
+        if (count0 + need < n) {
+          thr = bin_value(b);
+          cnt = have;
+          r = need;
+          n = count0 + need;
+          S = mass0 + (double)need * w;
+        }
+      }
+    }
+    if (z_min > thr) {
+      if (fabsf(z_min) < bin_value(kMid + 1)) return false;
+      int qn = 0;
+      double qm = 0.0;
+      for (int i = 0; i < kEach; ++i) {
+        const int b = bin_at(i);
+        if (b < 1 || !(bin_value(b) >= z_min)) continue;
+        qn += (int)sh.v.count[b];
+        qm += b == kMid ? mid : (double)sh.v.count[b] * sh.v.weight[b];
+      }
+      n = block_sum(qn);
+      S = block_sum(qm);
+      thr = z_min;
+      cnt = r = 0;
+    }
+    const bool partial = r < cnt;
+    thr_out = thr;
+    tie_out = V;
+    n_out = n;
+    S_out = S;
+    if (!sums) {
+      if (partial) {
+        count_equal(thr);
+        tie_out = tie_index(thr, r);
+      }
+      return true;
+    }
+    // the tiles' kept weights: a table of them, 0 below the cut, the cut's own value apart where it is kept in part
+    const double w_thr = weight(thr);
+    __syncthreads();
+    for (int i = 0; i < kEach; ++i) {
+      const int b = bin_at(i);
+      if (b >= 0 && (b < 1 || (b != kMid && !(partial ? bin_value(b) > thr : bin_value(b) >= thr)))) sh.v.weight[b] = 0.0;
+    }
+    const bool mid_kept = 0.f >= thr;
+    __syncthreads();
+    for (int i = tid; i < tiles; i += NT)
+      if (!(rec.max[i] >= thr)) {
+        rec.sum[i] = 0.0;
+        rec.count[i] = 0;
+      }
+    each_tile([&](int tile) { return rec.max[tile] >= thr; },
+              [&](const Tile<Tin>& x, int tile) {
+                double s = 0.0;
+                int same = 0;
+                u16x2 least = (u16x2)(unsigned short)1;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                  for (int q = 0; q < 4; ++q) {
+                    const s16x2 b = value_bins(x.v[j][q], least);
+                    s += sh.v.weight[kMid + b.x];
+                    s += sh.v.weight[kMid + b.y];
+                    if (partial)
+                      same += __popcll(__ballot(bf16_lo(x.v[j][q]) == thr)) + __popcll(__ballot(bf16_hi(x.v[j][q]) == thr));
+                  }
+                if (mid_kept) each_mid(tile, least, [&](float z) { s += weight(z); });
+                s = wave_sum_dpp(s);
+                if (lane == 0) {
+                  rec.sum[tile] = s;
+                  rec.count[tile] = same;
+                }
+              });
+    __syncthreads();
+    if (partial) {
+      tie_out = tie_index(thr, r);
+      for (int i = tid; i < tiles; i += NT) rec.sum[i] += (double)rec.count[i] * w_thr;
+      __syncthreads();
+    }
+    return true;
+  }
+
+  // ---- draws ----
+
   // Wave 0: the tile's first kept word at which the kept weights pass `left`, or its last kept word.
-  __device__ __forceinline__ int pick(int tile, double left, float thr, int tie) {
+  __device__ __forceinline__ int pick(int tile, double left, float thr, int tie) const {
     int found = -1, last = -1;
     each_vector(tile, [&](const u32x4& x, int j) {
-      double w[Tile<Tin>::EPV], s = 0.0;
+      double w[EPV], s = 0.0;
       int mine = -1;
 #pragma unroll
-      for (int e = 0; e < Tile<Tin>::EPV; ++e) {
+      for (int e = 0; e < EPV; ++e) {
         const float z = elem<Tin>(x, e);
         const int col = Tile<Tin>::col(tile, j, e);
         w[e] = kept(z, col, thr, tie) ? weight(z) : 0.0;
@@ -719,7 +1047,7 @@ struct RowWork {
         double run = excl;
         int col = -1;
 #pragma unroll
-        for (int e = 0; e < Tile<Tin>::EPV; ++e) {
+        for (int e = 0; e < EPV; ++e) {
           run += w[e];
           if (col < 0 && w[e] > 0.0 && run > left) col = Tile<Tin>::col(tile, j, e);
         }
@@ -733,19 +1061,19 @@ struct RowWork {
     return found >= 0 ? found : last;
   }
 
-  // The first kept word at which the kept weights pass u times their sum, from the tiles' sums in sh.tsum.
-  __device__ __forceinline__ int draw(double target, float thr, int tie) {
+  // The first kept word at which the kept weights pass `target`, from the tiles' sums in rec.sum.
+  __device__ __forceinline__ int draw(double target, float thr, int tie) const {
     double before = 0.0;
     int at = INT_MAX, last = -1;
-    for (int i0 = 0; i0 < tiles && at == INT_MAX; i0 += kNT) {
+    for (int i0 = 0; i0 < tiles && at == INT_MAX; i0 += NT) {
       const int i = i0 + threadIdx.x;
-      const double v = i < tiles ? sh.tsum[i] : 0.0;
+      const double v = i < tiles ? rec.sum[i] : 0.0;
       double total;
-      const double incl = before + block_scan(sh, v, total);
+      const double incl = before + block_scan(v, total);
       const bool here = v > 0.0 && incl > target;
-      at = block_min_int(sh, here ? i : INT_MAX);
+      at = block_min(here ? i : INT_MAX);
       if (i == at) sh.d0 = target - (incl - v);
-      last = max(last, block_max_int(sh, v > 0.0 ? i : -1));
+      last = max(last, block_max(v > 0.0 ? i : -1));
       before += total;
     }
     __syncthreads();
@@ -758,8 +1086,10 @@ struct RowWork {
     return sh.i0;
   }
 
+  // ---- bounds ----
+
   // A lower bound of the k-th largest of the n partial maxima in sh.sub, and so of the row's k-th word.
-  __device__ __forceinline__ float kth_bound(int n, int k) {
+  __device__ __forceinline__ float kth_bound(int n, int k) const {
     if (threadIdx.x < 64) {
       const int lane = threadIdx.x;
       uint32_t key[kMaxSubs / 64];
@@ -791,9 +1121,12 @@ struct RowWork {
   }
 };
 
-template <typename Tin, bool FUSED, bool DRAW>
-__global__ __launch_bounds__(kNT) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_sample_row(const RowArgs a, int row0) {
+template <typename Tin, bool FUSED, bool DRAW, int NT>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_sample_row(const RowArgs a, int row0) {
   __shared__ RowShared sh;
+  extern __shared__ double tile_mem[];
+  typedef RowWork<Tin, NT> Work;
+  constexpr int NW = NT / 64;
   const int t = row0 + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const Tin* row = static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld;
   const Settings st = load_settings(a.par, t);
@@ -810,28 +1143,33 @@ __global__ __launch_bounds__(kNT) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
   const bool k_on = st.k > 0 && st.k < a.V, p_on = st.p < 1.f, m_on = st.min_p > 0.f;
   const int subs = a.tiles * kSubs <= kMaxSubs ? a.tiles * kSubs : a.tiles <= kMaxSubs ? a.tiles : 0;
   const bool fine = a.tiles * kSubs <= kMaxSubs;
+  const RowTiles rec{tile_mem, reinterpret_cast<float*>(tile_mem + a.tiles),
+                     reinterpret_cast<int*>(tile_mem + a.tiles) + a.tiles};
+  Work w{sh, rec, row, a.V, a.tiles, 0.f, st.c, kLiveMin};
 
   // the tiles' records
-  float m = -INFINITY;
-  int live = 0, bad = 0;
+  float m = -INFINITY, lo = INFINITY;
+  int live = 0;
+  bool bad = false;
+  const SumMode mode = sum_mode(st, a.V, DRAW, FUSED);
   if (FUSED) {
-    const SumMode mode = sum_mode(st, a.V, DRAW);
-    for (int tile = wv; tile < a.tiles; tile += kNW) {
-      Tile<Tin> x;
-      x.load(row, a.V, tile);
-      const TileStats s = tile_stats<Tin>(x, mode, st.c);
-      if (fine && (lane & 7) == 0) sh.sub[tile * kSubs + (lane >> 3)] = s.sub;
-      if (lane == 0) {
-        if (!fine && subs) sh.sub[tile] = s.max;
-        sh.tsum[tile] = s.sum;
-        sh.tmax[tile] = s.max;
-        live += s.live;
-      }
-      m = fmaxf(m, s.max);
-      bad |= s.bad;
-    }
+    w.each_tile([](int) { return true; },
+                [&](const Tile<Tin>& x, int tile) {
+                  const TileStats s = tile_stats<Tin>(x, mode, st.c);
+                  if (fine && (lane & 7) == 0) sh.sub[tile * kSubs + (lane >> 3)] = s.sub;
+                  if (lane == 0) {
+                    if (!fine && subs) sh.sub[tile] = s.max;
+                    rec.sum[tile] = s.sum;
+                    rec.max[tile] = s.max;
+                  }
+                  live += s.live;
+                  m = fmaxf(m, s.max);
+                  lo = fminf(lo, s.lo);
+                  bad |= s.bad;
+                });
+    if (lane != 0) live = 0;
   } else {
-    for (int i = tid; i < a.tiles; i += kNT) {
+    for (int i = tid; i < a.tiles; i += NT) {
       const TileRec r = a.recs[(int64_t)t * a.tiles + i];
       float mx = r.sub[0];
 #pragma unroll
@@ -842,17 +1180,38 @@ __global__ __launch_bounds__(kNT) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
       } else if (subs) {
         sh.sub[i] = mx;
       }
-      sh.tsum[i] = r.sum;
-      sh.tmax[i] = mx;
+      rec.sum[i] = r.sum;
+      rec.max[i] = mx;
       live += r.live;
-      bad |= r.bad;
       m = fmaxf(m, mx);
+      lo = fminf(lo, r.lo);
+      bad |= r.bad != 0;
     }
   }
-  __syncthreads();
-  live = block_sum_int(sh, live);
-  bad = block_max_int(sh, bad);
-  m = key_value((uint32_t)block_max_int(sh, (int)(order_key(m) ^ 0x80000000u)) ^ 0x80000000u);
+  {  // over the workgroup, together
+    m = wave_max_dpp(m);
+    lo = -wave_max_dpp(-lo);
+    live = __builtin_amdgcn_readlane(scan_add(live), 63);
+    const bool any_bad = __any(bad);
+    if (lane == 0) {
+      sh.wf[0][wv] = m;
+      sh.wf[1][wv] = lo;
+      sh.wi[0][wv] = live;
+      sh.wi[1][wv] = any_bad;
+    }
+    __syncthreads();
+    live = 0;
+    bad = false;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      m = fmaxf(m, sh.wf[0][i]);
+      lo = fminf(lo, sh.wf[1][i]);
+      live += sh.wi[0][i];
+      bad |= sh.wi[1][i] != 0;
+    }
+    __syncthreads();
+  }
+  w.m = m;
 
   grpo_sampling_row out;
   out.max = m;
@@ -870,18 +1229,18 @@ __global__ __launch_bounds__(kNT) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
   } else if (live == 0) {
     flag = GRPO_FLAG_NONFINITE;
   } else {
-    RowWork<Tin> w{sh, row, a.V, a.tiles, m, st.c, kLiveMin};
     float thr = -1e8f;  // kept: above it
     int tie = -1, n = live;
     double S = 0.0;
+    bool drawn = !DRAW;
     if (st.greedy) {
       int first = INT_MAX;
-      for (int i = tid; i < a.tiles; i += kNT)
-        if (sh.tmax[i] == m) {
+      for (int i = tid; i < a.tiles; i += NT)
+        if (rec.max[i] == m) {
           first = i;
           break;
         }
-      first = block_min_int(sh, first);
+      first = w.block_min(first);
       if (wv == 0) {
         const int col = w.nth_equal(first, m, 1);
         if (lane == 0) sh.i0 = col;
@@ -892,43 +1251,55 @@ __global__ __launch_bounds__(kNT) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
       n = 1;
       S = 1.0;
       if (DRAW) act = tie;
+      drawn = true;
     } else {
-      // the tiles' sums relative to the row's maximum
-      double total = 0.0;
-      for (int i = tid; i < a.tiles; i += kNT) {
-        const double v = sh.tmax[i] >= kLiveMin ? sh.tsum[i] * w.weight(sh.tmax[i]) : 0.0;
-        sh.tsum[i] = v;
-        total += v;
+      if (mode != kNoSum) {  // the tiles' sums relative to the row's maximum
+        double total = 0.0;
+        for (int i = tid; i < a.tiles; i += NT) {
+          const double v = rec.max[i] >= kLiveMin ? rec.sum[i] * w.weight(rec.max[i]) : 0.0;
+          rec.sum[i] = v;
+          total += v;
+        }
+        S = w.block_sum(total);
       }
-      S = block_sum(sh, total);
-      bool drawn = !DRAW;
       if (k_on || p_on || m_on) {
         const int k = min(st.k, live);
-        const float z_min = m_on ? w.min_p_bound(log2((double)st.min_p)) : kLiveMin;
-        float x_lo = k_on && p_on ? kLiveMin : fmaxf(z_min, kLiveMin);  // top-p of top-k needs the first k words' sum
+        const double p = (double)st.p;
+        const float z_min = m_on ? fmaxf(w.min_p_bound(log2((double)st.min_p)), kLiveMin) : kLiveMin;
+        float x_lo = k_on && p_on ? kLiveMin : z_min;  // top-p of top-k needs the first k words' sum
         if (k_on && k <= subs) x_lo = fmaxf(x_lo, w.kth_bound(subs, k));
         if (p_on && !k_on) {
-          // all words lighter than (1 - p) S / live together weigh less than (1 - p) S
-          const double l = log2((double)live / ((1.0 - (double)st.p) * S)) + 0.01;
+          // all words lighter than (1 - p) S / live together weigh less than (1 - p) S; 0.01 covers S's error
+          const double l = log2((double)live / ((1.0 - p) * S)) + 0.01;
           const double z = (double)m - l / st.c;
           float zf = fminf((float)z, m);
           if ((double)zf > z) zf = nextafterf(zf, -INFINITY);
           x_lo = fmaxf(x_lo, zf);
         }
         w.x_lo = x_lo;
-        const int listed = w.gather(x_lo, INFINITY);
+        int listed = x_lo > kLiveMin || live <= kCap ? w.gather(x_lo, INFINITY) : live;
         if (listed <= kCap) {
-          sort_list(sh, listed);
+          w.sort_list(listed);
           w.scan_list(listed, 0.0);
           n = k_on ? min(k, listed) : listed;
           if (p_on) {
-            const double Sk = k_on ? sh.l.cum[n - 1] : S;
-            n = min(n, w.first_reaching(listed, (double)st.p * Sk));
+            int np;
+            if (k_on || mode == kSum64) {
+              np = w.first_reaching(listed, p * (k_on ? sh.l.cum[n - 1] : S));
+            } else {
+              np = w.first_reaching(listed, p * (S * (1.0 - kSum32Error)));
+              if (np != w.first_reaching(listed, p * (S * (1.0 + kSum32Error)))) {
+                int all;
+                S = w.kept_sums(kLiveMin, a.V, all);
+                np = w.first_reaching(listed, p * S);
+              }
+            }
+            n = min(n, np);
           }
           if (m_on) {
             int c = 0;
-            for (int i = tid; i < listed; i += kNT) c += w.list_value(i) >= z_min;
-            n = min(n, block_sum_int(sh, c));
+            for (int i = tid; i < listed; i += NT) c += w.list_value(i) >= z_min;
+            n = min(n, w.block_sum(c));
           }
           n = max(n, 1);
           thr = w.list_value(n - 1);
@@ -937,72 +1308,60 @@ __global__ __launch_bounds__(kNT) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
           __syncthreads();
           if (DRAW) {
             // the kept words in the order of their indices, smallest first: keys that fall as the index grows
-            for (int i = tid; i < n; i += kNT) {
+            for (int i = tid; i < n; i += NT) {
               const unsigned long long q = sh.l.key[i];
               sh.l.key[i] = (q << 32) | (q >> 32);
             }
             __syncthreads();
-            sort_list(sh, n);
+            w.sort_list(n);
             double before = 0.0;
             int at = INT_MAX, last = 0;
             const double target = (double)u * S;
-            for (int i0 = 0; i0 < n && at == INT_MAX; i0 += kNT) {
+            for (int i0 = 0; i0 < n && at == INT_MAX; i0 += NT) {
               const int i = i0 + tid;
               const double v = i < n ? w.weight(key_value((uint32_t)sh.l.key[i])) : 0.0;
               double all;
-              const double incl = before + block_scan(sh, v, all);
-              at = block_min_int(sh, v > 0.0 && incl > target ? i : INT_MAX);
-              last = max(last, block_max_int(sh, v > 0.0 ? i : 0));
+              const double incl = before + w.block_scan(v, all);
+              at = w.block_min(v > 0.0 && incl > target ? i : INT_MAX);
+              last = max(last, w.block_max(v > 0.0 ? i : 0));
               before += all;
             }
             act = (int)~(uint32_t)(sh.l.key[at == INT_MAX ? last : at] >> 32);
             drawn = true;
           }
         } else {
-          thr = kLiveMin;
-          tie = a.V;
-          auto narrow = [&](float z, int i) {
-            if (z > thr || (z == thr && i < tie)) {
-              thr = z;
-              tie = i;
-            }
-          };
-          if (k_on || p_on) {
-            w.histogram(0, x_lo, INFINITY, 0u, 0);
-            double Sk = S;
+          bool done = false;
+          if constexpr (Work::kByValue) {
+            if (m < kLimit && lo > -kLimit) done = w.by_value(k_on, k, p_on, p, z_min, DRAW, thr, tie, n, S);
+          }
+          if (!done) {
+            thr = kLiveMin;
+            tie = a.V;
+            auto narrow = [&](float z, int i) {
+              if (z > thr || (z == thr && i < tie)) {
+                thr = z;
+                tie = i;
+              }
+            };
+            if (k_on || p_on) {
+              if (p_on && !k_on && mode != kSum64) {  // S from the histogram: all live words
+                x_lo = kLiveMin;
+                w.x_lo = x_lo;
+              }
+              w.histogram(0, x_lo, INFINITY, 0u, 0);
+              double Sk = S;
+              if (p_on && !k_on && mode != kSum64) Sk = w.block_sum(tid < kBins ? sh.bin_mass[0][tid] : 0.0);
 #pragma unroll 1
-            for (int by_mass = 0; by_mass < 2; ++by_mass) {
-              if (by_mass ? !p_on : !k_on) continue;
-              const Cut cut = w.select(by_mass, k, (double)st.p * Sk);
-              narrow(cut.thr, cut.tie);
-              Sk = cut.mass;
+              for (int by_mass = 0; by_mass < 2; ++by_mass) {
+                if (by_mass ? !p_on : !k_on) continue;
+                const Cut cut = w.select(by_mass, k, p * Sk);
+                narrow(cut.thr, cut.tie);
+                Sk = cut.mass;
+              }
             }
+            if (m_on) narrow(z_min, a.V);
+            S = w.kept_sums(thr, tie, n);
           }
-          if (m_on) narrow(z_min, a.V);
-          // the kept words' sums, tile by tile in the order of the indices
-          int kept_here = 0;
-          for (int tile = wv; tile < a.tiles; tile += kNW) {
-            double s = 0.0;
-            if (sh.tmax[tile] >= thr) {
-              w.each_vector(tile, [&](const u32x4& x, int j) {
-#pragma unroll
-                for (int e = 0; e < Tile<Tin>::EPV; ++e) {
-                  const float z = elem<Tin>(x, e);
-                  if (w.kept(z, Tile<Tin>::col(tile, j, e), thr, tie)) {
-                    s += w.weight(z);
-                    ++kept_here;
-                  }
-                }
-              });
-              s = wave_sum_dpp(s);
-            }
-            if (lane == 0) sh.tsum[tile] = s;
-          }
-          __syncthreads();
-          double sum = 0.0;
-          for (int i = tid; i < a.tiles; i += kNT) sum += sh.tsum[i];
-          S = block_sum(sh, sum);
-          n = block_sum_int(sh, kept_here);
         }
       }
       if (!drawn) act = w.draw((double)u * S, thr, tie);
@@ -1129,7 +1488,12 @@ __global__ void k_clear_sampling_flag(int32_t* f) { *f = 0; }
 // ---- host -----------------------------------------------------------------------
 
 // Whether the tiles are reduced by a launch of their own.
-static bool split_rows(int64_t T, int64_t V) { return T < 192 && V > kNW * kTile; }
+static bool split_rows(int64_t T, int64_t V) { return T < 192 && V > 16384; }
+
+static int tile_count(int64_t V, bool bf16) {
+  const int words = bf16 ? Tile<uint16_t>::kWords : Tile<float>::kWords;
+  return (int)((V + words - 1) / words);
+}
 
 static int check_settings(const grpo_sampling* g) {
   if (!g) return GRPO_ERR_ARG;
@@ -1146,18 +1510,26 @@ static bool bad_shape(int64_t T, int64_t V, int64_t ld) {
   return T < 0 || T >= ((int64_t)1 << 31) || V < 1 || V > GRPO_SAMPLING_MAX_V || ld < V;
 }
 
+template <typename Tin, bool FUSED, bool DRAW>
+static void launch_row_kernel(const RowArgs& a, int64_t T, hipStream_t s) {
+  // one workgroup to a CU: twice the waves
+  const bool wide = T <= 256 && a.V > 16384;
+  const auto k = wide ? k_sample_row<Tin, FUSED, DRAW, 1024> : k_sample_row<Tin, FUSED, DRAW, 512>;
+  constexpr int64_t kRows = 1 << 20;  // a launch's threads stay below 2^32
+  for (int64_t r = 0; r < T; r += kRows)
+    hipLaunchKernelGGL(k, dim3((unsigned)std::min(kRows, T - r)), dim3(wide ? 1024 : 512),
+                       row_tile_bytes(a.tiles), s, a, (int)r);
+}
+
 template <typename Tin, bool DRAW>
 static void launch_rows(const RowArgs& a, int64_t T, hipStream_t s) {
   if (split_rows(T, a.V)) {
     const int waves = (int)T * a.tiles;
     hipLaunchKernelGGL(k_sample_tiles<Tin>, dim3((unsigned)(waves + 3) / 4), dim3(256), 0, s, a, waves, DRAW);
-    hipLaunchKernelGGL((k_sample_row<Tin, false, DRAW>), dim3((unsigned)T), dim3(kNT), 0, s, a, 0);
-    return;
+    launch_row_kernel<Tin, false, DRAW>(a, T, s);
+  } else {
+    launch_row_kernel<Tin, true, DRAW>(a, T, s);
   }
-  constexpr int64_t kRows = 1 << 20;  // a launch's threads stay below 2^32
-  for (int64_t r = 0; r < T; r += kRows)
-    hipLaunchKernelGGL((k_sample_row<Tin, true, DRAW>), dim3((unsigned)std::min(kRows, T - r)), dim3(kNT), 0, s, a,
-                       (int)r);
 }
 
 template <bool DRAW>
@@ -1178,7 +1550,7 @@ static int sample_call(const void* logits, int32_t dtype, int64_t T, int64_t V, 
   }
   if (flags) hipLaunchKernelGGL(k_clear_sampling_flag, dim3(1), dim3(1), 0, s, flags);
   if (T > 0) {
-    const RowArgs a{logits, ld,     (int)V, (int)((V + kTile - 1) / kTile), *par,  u, actions, actions_out,
+    const RowArgs a{logits, ld,     (int)V, tile_count(V, dtype == GRPO_BF16), *par,  u, actions, actions_out,
                     logp,   n_kept, rows,   flags, static_cast<TileRec*>(ws)};
     if (dtype == GRPO_BF16) launch_rows<uint16_t, DRAW>(a, T, s);
     else launch_rows<float, DRAW>(a, T, s);
@@ -1192,7 +1564,7 @@ using namespace grpo;
 
 extern "C" size_t grpo_sampling_workspace_bytes(int64_t T, int64_t V) {
   if (bad_shape(T, V, V)) return 0;
-  const size_t recs = split_rows(T, V) ? sizeof(TileRec) * (size_t)T * (size_t)((V + kTile - 1) / kTile) : 0;
+  const size_t recs = split_rows(T, V) ? sizeof(TileRec) * (size_t)T * (size_t)tile_count(V, false) : 0;
   return align_up(std::max(recs, (size_t)1));
 }
 

@@ -171,8 +171,8 @@ def test_strides_and_alignment(dtype, ld, offset):
 
 def test_large_vocabulary():
     """More tiles than have partial maxima, and more than have any."""
-    for V in (300_000, 2_200_000):
-        logits, z = make("peaked", 1, V, BF16, V)
+    for V, dtype in ((300_000, BF16), (2_200_000, BF16), (grpo.GRPO_SAMPLING_MAX_V, F32)):
+        logits, z = make("peaked", 1, V, dtype, V)
         for par in ({}, dict(top_k=30), dict(top_k=5000, top_p=0.9), dict(top_p=0.7)):
             check(logits, z, par, uniform(z, par, V), V)
 
