@@ -38,7 +38,8 @@ constexpr int kTileVecs = 4;       // a tile: 4 vectors of 16 bytes per lane, 2,
 constexpr int kSubs = 8;           // partial maxima of a tile, each over 8 lanes' words
 constexpr int kMaxSubs = 1280;     // partial maxima (or tiles' maxima) that bound the k-th largest word
 constexpr int kCap = 2048;         // words that are sorted in LDS
-constexpr int kBins = 128, kCols = 32;
+constexpr int kBins = 1024, kCols = 4;  // bins of 1/32 of a power of two of weight, each in kCols copies
+constexpr int kRankSort = 256;     // words that are sorted by counting
 constexpr int kMaxNW = 16;
 constexpr float kLimit = 64.f;     // logits that the count of values takes: below it in size
 constexpr float kLiveMin = -99999992.f;  // the smallest float above -1e8: the lowest live logit
@@ -151,12 +152,16 @@ __device__ __forceinline__ Settings load_settings(const grpo_sampling& g, int t)
   return s;
 }
 
-// How a tile's weights are summed: not at all, exactly enough for a cut or a draw (fp64), or for a log-prob alone, and for
-// a first estimate of a cut (fp32 terms, like the other log-probs of this library; off by less than kSum32Error).
-enum SumMode { kNoSum, kSum64, kSum32 };
+// How a tile's weights are summed: not at all, exactly enough for a cut or a draw (fp64), for a log-prob alone, and for a
+// first estimate of a cut (fp32 terms, like the other log-probs of this library; off by less than kSum32Error), or by
+// counting the row's values.
+enum SumMode { kNoSum, kSum64, kSum32, kCount };
 constexpr double kSum32Error = 1e-5;
-__device__ __forceinline__ SumMode sum_mode(const Settings& s, int V, bool draw, bool fused) {
-  if (!s.ok || s.greedy || (s.k > 0 && s.k < V)) return kNoSum;
+__device__ __forceinline__ SumMode sum_mode(const Settings& s, int V, bool draw, bool fused, bool by_value, int subs) {
+  if (!s.ok || s.greedy) return kNoSum;
+  const bool k_on = s.k > 0 && s.k < V;
+  if (fused && by_value && (k_on ? s.k > subs : s.p < 1.f)) return kCount;
+  if (k_on) return kNoSum;
   if (s.p < 1.f) return fused ? kSum32 : kSum64;
   if (s.min_p > 0.f) return kNoSum;
   return draw ? kSum64 : kSum32;
@@ -256,7 +261,7 @@ __device__ __forceinline__ TileStats tile_stats(const Tile<Tin>& x, SumMode mode
     lo = -wave_max_dpp(-mn);
   }
   s.lo = lo;
-  if (mode == kNoSum || s.bad || s.live == 0) return s;
+  if (mode == kNoSum || mode == kCount || s.bad || s.live == 0) return s;
   if (mode == kSum64) {
     const double m = (double)s.max;
     double sum = 0.0;
@@ -306,7 +311,7 @@ __global__ __launch_bounds__(256) void k_sample_tiles(const RowArgs a, int n_wav
   const Settings st = load_settings(a.par, t);
   Tile<Tin> x;
   x.load(static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld, a.V, tile);
-  const TileStats s = tile_stats<Tin>(x, sum_mode(st, a.V, draw, false), st.c);
+  const TileStats s = tile_stats<Tin>(x, sum_mode(st, a.V, draw, false, false, 0), st.c);
   TileRec* r = a.recs + w;
   if ((lane & 7) == 0) r->sub[lane >> 3] = s.sub;
   if (lane == 0) {
@@ -342,14 +347,17 @@ __device__ __forceinline__ float bin_value(int bin) {
 struct Cut {
   float thr;    // kept: z > thr, or z == thr and index <= tie
   int tie;
-  double mass;  // weight of the prefix that ends there
+  double mass;  // the prefix that ends there: its weight, its words
+  int count;
 };
 
 struct RowShared {
   union {
     struct {
-      unsigned long long mass[kBins * kCols];
+      unsigned long long mass[kBins * kCols];  // the list lies over it
       uint32_t count[kBins * kCols];
+      double bin_mass[kBins];
+      int bin_count[kBins];
     } h;
     struct {
       unsigned long long key[kCap];
@@ -362,9 +370,7 @@ struct RowShared {
     } v;
   };
   float sub[kMaxSubs];
-  double bin_mass[2][kBins];
-  int bin_count[2][kBins];
-  double wd[2][kMaxNW];
+  double wd[kMaxNW];
   int wi[2][kMaxNW];
   float wf[2][kMaxNW];
   // broadcast
@@ -396,11 +402,11 @@ struct RowWork {
   // ---- over the workgroup: the same value in every thread; two barriers each, so that `sh` may be reused ----
   __device__ __forceinline__ double block_sum(double v) const {
     v = wave_sum_dpp(v);
-    if ((threadIdx.x & 63) == 0) sh.wd[0][threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) sh.wd[threadIdx.x >> 6] = v;
     __syncthreads();
     double r = 0.0;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) r += sh.wd[0][i];
+    for (int i = 0; i < NW; ++i) r += sh.wd[i];
     __syncthreads();
     return r;
   }
@@ -432,7 +438,7 @@ struct RowWork {
     v = scan_add(v);
     if ((threadIdx.x & 63) == 63) {
       sh.wi[0][wv] = n;
-      sh.wd[0][wv] = v;
+      sh.wd[wv] = v;
     }
     __syncthreads();
     double before = 0.0;
@@ -446,7 +452,7 @@ struct RowWork {
         n_before = all_n;
       }
       all_n += sh.wi[0][i];
-      all_v += sh.wd[0][i];
+      all_v += sh.wd[i];
     }
     __syncthreads();
     n += n_before;
@@ -510,21 +516,32 @@ struct RowWork {
           return rec.max[tile] >= lo && __builtin_amdgcn_readfirstlane(*(volatile int*)&sh.n) <= kCap;
         },
         [&](const Tile<Tin>& x, int tile) {
+          int have[NV], all = 0;
 #pragma unroll
           for (int j = 0; j < NV; ++j) {
-            if (!__any(vec_max<Tin>(x.v[j], -INFINITY) >= lo)) continue;
+            have[j] = 0;
+            if (__any(vec_max<Tin>(x.v[j], -INFINITY) >= lo)) {
+#pragma unroll
+              for (int e = 0; e < EPV; ++e) have[j] += __popcll(__ballot(x.at(j, e) >= lo && x.at(j, e) <= hi));
+            }
+            all += have[j];
+          }
+          int at = 0;
+          if (lane == 0) at = atomicAdd(&sh.n, all);
+          at = __builtin_amdgcn_readfirstlane(at);
+          if (at + all > kCap) return;
+#pragma unroll
+          for (int j = 0; j < NV; ++j) {
+            if (have[j] == 0) continue;
 #pragma unroll
             for (int e = 0; e < EPV; ++e) {
               const float z = x.at(j, e);
               const bool in = z >= lo && z <= hi;
               const uint64_t mask = __ballot(in);
-              if (mask) {
-                int at = 0;
-                if (lane == 0) at = atomicAdd(&sh.n, __popcll(mask));
-                at = __builtin_amdgcn_readfirstlane(at) + (int)__popcll(mask & ((1ull << lane) - 1));
-                if (in && at < kCap)
-                  sh.l.key[at] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~x.col(tile, j, e);
-              }
+              if (in)
+                sh.l.key[at + (int)__popcll(mask & ((1ull << lane) - 1))] =
+                    ((unsigned long long)order_key(z) << 32) | (uint32_t)~x.col(tile, j, e);
+              at += __popcll(mask);
             }
           }
         });
@@ -534,10 +551,24 @@ struct RowWork {
     return n;
   }
 
-  // Sorts the n keys in sh.l.key, largest first, padded with zeros to a power of two.
+  // Sorts the n keys in sh.l.key, all different, largest first.
   __device__ __forceinline__ void sort_list(int n) const {
     const int tid = threadIdx.x;
-    int P = 2;
+    if (n <= kRankSort) {  // a word's place is the number of larger ones: kRanks threads count them for each
+      constexpr int kRanks = NT / kRankSort;
+      const int i = tid / kRanks;
+      const unsigned long long mine = i < n ? sh.l.key[i] : 0ull;
+      int rank = 0;
+      if (i < n)
+        for (int q = tid % kRanks; q < n; q += kRanks) rank += sh.l.key[q] > mine;
+#pragma unroll
+      for (int o = 1; o < kRanks; o <<= 1) rank += __shfl_xor(rank, o, 64);
+      __syncthreads();
+      if (i < n && tid % kRanks == 0) sh.l.key[rank] = mine;
+      __syncthreads();
+      return;
+    }
+    int P = 2 * kRankSort;  // a bitonic sort, padded with zeros
     while (P < n) P <<= 1;
     for (int i = n + tid; i < P; i += NT) sh.l.key[i] = 0ull;
     __syncthreads();
@@ -654,21 +685,26 @@ struct RowWork {
 
   // ---- histograms of weight ----
 
-  __device__ __forceinline__ int bin_of(float z) const {
-    const double q = -4.0 * t2(z);
+  static constexpr double kPerOctave = 32.0;
+  __device__ __forceinline__ int bin_of(double t) const {
+    const double q = -kPerOctave * t;
     return q < (double)(kBins - 1) ? (int)q : kBins - 1;
   }
 
-  // Histogram `to`: the words of [lo, hi] by bins of a quarter power of two of weight (top = 0), or by the bits of their
-  // keys below `top`, `shift` bits to a bin.  Weights relative to the bin's top, in 2^-44, then in units of the row's.
-  __device__ __forceinline__ void histogram(int to, float lo, float hi, uint32_t top, int shift) const {
-    const int tid = threadIdx.x, colm = tid & (kCols - 1);
+  // The words of [lo, hi] counted and weighed, by bins of 1/kPerOctave power of two of weight (top = 0), or by the bits of
+  // their keys below `top`, `shift` bits to a bin; into sh.h.bin_count and bin_mass.  Weights are added relative to the
+  // bin's top, in 2^-44.  The last bin by weight, which has no lower end and may hold most of a row, is added up in
+  // registers.
+  __device__ __forceinline__ void histogram(float lo, float hi, uint32_t top, int shift) const {
+    const int tid = threadIdx.x, copy = tid & (kCols - 1);
     for (int i = tid; i < kBins * kCols; i += NT) {
       sh.h.mass[i] = 0ull;
       sh.h.count[i] = 0u;
     }
     __syncthreads();
     const double t_top = top ? t2(key_value(top)) : 0.0;
+    int rest = 0;
+    double rest_mass = 0.0;
     for (int tile = tid >> 6; tile < tiles; tile += NW) {
       if (rec.max[tile] < lo) continue;
       each_vector(tile, [&](const u32x4& x, int) {
@@ -683,63 +719,72 @@ struct RowWork {
               b = min((int)((top - order_key(z)) >> shift), kBins - 1);
               rel = t - t_top;
             } else {
-              b = bin_of(z);
-              rel = fma((double)b, 0.25, t);
+              b = bin_of(t);
+              rel = b == kBins - 1 ? t : fma((double)b, 1.0 / kPerOctave, t);
             }
-            const double y = exp2_neg(fmin(rel, 0.0)) + 256.0;  // the weight in 2^-44 in the low bits
-            const unsigned long long w = __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull;
-            atomicAdd(&sh.h.mass[b * kCols + colm], w);
-            atomicAdd(&sh.h.count[b * kCols + colm], 1u);
+            const double r = exp2_neg(fmin(rel, 0.0));
+            if (!top && b == kBins - 1) {
+              ++rest;
+              rest_mass += r;
+            } else {
+              const double y = r + 256.0;  // the weight in 2^-44 in the low bits
+              atomicAdd(&sh.h.mass[b * kCols + copy], __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
+              atomicAdd(&sh.h.count[b * kCols + copy], 1u);
+            }
           }
         }
       });
     }
-    __syncthreads();
-    // four threads to a bin, eight columns each
-    static_assert(NT >= 4 * kBins && kCols == 32, "threads to bins");
-    const int b = tid >> 2, q = (tid & 3) * (kCols / 4);
-    if (b < kBins) {
+    rest = block_sum(rest);
+    rest_mass = block_sum(rest_mass);
+    for (int b = tid; b < kBins; b += NT) {
       double mass = 0.0;
       int count = 0;
 #pragma unroll
-      for (int i = 0; i < kCols / 4; ++i) {
-        const int at = b * kCols + q + ((i + (tid >> 2)) & (kCols / 4 - 1));
-        mass += (double)sh.h.mass[at] * 0x1p-44;
-        count += (int)sh.h.count[at];
+      for (int i = 0; i < kCols; ++i) {
+        mass += (double)sh.h.mass[b * kCols + i] * 0x1p-44;
+        count += (int)sh.h.count[b * kCols + i];
       }
-      mass += __shfl_xor(mass, 1, 64);
-      mass += __shfl_xor(mass, 2, 64);
-      count += __shfl_xor(count, 1, 64);
-      count += __shfl_xor(count, 2, 64);
-      if ((tid & 3) == 0) {
-        sh.bin_mass[to][b] = mass * exp2_neg(top ? t_top : -0.25 * b);
-        sh.bin_count[to][b] = count;
-      }
+      const bool last = !top && b == kBins - 1;
+      sh.h.bin_mass[b] = last ? rest_mass : mass * exp2_neg(top ? t_top : (double)b * (-1.0 / kPerOctave));
+      sh.h.bin_count[b] = last ? rest : count;
     }
     __syncthreads();
   }
 
-  // The first bin of histogram `of` up to which count0 (mass0) and the bins' counts (masses) reach the target, or the
-  // last one that holds a word; count0 and mass0 then end before it.
-  __device__ __forceinline__ int find_bin(int of, bool by_mass, int& count0, double& mass0, int k, double target,
-                                          int& in_bin) const {
-    const int tid = threadIdx.x, lane = tid & 63;
-    if (tid < 64) {
-      const int c0 = sh.bin_count[of][2 * lane], c1 = sh.bin_count[of][2 * lane + 1];
-      const double m0 = sh.bin_mass[of][2 * lane], m1 = sh.bin_mass[of][2 * lane + 1];
-      const int ce = scan_add(c0 + c1) - (c0 + c1) + count0;
-      double me = __shfl_up(scan_add(m0 + m1), 1, 64);
-      me = (lane == 0 ? 0.0 : me) + mass0;
-      const bool at0 = c0 > 0 && (by_mass ? me + m0 >= target : ce + c0 >= k);
-      const bool at1 = c1 > 0 && (by_mass ? me + m0 + m1 >= target : ce + c0 + c1 >= k);
-      const uint64_t any = __ballot(at0 || at1), held = __ballot(c0 + c1 > 0);
-      const int l = any ? __ffsll((unsigned long long)any) - 1 : 63 - __clzll((long long)(held | 1ull));
-      if (lane == l) {
-        const bool first = any ? at0 : c1 == 0;
-        sh.bin = 2 * lane + (first ? 0 : 1);
-        sh.i0 = first ? ce : ce + c0;
-        sh.d0 = first ? me : me + m0;
-        sh.n = first ? c0 : c1;
+  // The first bin up to which count0 (mass0) and the bins' counts (weights) reach the target, or the last one that holds a
+  // word; count0 and mass0 then end before it.
+  __device__ __forceinline__ int find_bin(bool by_mass, int& count0, double& mass0, int k, double target, int& in_bin) const {
+    constexpr int kEach = kBins / NT;
+    const int tid = threadIdx.x;
+    int n = 0, all_n;
+    double w = 0.0, all_w;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      n += sh.h.bin_count[tid * kEach + i];
+      w += sh.h.bin_mass[tid * kEach + i];
+    }
+    const int mine = n;
+    const double my_w = w;
+    block_scan(n, w, all_n, all_w);
+    n += count0;
+    w += mass0;
+    const int first = block_min(mine > 0 && (by_mass ? w >= target : n >= k) ? tid : INT_MAX);
+    const int at = first != INT_MAX ? first : block_max(mine > 0 ? tid : -1);
+    if (tid == at) {
+      n -= mine;
+      w -= my_w;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int b = tid * kEach + i, q = sh.h.bin_count[b];
+        if (q == 0) continue;
+        sh.bin = b;  // the last one with a word, where rounding leaves the target above them
+        sh.i0 = n;
+        sh.d0 = w;
+        sh.n = q;
+        n += q;
+        w += sh.h.bin_mass[b];
+        if (by_mass ? w >= target : n >= k) break;
       }
     }
     __syncthreads();
@@ -751,17 +796,17 @@ struct RowWork {
     return b;
   }
 
-  // The cut after the k-th word, or after the shortest prefix of weight `target`, from histogram 0.
+  // The cut after the k-th word, or after the shortest prefix of weight `target`, among the words from x_lo up.
   __device__ __forceinline__ Cut select(bool by_mass, int k, double target) const {
     int count0 = 0, cnt;
     double mass0 = 0.0;
-    const int b = find_bin(0, by_mass, count0, mass0, k, target, cnt);
+    const int b = find_bin(by_mass, count0, mass0, k, target, cnt);
     // the keys that fall into bin b: bin_of only falls as the key grows
     auto lowest = [&](int bin) {
       uint32_t lo = order_key(x_lo), hi = order_key(m);
       while (lo < hi) {
         const uint32_t mid = lo + (hi - lo) / 2;
-        if (bin_of(key_value(mid)) <= bin) hi = mid;
+        if (bin_of(t2(key_value(mid))) <= bin) hi = mid;
         else lo = mid + 1;
       }
       return lo;
@@ -770,9 +815,9 @@ struct RowWork {
     uint32_t klo = lowest(b), khi = b == 0 ? order_key(m) : lowest(b - 1) - 1;
     while (cnt > kCap && klo < khi) {
       const int bits = 32 - __clz((int)(khi - klo));
-      const int shift = max(0, bits - 7);
-      histogram(1, key_value(klo), key_value(khi), khi, shift);
-      const int q = find_bin(1, by_mass, count0, mass0, k, target, cnt);
+      const int shift = max(0, bits - 10);  // at most kBins
+      histogram(key_value(klo), key_value(khi), khi, shift);
+      const int q = find_bin(by_mass, count0, mass0, k, target, cnt);
       khi -= (uint32_t)q << shift;
       klo = max(klo, khi - ((1u << shift) - 1));
       khi -= khi == kMinusZero;  // as a bound it would let the zeros in
@@ -786,6 +831,7 @@ struct RowWork {
       else if (w > 0.0) r = (int)fmin(ceil((target - mass0) / w), (double)cnt);
       r = max(1, min(r, cnt));
       cut.mass = mass0 + (double)r * w;
+      cut.count = count0 + r;
       cut.tie = V;
       if (r < cnt) {
         count_equal(cut.thr);
@@ -800,6 +846,7 @@ struct RowWork {
     cut.thr = list_value(r - 1);
     cut.tie = list_index(r - 1);
     cut.mass = sh.l.cum[r - 1];
+    cut.count = count0 + r;
     __syncthreads();
     return cut;
   }
@@ -835,42 +882,51 @@ struct RowWork {
 
   // ---- the count of bf16 values ----
 
-  // The row's cut from the count of each value, S and the number of kept words, and with `sums` the tiles' kept weights
-  // in rec.sum.  False where the cut falls among the words of bin kMid, which are not told apart.
-  __device__ __forceinline__ bool by_value(bool k_on, int k, bool p_on, double p, float z_min, bool sums, float& thr_out,
-                                           int& tie_out, int& n_out, double& S_out) const {
+  // f(word) for a tile's words of bin kMid: 1 in 80,000 of normal logits, so in a pass of its own.
+  template <typename F>
+  __device__ __forceinline__ void each_mid(int tile, u16x2 least, F f) const {
+    if (!__any(least.x == 0 || least.y == 0)) return;
+    each_vector(tile, [&](const u32x4& x, int) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e)
+        if (fabsf(elem<Tin>(x, e)) < bin_value(kMid + 1)) f(elem<Tin>(x, e));
+    });
+  }
+
+  __device__ __forceinline__ void clear_values() const {
+    for (int i = threadIdx.x; i < kValues; i += NT) sh.v.count[i] = 0u;
+    if (threadIdx.x == 0) sh.v.mid = 0ull;
+    __syncthreads();
+  }
+
+  // A tile's words added to the counts of values.
+  __device__ __forceinline__ void count_values(const Tile<Tin>& x, int tile) const {
+    u16x2 least = (u16x2)(unsigned short)1;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const s16x2 b = value_bins(x.v[j][q], least);
+        atomicAdd(&sh.v.count[kMid + b.x], 1u);
+        atomicAdd(&sh.v.count[kMid + b.y], 1u);
+      }
+    each_mid(tile, least, [&](float z) {
+      const double y = exp2_neg(((double)z - (double)bin_value(kMid + 1)) * c) + 256.0;
+      atomicAdd(&sh.v.mid, __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
+    });
+  }
+
+  struct ValueCut {
+    float thr;
+    int n, r, of;  // kept words; of the `of` words that equal thr the first r (r = of = 0: all)
+    double S;
+  };
+
+  // The row's cut from the counts of values.  False where it falls among the words of bin kMid, which are not told apart.
+  __device__ __forceinline__ bool cut_values(bool k_on, int k, bool p_on, double p, float z_min, ValueCut& out) const {
     constexpr int kEach = (kValues + NT - 1) / NT;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x;
     const double mid_top = t2(bin_value(kMid + 1));
-    // f(word) for a tile's words of bin kMid: 1 in 80,000 of normal logits, so in a pass of its own
-    auto each_mid = [&](int tile, u16x2 least, auto f) {
-      if (!__any(least.x == 0 || least.y == 0)) return;
-      each_vector(tile, [&](const u32x4& x, int) {
-#pragma unroll
-        for (int e = 0; e < EPV; ++e)
-          if (fabsf(elem<Tin>(x, e)) < bin_value(kMid + 1)) f(elem<Tin>(x, e));
-      });
-    };
-    for (int i = tid; i < kValues; i += NT) sh.v.count[i] = 0u;
-    if (tid == 0) sh.v.mid = 0ull;
-    __syncthreads();
-    each_tile([](int) { return true; },
-              [&](const Tile<Tin>& x, int tile) {
-                u16x2 least = (u16x2)(unsigned short)1;
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                  for (int q = 0; q < 4; ++q) {
-                    const s16x2 b = value_bins(x.v[j][q], least);
-                    atomicAdd(&sh.v.count[kMid + b.x], 1u);
-                    atomicAdd(&sh.v.count[kMid + b.y], 1u);
-                  }
-                each_mid(tile, least, [&](float z) {
-                  const double y = exp2_neg(fmin(t2(z) - mid_top, 0.0)) + 256.0;
-                  atomicAdd(&sh.v.mid, __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
-                });
-              });
-    __syncthreads();
     // each thread kEach bins, from the largest value down; the last one holds the masked words
     const double mid = (double)sh.v.mid * 0x1p-44 * exp2_neg(mid_top);
     auto bin_at = [&](int i) { return kValues - 1 - (tid * kEach + i); };
@@ -967,24 +1023,27 @@ struct RowWork {
       thr = z_min;
       cnt = r = 0;
     }
-    const bool partial = r < cnt;
-    thr_out = thr;
-    tie_out = V;
-    n_out = n;
-    S_out = S;
-    if (!sums) {
-      if (partial) {
-        count_equal(thr);
-        tie_out = tie_index(thr, r);
-      }
-      return true;
-    }
-    // the tiles' kept weights: a table of them, 0 below the cut, the cut's own value apart where it is kept in part
-    const double w_thr = weight(thr);
+    out = ValueCut{thr, n, r, cnt, S};
     __syncthreads();
-    for (int i = 0; i < kEach; ++i) {
-      const int b = bin_at(i);
-      if (b >= 0 && (b < 1 || (b != kMid && !(partial ? bin_value(b) > thr : bin_value(b) >= thr)))) sh.v.weight[b] = 0.0;
+    return true;
+  }
+
+  // The last kept index of the cut's value.
+  __device__ __forceinline__ int value_tie(const ValueCut& cut) const {
+    if (cut.r >= cut.of) return V;
+    count_equal(cut.thr);
+    return tie_index(cut.thr, cut.r);
+  }
+
+  // rec.sum = the tiles' kept weights, from the table that cut_values leaves; the last kept index of the cut's value.
+  __device__ __forceinline__ int value_sums(const ValueCut& cut) const {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const float thr = cut.thr;
+    const bool partial = cut.r < cut.of;
+    // 0 below the cut; the cut's own value apart where it is kept in part
+    const double w_thr = weight(thr);
+    for (int b = tid; b < kValues; b += NT) {
+      if ((b < 1 || (b != kMid && !(partial ? bin_value(b) > thr : bin_value(b) >= thr)))) sh.v.weight[b] = 0.0;
     }
     const bool mid_kept = 0.f >= thr;
     __syncthreads();
@@ -1016,49 +1075,71 @@ struct RowWork {
                 }
               });
     __syncthreads();
+    int tie = V;
     if (partial) {
-      tie_out = tie_index(thr, r);
+      tie = tie_index(thr, cut.r);
       for (int i = tid; i < tiles; i += NT) rec.sum[i] += (double)rec.count[i] * w_thr;
       __syncthreads();
     }
-    return true;
+    return tie;
   }
 
   // ---- draws ----
 
   // Wave 0: the tile's first kept word at which the kept weights pass `left`, or its last kept word.
   __device__ __forceinline__ int pick(int tile, double left, float thr, int tie) const {
-    int found = -1, last = -1;
-    each_vector(tile, [&](const u32x4& x, int j) {
-      double w[EPV], s = 0.0;
-      int mine = -1;
+    const int lane = threadIdx.x & 63;
+    Tile<Tin> x;
+    x.load(row, V, tile);
+    // the vector and the lane that hold it
+    double s[NV];
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        const float z = elem<Tin>(x, e);
-        const int col = Tile<Tin>::col(tile, j, e);
-        w[e] = kept(z, col, thr, tie) ? weight(z) : 0.0;
-        if (w[e] > 0.0) mine = col;
-        s += w[e];
-      }
-      const double incl = scan_add(s), excl = incl - s;
-      const uint64_t mask = __ballot(s > 0.0 && incl > left);
-      if (mask && found < 0) {
-        const int l = __ffsll((unsigned long long)mask) - 1;
-        double run = excl;
-        int col = -1;
+    for (int j = 0; j < NV; ++j) {
+      s[j] = 0.0;
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          run += w[e];
-          if (col < 0 && w[e] > 0.0 && run > left) col = Tile<Tin>::col(tile, j, e);
-        }
-        if (col < 0) col = mine;  // the lane's own sum in another order
-        found = __builtin_amdgcn_readlane(col, l);
+      for (int e = 0; e < EPV; ++e)
+        if (kept(x.at(j, e), Tile<Tin>::col(tile, j, e), thr, tie)) s[j] += weight(x.at(j, e));
+    }
+    int at_j = -1, at_l = 0, last_j = 0, last_l = 0;
+    double run = 0.0, base = 0.0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const double incl = run + scan_add(s[j]);
+      const uint64_t over = __ballot(s[j] > 0.0 && incl > left), some = __ballot(s[j] > 0.0);
+      if (at_j < 0 && over) {
+        at_j = j;
+        at_l = __ffsll((unsigned long long)over) - 1;
+        base = readlane_f64(incl - s[j], at_l);
       }
-      const uint64_t some = __ballot(mine >= 0);
-      if (some) last = __builtin_amdgcn_readlane(mine, 63 - __clzll((long long)some));
-      left -= readlane_f64(incl, 63);
-    });
-    return found >= 0 ? found : last;
+      if (some) {
+        last_j = j;
+        last_l = 63 - __clzll((long long)some);
+      }
+      run = readlane_f64(incl, 63);
+    }
+    if (at_j < 0) {
+      at_j = last_j;
+      at_l = last_l;
+      left = INFINITY;
+    }
+    // its words, one to a lane
+    u32x4 v = x.v[0];
+#pragma unroll
+    for (int j = 1; j < NV; ++j)
+      if (at_j == j) v = x.v[j];
+    uint32_t d = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t w = __builtin_amdgcn_readlane(v[q], at_l);
+      if (lane * (int)sizeof(Tin) / 4 == q) d = w;
+    }
+    const float z = sizeof(Tin) == 4 ? __uint_as_float(d) : (lane & 1) ? bf16_hi(d) : bf16_lo(d);
+    const int col = tile * Tile<Tin>::kWords + (at_j * 64 + at_l) * EPV + lane;
+    const double w = lane < EPV && kept(z, col, thr, tie) ? weight(z) : 0.0;
+    const double incl = base + scan_add(w);
+    const uint64_t over = __ballot(w > 0.0 && incl > left), some = __ballot(w > 0.0);
+    const int e = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll((long long)(some | 1ull));
+    return tile * Tile<Tin>::kWords + (at_j * 64 + at_l) * EPV + e;
   }
 
   // The first kept word at which the kept weights pass `target`, from the tiles' sums in rec.sum.
@@ -1088,26 +1169,30 @@ struct RowWork {
 
   // ---- bounds ----
 
-  // A lower bound of the k-th largest of the n partial maxima in sh.sub, and so of the row's k-th word.
+  // A lower bound of the k-th largest of the n partial maxima in sh.sub, and so of the row's k-th word: the upper 20 bits
+  // of its key, each wave trying another value of the next ones.
   __device__ __forceinline__ float kth_bound(int n, int k) const {
-    if (threadIdx.x < 64) {
-      const int lane = threadIdx.x;
-      uint32_t key[kMaxSubs / 64];
+    constexpr int kBits = NW == 16 ? 4 : 3;
+    static_assert(NW == 1 << kBits, "waves to values");
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    uint32_t key[kMaxSubs / 64];
 #pragma unroll
-      for (int i = 0; i < kMaxSubs / 64; ++i) key[i] = i * 64 + lane < n ? order_key(sh.sub[i * 64 + lane]) : 0u;
-      uint32_t t = 0;
+    for (int i = 0; i < kMaxSubs / 64; ++i) key[i] = i * 64 + lane < n ? order_key(sh.sub[i * 64 + lane]) : 0u;
+    uint32_t t = 0;
+    int parity = 0;
 #pragma unroll 1
-      for (int bit = 31; bit >= 12; --bit) {
-        const uint32_t cand = t | (1u << bit);
-        int have = 0;
+    for (int shift = 32 - kBits; shift > 12 - kBits; shift -= kBits) {
+      const uint32_t cand = t + ((uint32_t)wv << shift);
+      int have = 0;
 #pragma unroll
-        for (int i = 0; i < kMaxSubs / 64; ++i) have += __popcll(__ballot(key[i] >= cand));
-        if (have >= k) t = cand;
-      }
-      if (lane == 0) sh.key = t;
+      for (int i = 0; i < kMaxSubs / 64; ++i)
+        if (i * 64 < n) have += __popcll(__ballot(key[i] >= cand));
+      if (lane == 0) sh.wi[parity][wv] = have >= k;
+      __syncthreads();
+      const uint64_t mask = __ballot(lane < NW && sh.wi[parity][lane & (NW - 1)] != 0);
+      t += (uint32_t)(63 - __clzll((long long)(mask | 1ull))) << shift;
+      parity ^= 1;
     }
-    __syncthreads();
-    const uint32_t t = sh.key;
     __syncthreads();
     return t > order_key(kLiveMin) ? key_value(t) : kLiveMin;
   }
@@ -1151,10 +1236,16 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
   float m = -INFINITY, lo = INFINITY;
   int live = 0;
   bool bad = false;
-  const SumMode mode = sum_mode(st, a.V, DRAW, FUSED);
+  const SumMode mode = sum_mode(st, a.V, DRAW, FUSED, Work::kByValue, subs);
   if (FUSED) {
+    if constexpr (Work::kByValue) {
+      if (mode == kCount) w.clear_values();
+    }
     w.each_tile([](int) { return true; },
                 [&](const Tile<Tin>& x, int tile) {
+                  if constexpr (Work::kByValue) {
+                    if (mode == kCount) w.count_values(x, tile);
+                  }
                   const TileStats s = tile_stats<Tin>(x, mode, st.c);
                   if (fine && (lane & 7) == 0) sh.sub[tile * kSubs + (lane >> 3)] = s.sub;
                   if (lane == 0) {
@@ -1253,7 +1344,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
       if (DRAW) act = tie;
       drawn = true;
     } else {
-      if (mode != kNoSum) {  // the tiles' sums relative to the row's maximum
+      if (mode == kSum64 || mode == kSum32) {  // the tiles' sums relative to the row's maximum
         double total = 0.0;
         for (int i = tid; i < a.tiles; i += NT) {
           const double v = rec.max[i] >= kLiveMin ? rec.sum[i] * w.weight(rec.max[i]) : 0.0;
@@ -1268,7 +1359,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
         const float z_min = m_on ? fmaxf(w.min_p_bound(log2((double)st.min_p)), kLiveMin) : kLiveMin;
         float x_lo = k_on && p_on ? kLiveMin : z_min;  // top-p of top-k needs the first k words' sum
         if (k_on && k <= subs) x_lo = fmaxf(x_lo, w.kth_bound(subs, k));
-        if (p_on && !k_on) {
+        if (p_on && !k_on && mode != kCount) {
           // all words lighter than (1 - p) S / live together weigh less than (1 - p) S; 0.01 covers S's error
           const double l = log2((double)live / ((1.0 - p) * S)) + 0.01;
           const double z = (double)m - l / st.c;
@@ -1277,34 +1368,57 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
           x_lo = fmaxf(x_lo, zf);
         }
         w.x_lo = x_lo;
-        int listed = x_lo > kLiveMin || live <= kCap ? w.gather(x_lo, INFINITY) : live;
-        if (listed <= kCap) {
-          w.sort_list(listed);
-          w.scan_list(listed, 0.0);
-          n = k_on ? min(k, listed) : listed;
-          if (p_on) {
-            int np;
-            if (k_on || mode == kSum64) {
-              np = w.first_reaching(listed, p * (k_on ? sh.l.cum[n - 1] : S));
-            } else {
-              np = w.first_reaching(listed, p * (S * (1.0 - kSum32Error)));
-              if (np != w.first_reaching(listed, p * (S * (1.0 + kSum32Error)))) {
-                int all;
-                S = w.kept_sums(kLiveMin, a.V, all);
-                np = w.first_reaching(listed, p * S);
-              }
+        int listed = -1;
+        if (mode != kCount) listed = x_lo > kLiveMin || live <= kCap ? w.gather(x_lo, INFINITY) : live;
+        bool cut_known = false;
+        if constexpr (Work::kByValue) {
+          if ((mode == kCount || listed > kCap) && m < kLimit && lo > -kLimit) {
+            if (mode != kCount) {
+              w.clear_values();
+              w.each_tile([](int) { return true; }, [&](const Tile<Tin>& x, int tile) { w.count_values(x, tile); });
+              __syncthreads();
             }
-            n = min(n, np);
+            typename Work::ValueCut cut;
+            cut_known = w.cut_values(k_on, k, p_on, p, z_min, cut);
+            if (cut_known) {
+              thr = cut.thr;
+              n = cut.n;
+              S = cut.S;
+              if (n - cut.r + cut.of <= kCap) listed = w.gather(thr, INFINITY);
+              else if (DRAW) tie = w.value_sums(cut);
+              else tie = w.value_tie(cut);
+            }
           }
-          if (m_on) {
-            int c = 0;
-            for (int i = tid; i < listed; i += NT) c += w.list_value(i) >= z_min;
-            n = min(n, w.block_sum(c));
+        }
+        if (listed >= 0 && listed <= kCap) {
+          w.sort_list(listed);
+          if (!cut_known) {
+            w.scan_list(listed, 0.0);
+            n = k_on ? min(k, listed) : listed;
+            if (p_on) {
+              int np;
+              if (k_on || mode == kSum64) {
+                np = w.first_reaching(listed, p * (k_on ? sh.l.cum[n - 1] : S));
+              } else {
+                np = w.first_reaching(listed, p * (S * (1.0 - kSum32Error)));
+                if (np != w.first_reaching(listed, p * (S * (1.0 + kSum32Error)))) {
+                  int all;
+                  S = w.kept_sums(kLiveMin, a.V, all);
+                  np = w.first_reaching(listed, p * S);
+                }
+              }
+              n = min(n, np);
+            }
+            if (m_on) {
+              int c = 0;
+              for (int i = tid; i < listed; i += NT) c += w.list_value(i) >= z_min;
+              n = min(n, w.block_sum(c));
+            }
+            n = max(n, 1);
+            S = sh.l.cum[n - 1];
           }
-          n = max(n, 1);
           thr = w.list_value(n - 1);
           tie = w.list_index(n - 1);
-          S = sh.l.cum[n - 1];
           __syncthreads();
           if (DRAW) {
             // the kept words in the order of their indices, smallest first: keys that fall as the index grows
@@ -1329,39 +1443,36 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
             act = (int)~(uint32_t)(sh.l.key[at == INT_MAX ? last : at] >> 32);
             drawn = true;
           }
-        } else {
-          bool done = false;
-          if constexpr (Work::kByValue) {
-            if (m < kLimit && lo > -kLimit) done = w.by_value(k_on, k, p_on, p, z_min, DRAW, thr, tie, n, S);
-          }
-          if (!done) {
-            thr = kLiveMin;
-            tie = a.V;
-            auto narrow = [&](float z, int i) {
-              if (z > thr || (z == thr && i < tie)) {
-                thr = z;
-                tie = i;
-              }
-            };
-            if (k_on || p_on) {
-              if (p_on && !k_on && mode != kSum64) {  // S from the histogram: all live words
-                x_lo = kLiveMin;
-                w.x_lo = x_lo;
-              }
-              w.histogram(0, x_lo, INFINITY, 0u, 0);
-              double Sk = S;
-              if (p_on && !k_on && mode != kSum64) Sk = w.block_sum(tid < kBins ? sh.bin_mass[0][tid] : 0.0);
-#pragma unroll 1
-              for (int by_mass = 0; by_mass < 2; ++by_mass) {
-                if (by_mass ? !p_on : !k_on) continue;
-                const Cut cut = w.select(by_mass, k, p * Sk);
-                narrow(cut.thr, cut.tie);
-                Sk = cut.mass;
-              }
+        } else if (!cut_known) {
+          thr = kLiveMin;
+          tie = a.V;
+          auto narrow = [&](float z, int i) {
+            if (z > thr || (z == thr && i < tie)) {
+              thr = z;
+              tie = i;
             }
-            if (m_on) narrow(z_min, a.V);
-            S = w.kept_sums(thr, tie, n);
+          };
+          if (k_on || p_on) {
+            const bool sum_all = p_on && !k_on && mode != kSum64;  // S from the histogram: all live words
+            if (sum_all) w.x_lo = x_lo = kLiveMin;
+            double Sk = S;
+#pragma unroll 1
+            for (int by_mass = 0; by_mass < 2; ++by_mass) {
+              if (by_mass ? !p_on : !k_on) continue;
+              w.histogram(x_lo, INFINITY, 0u, 0);
+              if (sum_all) {
+                double q = 0.0;
+                for (int i = tid; i < kBins; i += NT) q += sh.h.bin_mass[i];
+                Sk = w.block_sum(q);
+              }
+              const Cut cut = w.select(by_mass, k, p * Sk);
+              narrow(cut.thr, cut.tie);
+              Sk = S = cut.mass;
+              n = cut.count;
+            }
           }
+          if (m_on) narrow(z_min, a.V);
+          if (DRAW || m_on) S = w.kept_sums(thr, tie, n);
         }
       }
       if (!drawn) act = w.draw((double)u * S, thr, tie);
