@@ -132,6 +132,16 @@ __device__ __forceinline__ T scan_add(T v) {
   return v;
 }
 
+template <typename F>
+__device__ __forceinline__ int wave_reduce(int v, F f) {
+  v = f(v, (int)dpp_u32<0xB1>((uint32_t)v));
+  v = f(v, (int)dpp_u32<0x4E>((uint32_t)v));
+  v = f(v, (int)dpp_u32<0x141>((uint32_t)v));
+  v = f(v, (int)dpp_u32<0x140>((uint32_t)v));
+  return f(f(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+           f(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+
 // ---- a row's settings -----------------------------------------------------------
 struct Settings {
   float tau, p, min_p;
@@ -212,6 +222,19 @@ struct Tile {
     }
   }
   __device__ __forceinline__ float at(int j, int e) const { return elem<Tin>(v[j], e); }
+  // Vector j, the same j in every lane: a loop over them that is not unrolled keeps the code short, which most of this
+  // file is bound by where a row is worked on by one workgroup (code is fetched once by each).
+  __device__ __forceinline__ u32x4 vec(int j) const {
+    u32x4 r = v[0];
+    asm("" : "+v"(r));  // registers chosen between, not a place in memory
+#pragma unroll
+    for (int i = 1; i < NV; ++i) {
+      u32x4 q = v[i];
+      asm("" : "+v"(q));
+      r = j == i ? q : r;
+    }
+    return r;
+  }
 };
 
 struct TileStats {
@@ -250,14 +273,16 @@ __device__ __forceinline__ TileStats tile_stats(const Tile<Tin>& x, SumMode mode
   if (!all_live) {
     s.live = 0;
     mn = INFINITY;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
+#pragma unroll 1
+    for (int j = 0; j < NV; ++j) {
+      const u32x4 v = x.vec(j);
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
-        const float z = x.at(j, e);
+        const float z = elem<Tin>(v, e);
         s.live += __popcll(__ballot(z >= kLiveMin));
         if (z >= kLiveMin) mn = fminf(mn, z);
       }
+    }
     lo = -wave_max_dpp(-mn);
   }
   s.lo = lo;
@@ -266,18 +291,22 @@ __device__ __forceinline__ TileStats tile_stats(const Tile<Tin>& x, SumMode mode
     const double m = (double)s.max;
     double sum = 0.0;
     if (all_live && (m - (double)lo) * c < 1000.0) {
+#pragma unroll 1
+      for (int j = 0; j < NV; ++j) {
+        const u32x4 v = x.vec(j);
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) sum += exp2_neg<false>(((double)x.at(j, e) - m) * c);
+        for (int e = 0; e < EPV; ++e) sum += exp2_neg<false>(((double)elem<Tin>(v, e) - m) * c);
+      }
     } else {
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
+#pragma unroll 1
+      for (int j = 0; j < NV; ++j) {
+        const u32x4 v = x.vec(j);
 #pragma unroll
         for (int e = 0; e < EPV; ++e) {
-          const float z = x.at(j, e);
+          const float z = elem<Tin>(v, e);
           sum += z >= kLiveMin ? exp2_neg(((double)z - m) * c) : 0.0;
         }
+      }
     }
     s.sum = wave_sum_dpp(sum);
   } else {
@@ -289,13 +318,15 @@ __device__ __forceinline__ TileStats tile_stats(const Tile<Tin>& x, SumMode mode
 #pragma unroll
         for (int e = 0; e < EPV; ++e) sum += __builtin_amdgcn_exp2f((x.at(j, e) - s.max) * c32);
     } else {
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
+#pragma unroll 1
+      for (int j = 0; j < NV; ++j) {
+        const u32x4 v = x.vec(j);
 #pragma unroll
         for (int e = 0; e < EPV; ++e) {
-          const float z = x.at(j, e);
+          const float z = elem<Tin>(v, e);
           sum += z >= kLiveMin ? __builtin_amdgcn_exp2f((z - s.max) * c32) : 0.f;
         }
+      }
     }
     s.sum = wave_sum_dpp((double)sum);
   }
@@ -370,9 +401,10 @@ struct RowShared {
     } v;
   };
   float sub[kMaxSubs];
-  double wd[kMaxNW];
+  double wd[2][kMaxNW];
   int wi[2][kMaxNW];
   float wf[2][kMaxNW];
+  uint32_t radix[256];
   // broadcast
   int n, bin, i0;
   uint32_t key;
@@ -399,46 +431,51 @@ struct RowWork {
   double c;  // log2(e) / tau
   float x_lo;  // words below it are not looked at
 
-  // ---- over the workgroup: the same value in every thread; two barriers each, so that `sh` may be reused ----
-  __device__ __forceinline__ double block_sum(double v) const {
+  int turn = 0;  // which of the two sets of sh.w* the next reduction takes
+
+  // ---- over the workgroup: the same value in every thread.  One barrier each: a set is written again after the next
+  // reduction's barrier, when every wave has read it. ----
+  __device__ __forceinline__ double block_sum(double v) {
+    const int b = turn;
+    turn ^= 1;
     v = wave_sum_dpp(v);
-    if ((threadIdx.x & 63) == 0) sh.wd[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) sh.wd[b][threadIdx.x >> 6] = v;
     __syncthreads();
     double r = 0.0;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) r += sh.wd[i];
-    __syncthreads();
+    for (int i = 0; i < NW; ++i) r += sh.wd[b][i];
     return r;
   }
   template <typename F>
-  __device__ __forceinline__ int block_reduce(int v, F f) const {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, 64));
-    if ((threadIdx.x & 63) == 0) sh.wi[0][threadIdx.x >> 6] = v;
+  __device__ __forceinline__ int block_reduce(int v, F f) {
+    const int b = turn;
+    turn ^= 1;
+    v = wave_reduce(v, f);
+    if ((threadIdx.x & 63) == 0) sh.wi[b][threadIdx.x >> 6] = v;
     __syncthreads();
-    int r = sh.wi[0][0];
+    int r = sh.wi[b][0];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) r = f(r, sh.wi[0][i]);
-    __syncthreads();
+    for (int i = 1; i < NW; ++i) r = f(r, sh.wi[b][i]);
     return r;
   }
-  __device__ __forceinline__ int block_sum(int v) const {
+  __device__ __forceinline__ int block_sum(int v) {
     return block_reduce(v, [](int a, int b) { return a + b; });
   }
-  __device__ __forceinline__ int block_min(int v) const {
+  __device__ __forceinline__ int block_min(int v) {
     return block_reduce(v, [](int a, int b) { return min(a, b); });
   }
-  __device__ __forceinline__ int block_max(int v) const {
+  __device__ __forceinline__ int block_max(int v) {
     return block_reduce(v, [](int a, int b) { return max(a, b); });
   }
   // Sums of a count and a weight over the threads up to this one.
-  __device__ __forceinline__ void block_scan(int& n, double& v, int& all_n, double& all_v) const {
-    const int wv = threadIdx.x >> 6;
+  __device__ __forceinline__ void block_scan(int& n, double& v, int& all_n, double& all_v) {
+    const int wv = threadIdx.x >> 6, b = turn;
+    turn ^= 1;
     n = scan_add(n);
     v = scan_add(v);
     if ((threadIdx.x & 63) == 63) {
-      sh.wi[0][wv] = n;
-      sh.wd[wv] = v;
+      sh.wi[b][wv] = n;
+      sh.wd[b][wv] = v;
     }
     __syncthreads();
     double before = 0.0;
@@ -451,14 +488,13 @@ struct RowWork {
         before = all_v;
         n_before = all_n;
       }
-      all_n += sh.wi[0][i];
-      all_v += sh.wd[i];
+      all_n += sh.wi[b][i];
+      all_v += sh.wd[b][i];
     }
-    __syncthreads();
     n += n_before;
     v += before;
   }
-  __device__ __forceinline__ double block_scan(double v, double& all) const {
+  __device__ __forceinline__ double block_scan(double v, double& all) {
     int n = 0, all_n;
     block_scan(n, v, all_n, all);
     return v;
@@ -486,16 +522,14 @@ struct RowWork {
     }
   }
 
-  // f(vector, j) over a tile's vectors, the next one's load in flight: for the passes whose work per word is long.
-  template <typename F>
-  __device__ __forceinline__ void each_vector(int tile, F f) const {
-    u32x4 x = Tile<Tin>::load_one(row, V, tile, 0);
+  // The same with f(vector, tile, j) for each of their vectors, then done(tile).
+  template <typename P, typename F, typename G>
+  __device__ __forceinline__ void each_vector(P want, F f, G done) const {
+    each_tile(want, [&](const Tile<Tin>& x, int tile) {
 #pragma unroll 1
-    for (int j = 0; j < NV; ++j) {
-      const u32x4 next = Tile<Tin>::load_one(row, V, tile, min(j + 1, NV - 1));
-      f(x, j);
-      x = next;
-    }
+      for (int j = 0; j < NV; ++j) f(x.vec(j), tile, j);
+      done(tile);
+    });
   }
 
   __device__ __forceinline__ double t2(float z) const { return ((double)z - (double)m) * c; }
@@ -507,8 +541,9 @@ struct RowWork {
   // ---- a list of words in LDS ----
 
   // The words of [lo, hi] appended to the list while it has room; returns how many there are, or more than kCap.
-  __device__ __forceinline__ int gather(float lo, float hi) const {
+  __device__ __forceinline__ int gather(float lo, float hi) {
     const int tid = threadIdx.x, lane = tid & 63;
+    __syncthreads();
     if (tid == 0) sh.n = 0;
     __syncthreads();
     each_tile(
@@ -516,26 +551,26 @@ struct RowWork {
           return rec.max[tile] >= lo && __builtin_amdgcn_readfirstlane(*(volatile int*)&sh.n) <= kCap;
         },
         [&](const Tile<Tin>& x, int tile) {
-          int have[NV], all = 0;
-#pragma unroll
+          int all = 0;
+#pragma unroll 1
           for (int j = 0; j < NV; ++j) {
-            have[j] = 0;
-            if (__any(vec_max<Tin>(x.v[j], -INFINITY) >= lo)) {
+            const u32x4 v = x.vec(j);
+            if (!__any(vec_max<Tin>(v, -INFINITY) >= lo)) continue;
 #pragma unroll
-              for (int e = 0; e < EPV; ++e) have[j] += __popcll(__ballot(x.at(j, e) >= lo && x.at(j, e) <= hi));
-            }
-            all += have[j];
+            for (int e = 0; e < EPV; ++e) all += __popcll(__ballot(elem<Tin>(v, e) >= lo && elem<Tin>(v, e) <= hi));
           }
+          if (all == 0) return;
           int at = 0;
           if (lane == 0) at = atomicAdd(&sh.n, all);
           at = __builtin_amdgcn_readfirstlane(at);
           if (at + all > kCap) return;
-#pragma unroll
+#pragma unroll 1
           for (int j = 0; j < NV; ++j) {
-            if (have[j] == 0) continue;
+            const u32x4 v = x.vec(j);
+            if (!__any(vec_max<Tin>(v, -INFINITY) >= lo)) continue;
 #pragma unroll
             for (int e = 0; e < EPV; ++e) {
-              const float z = x.at(j, e);
+              const float z = elem<Tin>(v, e);
               const bool in = z >= lo && z <= hi;
               const uint64_t mask = __ballot(in);
               if (in)
@@ -546,13 +581,11 @@ struct RowWork {
           }
         });
     __syncthreads();
-    const int n = sh.n;
-    __syncthreads();
-    return n;
+    return sh.n;
   }
 
   // Sorts the n keys in sh.l.key, all different, largest first.
-  __device__ __forceinline__ void sort_list(int n) const {
+  __device__ __forceinline__ void sort_list(int n) {
     const int tid = threadIdx.x;
     if (n <= kRankSort) {  // a word's place is the number of larger ones: kRanks threads count them for each
       constexpr int kRanks = NT / kRankSort;
@@ -572,6 +605,8 @@ struct RowWork {
     while (P < n) P <<= 1;
     for (int i = n + tid; i < P; i += NT) sh.l.key[i] = 0ull;
     __syncthreads();
+    // Pairs at most 64 apart lie within the 128 keys of 64 neighbouring comparisons, which one wave makes: between such
+    // stages its own LDS accesses are in order and no other wave's matter.
     for (int k = 2; k <= P; k <<= 1) {
       for (int j = k >> 1; j > 0; j >>= 1) {
         for (int q = tid; q < (P >> 1); q += NT) {
@@ -582,16 +617,18 @@ struct RowWork {
             sh.l.key[i | j] = x;
           }
         }
-        __syncthreads();
+        if (j > 64 || (j == 1 && k >= 128)) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
+    __syncthreads();
   }
 
   __device__ __forceinline__ float list_value(int i) const { return key_value((uint32_t)(sh.l.key[i] >> 32)); }
   __device__ __forceinline__ int list_index(int i) const { return (int)~(uint32_t)sh.l.key[i]; }
 
   // sh.l.cum = the prefix sums of the list's weights, from `base` on.
-  __device__ __forceinline__ void scan_list(int n, double base) const {
+  __device__ __forceinline__ void scan_list(int n, double base) {
     for (int i0 = 0; i0 < n; i0 += NT) {
       const int i = i0 + threadIdx.x;
       double total;
@@ -603,7 +640,7 @@ struct RowWork {
   }
 
   // The least r >= 1 with cum[r - 1] >= target, or n.
-  __device__ __forceinline__ int first_reaching(int n, double target) const {
+  __device__ __forceinline__ int first_reaching(int n, double target) {
     int r = n;
     for (int i = threadIdx.x; i < n; i += NT)
       if (sh.l.cum[i] >= target) {
@@ -618,10 +655,14 @@ struct RowWork {
   // Wave 0: the tile's r-th word (from 1) that equals z, by index.
   __device__ __forceinline__ int nth_equal(int tile, float z, int r) const {
     int found = 0;
-    each_vector(tile, [&](const u32x4& x, int j) {
+    Tile<Tin> x;
+    x.load(row, V, tile);
+#pragma unroll 1
+    for (int j = 0; j < NV; ++j) {
+      const u32x4 v = x.vec(j);
       int n = 0;
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) n += elem<Tin>(x, e) == z;
+      for (int e = 0; e < EPV; ++e) n += elem<Tin>(v, e) == z;
       const int incl = scan_add(n);
       const int all = __builtin_amdgcn_readlane(incl, 63);
       if (r >= 1 && r <= all) {
@@ -629,14 +670,14 @@ struct RowWork {
         int left = r - (incl - n), col = 0;
 #pragma unroll
         for (int e = 0; e < EPV; ++e) {
-          const bool same = elem<Tin>(x, e) == z;
+          const bool same = elem<Tin>(v, e) == z;
           left -= same;
           if (left == 0 && same) col = Tile<Tin>::col(tile, j, e);
         }
         found = __builtin_amdgcn_readlane(col, l);
       }
       r -= all;
-    });
+    }
     return found;
   }
 
@@ -644,15 +685,16 @@ struct RowWork {
   __device__ __forceinline__ void count_equal(float z) const {
     for (int i = threadIdx.x; i < tiles; i += NT)
       if (!(rec.max[i] >= z)) rec.count[i] = 0;
-    each_tile([&](int tile) { return rec.max[tile] >= z; },
-              [&](const Tile<Tin>& x, int tile) {
-                int n = 0;
+    int n = 0;
+    each_vector([&](int tile) { return rec.max[tile] >= z; },
+                [&](const u32x4& v, int, int) {
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                  for (int e = 0; e < EPV; ++e) n += __popcll(__ballot(x.at(j, e) == z));
-                if ((threadIdx.x & 63) == 0) rec.count[tile] = n;
-              });
+                  for (int e = 0; e < EPV; ++e) n += __popcll(__ballot(elem<Tin>(v, e) == z));
+                },
+                [&](int tile) {
+                  if ((threadIdx.x & 63) == 0) rec.count[tile] = n;
+                  n = 0;
+                });
     __syncthreads();
   }
 
@@ -695,7 +737,7 @@ struct RowWork {
   // their keys below `top`, `shift` bits to a bin; into sh.h.bin_count and bin_mass.  Weights are added relative to the
   // bin's top, in 2^-44.  The last bin by weight, which has no lower end and may hold most of a row, is added up in
   // registers.
-  __device__ __forceinline__ void histogram(float lo, float hi, uint32_t top, int shift) const {
+  __device__ __forceinline__ void histogram(float lo, float hi, uint32_t top, int shift) {
     const int tid = threadIdx.x, copy = tid & (kCols - 1);
     for (int i = tid; i < kBins * kCols; i += NT) {
       sh.h.mass[i] = 0ull;
@@ -705,36 +747,37 @@ struct RowWork {
     const double t_top = top ? t2(key_value(top)) : 0.0;
     int rest = 0;
     double rest_mass = 0.0;
-    for (int tile = tid >> 6; tile < tiles; tile += NW) {
-      if (rec.max[tile] < lo) continue;
-      each_vector(tile, [&](const u32x4& x, int) {
+    each_vector(
+        [&](int tile) { return rec.max[tile] >= lo; },
+        [&](const u32x4& x, int, int) {
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          const float z = elem<Tin>(x, e);
-          if (z >= lo && z <= hi) {
-            const double t = t2(z);
-            int b;
-            double rel;
-            if (top) {
-              b = min((int)((top - order_key(z)) >> shift), kBins - 1);
-              rel = t - t_top;
-            } else {
-              b = bin_of(t);
-              rel = b == kBins - 1 ? t : fma((double)b, 1.0 / kPerOctave, t);
-            }
-            const double r = exp2_neg(fmin(rel, 0.0));
-            if (!top && b == kBins - 1) {
-              ++rest;
-              rest_mass += r;
-            } else {
-              const double y = r + 256.0;  // the weight in 2^-44 in the low bits
-              atomicAdd(&sh.h.mass[b * kCols + copy], __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
-              atomicAdd(&sh.h.count[b * kCols + copy], 1u);
+          for (int e = 0; e < EPV; ++e) {
+            const float z = elem<Tin>(x, e);
+            if (z >= lo && z <= hi) {
+              const double t = t2(z);
+              int b;
+              double rel;
+              if (top) {
+                b = min((int)((top - order_key(z)) >> shift), kBins - 1);
+                rel = t - t_top;
+              } else {
+                b = bin_of(t);
+                rel = b == kBins - 1 ? t : fma((double)b, 1.0 / kPerOctave, t);
+              }
+              const double r = exp2_neg(fmin(rel, 0.0));
+              if (!top && b == kBins - 1) {
+                ++rest;
+                rest_mass += r;
+              } else {
+                const double y = r + 256.0;  // the weight in 2^-44 in the low bits
+                atomicAdd(&sh.h.mass[b * kCols + copy], __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
+                atomicAdd(&sh.h.count[b * kCols + copy], 1u);
+              }
             }
           }
-        }
-      });
-    }
+        },
+        [](int) {});
+    __syncthreads();
     rest = block_sum(rest);
     rest_mass = block_sum(rest_mass);
     for (int b = tid; b < kBins; b += NT) {
@@ -754,7 +797,7 @@ struct RowWork {
 
   // The first bin up to which count0 (mass0) and the bins' counts (weights) reach the target, or the last one that holds a
   // word; count0 and mass0 then end before it.
-  __device__ __forceinline__ int find_bin(bool by_mass, int& count0, double& mass0, int k, double target, int& in_bin) const {
+  __device__ __forceinline__ int find_bin(bool by_mass, int& count0, double& mass0, int k, double target, int& in_bin) {
     constexpr int kEach = kBins / NT;
     const int tid = threadIdx.x;
     int n = 0, all_n;
@@ -797,17 +840,19 @@ struct RowWork {
   }
 
   // The cut after the k-th word, or after the shortest prefix of weight `target`, among the words from x_lo up.
-  __device__ __forceinline__ Cut select(bool by_mass, int k, double target) const {
+  __device__ __forceinline__ Cut select(bool by_mass, int k, double target) {
     int count0 = 0, cnt;
     double mass0 = 0.0;
     const int b = find_bin(by_mass, count0, mass0, k, target, cnt);
-    // the keys that fall into bin b: bin_of only falls as the key grows
+    // the keys that fall into bin b: bin_of only falls as the key grows; each lane tries one of 64 between the ends
     auto lowest = [&](int bin) {
       uint32_t lo = order_key(x_lo), hi = order_key(m);
       while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (bin_of(t2(key_value(mid))) <= bin) hi = mid;
-        else lo = mid + 1;
+        const uint32_t step = (hi - lo) / 64 + 1, key = lo + (threadIdx.x & 63) * step;
+        const uint64_t mask = __ballot(key >= hi || bin_of(t2(key_value(key))) <= bin);
+        const uint32_t l = mask ? (uint32_t)__ffsll((unsigned long long)mask) - 1 : 64;
+        if (l < 64) hi = min(hi, lo + l * step);
+        if (l > 0) lo = lo + (l - 1) * step + 1;
       }
       return lo;
     };
@@ -852,26 +897,27 @@ struct RowWork {
   }
 
   // rec.sum = the tiles' kept weights; their sum, and the number of kept words.
-  __device__ __forceinline__ double kept_sums(float thr, int tie, int& n) const {
-    const int lane = threadIdx.x & 63;
+  __device__ __forceinline__ double kept_sums(float thr, int tie, int& n) {
     int here = 0;
-    for (int tile = threadIdx.x >> 6; tile < tiles; tile += NW) {
-      double s = 0.0;
-      if (rec.max[tile] >= thr) {
-        each_vector(tile, [&](const u32x4& x, int j) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < tiles; i += NT)
+      if (!(rec.max[i] >= thr)) rec.sum[i] = 0.0;
+    each_vector([&](int tile) { return rec.max[tile] >= thr; },
+                [&](const u32x4& x, int tile, int j) {
 #pragma unroll
-          for (int e = 0; e < EPV; ++e) {
-            const float z = elem<Tin>(x, e);
-            if (kept(z, Tile<Tin>::col(tile, j, e), thr, tie)) {
-              s += weight(z);
-              ++here;
-            }
-          }
-        });
-        s = wave_sum_dpp(s);
-      }
-      if (lane == 0) rec.sum[tile] = s;
-    }
+                  for (int e = 0; e < EPV; ++e) {
+                    const float z = elem<Tin>(x, e);
+                    if (kept(z, Tile<Tin>::col(tile, j, e), thr, tie)) {
+                      s += weight(z);
+                      ++here;
+                    }
+                  }
+                },
+                [&](int tile) {
+                  s = wave_sum_dpp(s);
+                  if ((threadIdx.x & 63) == 0) rec.sum[tile] = s;
+                  s = 0.0;
+                });
     __syncthreads();
     double sum = 0.0;
     for (int i = threadIdx.x; i < tiles; i += NT) sum += rec.sum[i];
@@ -882,15 +928,17 @@ struct RowWork {
 
   // ---- the count of bf16 values ----
 
-  // f(word) for a tile's words of bin kMid: 1 in 80,000 of normal logits, so in a pass of its own.
+  // f(word) for the words of bin kMid among a tile's: 1 in 80,000 of normal logits.
   template <typename F>
-  __device__ __forceinline__ void each_mid(int tile, u16x2 least, F f) const {
+  __device__ __forceinline__ void each_mid(const Tile<Tin>& x, u16x2 least, F f) const {
     if (!__any(least.x == 0 || least.y == 0)) return;
-    each_vector(tile, [&](const u32x4& x, int) {
+#pragma unroll 1
+    for (int j = 0; j < NV; ++j) {
+      const u32x4 v = x.vec(j);
 #pragma unroll
       for (int e = 0; e < EPV; ++e)
-        if (fabsf(elem<Tin>(x, e)) < bin_value(kMid + 1)) f(elem<Tin>(x, e));
-    });
+        if (fabsf(elem<Tin>(v, e)) < bin_value(kMid + 1)) f(elem<Tin>(v, e));
+    }
   }
 
   __device__ __forceinline__ void clear_values() const {
@@ -900,7 +948,7 @@ struct RowWork {
   }
 
   // A tile's words added to the counts of values.
-  __device__ __forceinline__ void count_values(const Tile<Tin>& x, int tile) const {
+  __device__ __forceinline__ void count_values(const Tile<Tin>& x) const {
     u16x2 least = (u16x2)(unsigned short)1;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -910,7 +958,7 @@ struct RowWork {
         atomicAdd(&sh.v.count[kMid + b.x], 1u);
         atomicAdd(&sh.v.count[kMid + b.y], 1u);
       }
-    each_mid(tile, least, [&](float z) {
+    each_mid(x, least, [&](float z) {
       const double y = exp2_neg(((double)z - (double)bin_value(kMid + 1)) * c) + 256.0;
       atomicAdd(&sh.v.mid, __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
     });
@@ -923,7 +971,7 @@ struct RowWork {
   };
 
   // The row's cut from the counts of values.  False where it falls among the words of bin kMid, which are not told apart.
-  __device__ __forceinline__ bool cut_values(bool k_on, int k, bool p_on, double p, float z_min, ValueCut& out) const {
+  __device__ __forceinline__ bool cut_values(bool k_on, int k, bool p_on, double p, float z_min, ValueCut& out) {
     constexpr int kEach = (kValues + NT - 1) / NT;
     const int tid = threadIdx.x;
     const double mid_top = t2(bin_value(kMid + 1));
@@ -978,35 +1026,25 @@ struct RowWork {
     double S = all_m;
     float thr = kLiveMin;
     int r = 0, cnt = 0;  // of the cut's value, r words of cnt are kept (0: all)
-    if (k_on && k < all_n) {
-      int count0;
-      double mass0;
-      const int b = find(false, k, 0.0, count0, mass0);
-      if (b <= 0 || b == kMid) return false;
-      thr = bin_value(b);
-      cnt = (int)sh.v.count[b];
-      r = k - count0;
-      n = k;
-      S = mass0 + (double)r * sh.v.weight[b];
-    }
-    if (p_on) {
+#pragma unroll 1
+    for (int by_mass = 0; by_mass < 2; ++by_mass) {
+      if (by_mass ? !p_on : !(k_on && k < all_n)) continue;
       const double target = p * S;
       int count0;
       double mass0;
-      const int b = find(true, 0, target, count0, mass0);
+      const int b = find(by_mass, k, target, count0, mass0);
       if (b == kMid) return false;
-      if (b > 0) {
-        const double w = sh.v.weight[b];
-        const int have = (int)sh.v.count[b];
-        const int need = w > 0.0 ? max(1, (int)fmin(ceil((target - mass0) / w), (double)have)) : have;
-        if (count0 + need < n) {
-          thr = bin_value(b);
-          cnt = have;
-          r = need;
-          n = count0 + need;
-          S = mass0 + (double)need * w;
-        }
-      }
+      if (b < 0) continue;  // rounding left the target above all words
+      const double w = sh.v.weight[b];
+      const int have = (int)sh.v.count[b];
+      int need = k - count0;
+      if (by_mass) need = w > 0.0 ? max(1, (int)fmin(ceil((target - mass0) / w), (double)have)) : have;
+      if (count0 + need >= n) continue;
+      thr = bin_value(b);
+      cnt = have;
+      r = need;
+      n = count0 + need;
+      S = mass0 + (double)need * w;
     }
     if (z_min > thr) {
       if (fabsf(z_min) < bin_value(kMid + 1)) return false;
@@ -1067,7 +1105,7 @@ struct RowWork {
                     if (partial)
                       same += __popcll(__ballot(bf16_lo(x.v[j][q]) == thr)) + __popcll(__ballot(bf16_hi(x.v[j][q]) == thr));
                   }
-                if (mid_kept) each_mid(tile, least, [&](float z) { s += weight(z); });
+                if (mid_kept) each_mid(x, least, [&](float z) { s += weight(z); });
                 s = wave_sum_dpp(s);
                 if (lane == 0) {
                   rec.sum[tile] = s;
@@ -1086,82 +1124,55 @@ struct RowWork {
 
   // ---- draws ----
 
-  // Wave 0: the tile's first kept word at which the kept weights pass `left`, or its last kept word.
-  __device__ __forceinline__ int pick(int tile, double left, float thr, int tie) const {
-    const int lane = threadIdx.x & 63;
-    Tile<Tin> x;
-    x.load(row, V, tile);
-    // the vector and the lane that hold it
-    double s[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      s[j] = 0.0;
-#pragma unroll
-      for (int e = 0; e < EPV; ++e)
-        if (kept(x.at(j, e), Tile<Tin>::col(tile, j, e), thr, tie)) s[j] += weight(x.at(j, e));
-    }
-    int at_j = -1, at_l = 0, last_j = 0, last_l = 0;
-    double run = 0.0, base = 0.0;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const double incl = run + scan_add(s[j]);
-      const uint64_t over = __ballot(s[j] > 0.0 && incl > left), some = __ballot(s[j] > 0.0);
-      if (at_j < 0 && over) {
-        at_j = j;
-        at_l = __ffsll((unsigned long long)over) - 1;
-        base = readlane_f64(incl - s[j], at_l);
+  // The first kept word at which the kept weights pass `target`, from the tiles' sums in rec.sum: its tile, then its
+  // words, a few to a thread; the last kept word where rounding leaves none.
+  __device__ __forceinline__ int draw(double target, float thr, int tie) {
+    constexpr int kEach = (Tile<Tin>::kWords + NT - 1) / NT;
+    const int tid = threadIdx.x;
+    double left = target, total;
+    int tile = -1, last = -1;
+    for (int i0 = 0; i0 < tiles && tile < 0; i0 += NT) {
+      const int i = i0 + tid;
+      const double v = i < tiles ? rec.sum[i] : 0.0;
+      const double incl = block_scan(v, total);
+      const int at = block_min(v > 0.0 && incl > left ? i : INT_MAX);
+      last = max(last, block_max(v > 0.0 ? i : -1));
+      if (at != INT_MAX) {
+        if (i == at) sh.d0 = left - (incl - v);
+        __syncthreads();
+        left = sh.d0;
+        tile = at;
+      } else {
+        left -= total;
       }
-      if (some) {
-        last_j = j;
-        last_l = 63 - __clzll((long long)some);
-      }
-      run = readlane_f64(incl, 63);
     }
-    if (at_j < 0) {
-      at_j = last_j;
-      at_l = last_l;
+    if (tile < 0) {
+      tile = last;
       left = INFINITY;
     }
-    // its words, one to a lane
-    u32x4 v = x.v[0];
-#pragma unroll
-    for (int j = 1; j < NV; ++j)
-      if (at_j == j) v = x.v[j];
-    uint32_t d = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t w = __builtin_amdgcn_readlane(v[q], at_l);
-      if (lane * (int)sizeof(Tin) / 4 == q) d = w;
-    }
-    const float z = sizeof(Tin) == 4 ? __uint_as_float(d) : (lane & 1) ? bf16_hi(d) : bf16_lo(d);
-    const int col = tile * Tile<Tin>::kWords + (at_j * 64 + at_l) * EPV + lane;
-    const double w = lane < EPV && kept(z, col, thr, tie) ? weight(z) : 0.0;
-    const double incl = base + scan_add(w);
-    const uint64_t over = __ballot(w > 0.0 && incl > left), some = __ballot(w > 0.0);
-    const int e = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll((long long)(some | 1ull));
-    return tile * Tile<Tin>::kWords + (at_j * 64 + at_l) * EPV + e;
-  }
-
-  // The first kept word at which the kept weights pass `target`, from the tiles' sums in rec.sum.
-  __device__ __forceinline__ int draw(double target, float thr, int tie) const {
-    double before = 0.0;
-    int at = INT_MAX, last = -1;
-    for (int i0 = 0; i0 < tiles && at == INT_MAX; i0 += NT) {
-      const int i = i0 + threadIdx.x;
-      const double v = i < tiles ? rec.sum[i] : 0.0;
-      double total;
-      const double incl = before + block_scan(v, total);
-      const bool here = v > 0.0 && incl > target;
-      at = block_min(here ? i : INT_MAX);
-      if (i == at) sh.d0 = target - (incl - v);
-      last = max(last, block_max(v > 0.0 ? i : -1));
-      before += total;
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {
-      const bool there = at != INT_MAX;
-      const int col = pick(there ? at : last, there ? sh.d0 : (double)INFINITY, thr, tie);
-      if (threadIdx.x == 0) sh.i0 = col;
+    const int col0 = tile * Tile<Tin>::kWords + tid * kEach;
+    auto word = [&](int e) {
+      const int col = col0 + e;
+      if (tid * kEach + e >= Tile<Tin>::kWords || col >= V) return 0.0;
+      const float z = load_elem(row + col);
+      return kept(z, col, thr, tie) ? weight(z) : 0.0;
+    };
+    double s = 0.0;
+#pragma unroll 1
+    for (int e = 0; e < kEach; ++e) s += word(e);
+    const double incl = block_scan(s, total);
+    const int first = block_min(s > 0.0 && incl > left ? tid : INT_MAX), end = block_max(s > 0.0 ? tid : -1);
+    if (tid == (first != INT_MAX ? first : end)) {
+      double run = incl - s;
+      int col = col0;
+#pragma unroll 1
+      for (int e = 0; e < kEach; ++e) {
+        const double v = word(e);
+        run += v;
+        if (v > 0.0) col = col0 + e;  // the last one where the sum in another order does not pass
+        if (v > 0.0 && run > left) break;
+      }
+      sh.i0 = col;
     }
     __syncthreads();
     return sh.i0;
@@ -1169,31 +1180,41 @@ struct RowWork {
 
   // ---- bounds ----
 
-  // A lower bound of the k-th largest of the n partial maxima in sh.sub, and so of the row's k-th word: the upper 20 bits
-  // of its key, each wave trying another value of the next ones.
+  // A lower bound of the k-th largest of the n partial maxima in sh.sub, and so of the row's k-th word: the upper 16 bits
+  // of its key, 8 at a time.
   __device__ __forceinline__ float kth_bound(int n, int k) const {
-    constexpr int kBits = NW == 16 ? 4 : 3;
-    static_assert(NW == 1 << kBits, "waves to values");
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    uint32_t key[kMaxSubs / 64];
-#pragma unroll
-    for (int i = 0; i < kMaxSubs / 64; ++i) key[i] = i * 64 + lane < n ? order_key(sh.sub[i * 64 + lane]) : 0u;
+    const int tid = threadIdx.x;
     uint32_t t = 0;
-    int parity = 0;
 #pragma unroll 1
-    for (int shift = 32 - kBits; shift > 12 - kBits; shift -= kBits) {
-      const uint32_t cand = t + ((uint32_t)wv << shift);
-      int have = 0;
-#pragma unroll
-      for (int i = 0; i < kMaxSubs / 64; ++i)
-        if (i * 64 < n) have += __popcll(__ballot(key[i] >= cand));
-      if (lane == 0) sh.wi[parity][wv] = have >= k;
+    for (int shift = 24; shift >= 16; shift -= 8) {
+      if (tid < 256) sh.radix[tid] = 0u;
       __syncthreads();
-      const uint64_t mask = __ballot(lane < NW && sh.wi[parity][lane & (NW - 1)] != 0);
-      t += (uint32_t)(63 - __clzll((long long)(mask | 1ull))) << shift;
-      parity ^= 1;
+      for (int i = tid; i < n; i += NT) {
+        const uint32_t key = order_key(sh.sub[i]);
+        if (shift == 24 || (key ^ t) >> 24 == 0) atomicAdd(&sh.radix[(key >> shift) & 255], 1u);
+      }
+      __syncthreads();
+      if (tid < 64) {  // four bins to a lane, from the largest down
+        int q[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          q[i] = (int)sh.radix[255 - (tid * 4 + i)];
+          sum += q[i];
+        }
+        int before = scan_add(sum) - sum;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (before < k && before + q[i] >= k) {
+            sh.key = t | (uint32_t)(255 - (tid * 4 + i)) << shift;
+            sh.i0 = before;
+          }
+          before += q[i];
+        }
+      }
+      __syncthreads();
+      t = sh.key;
+      k -= sh.i0;
     }
-    __syncthreads();
     return t > order_key(kLiveMin) ? key_value(t) : kLiveMin;
   }
 
@@ -1244,7 +1265,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
     w.each_tile([](int) { return true; },
                 [&](const Tile<Tin>& x, int tile) {
                   if constexpr (Work::kByValue) {
-                    if (mode == kCount) w.count_values(x, tile);
+                    if (mode == kCount) w.count_values(x);
                   }
                   const TileStats s = tile_stats<Tin>(x, mode, st.c);
                   if (fine && (lane & 7) == 0) sh.sub[tile * kSubs + (lane >> 3)] = s.sub;
@@ -1300,7 +1321,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
       live += sh.wi[0][i];
       bad |= sh.wi[1][i] != 0;
     }
-    __syncthreads();
+    __syncthreads();  // both sets are free again
   }
   w.m = m;
 
@@ -1375,7 +1396,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
           if ((mode == kCount || listed > kCap) && m < kLimit && lo > -kLimit) {
             if (mode != kCount) {
               w.clear_values();
-              w.each_tile([](int) { return true; }, [&](const Tile<Tin>& x, int tile) { w.count_values(x, tile); });
+              w.each_tile([](int) { return true; }, [&](const Tile<Tin>& x, int) { w.count_values(x); });
               __syncthreads();
             }
             typename Work::ValueCut cut;
@@ -1384,7 +1405,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
               thr = cut.thr;
               n = cut.n;
               S = cut.S;
-              if (n - cut.r + cut.of <= kCap) listed = w.gather(thr, INFINITY);
+              if (n - cut.r + cut.of <= kRankSort) listed = w.gather(thr, INFINITY);
               else if (DRAW) tie = w.value_sums(cut);
               else tie = w.value_tie(cut);
             }
@@ -1420,28 +1441,23 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
           thr = w.list_value(n - 1);
           tie = w.list_index(n - 1);
           __syncthreads();
-          if (DRAW) {
+          if (DRAW && n <= kRankSort) {
             // the kept words in the order of their indices, smallest first: keys that fall as the index grows
-            for (int i = tid; i < n; i += NT) {
-              const unsigned long long q = sh.l.key[i];
-              sh.l.key[i] = (q << 32) | (q >> 32);
-            }
+            const unsigned long long q = tid < n ? sh.l.key[tid] : 0ull;
+            __syncthreads();
+            if (tid < n) sh.l.key[tid] = (q << 32) | (q >> 32);
             __syncthreads();
             w.sort_list(n);
-            double before = 0.0;
-            int at = INT_MAX, last = 0;
-            const double target = (double)u * S;
-            for (int i0 = 0; i0 < n && at == INT_MAX; i0 += NT) {
-              const int i = i0 + tid;
-              const double v = i < n ? w.weight(key_value((uint32_t)sh.l.key[i])) : 0.0;
-              double all;
-              const double incl = before + w.block_scan(v, all);
-              at = w.block_min(v > 0.0 && incl > target ? i : INT_MAX);
-              last = max(last, w.block_max(v > 0.0 ? i : 0));
-              before += all;
-            }
+            const double v = tid < n ? w.weight(key_value((uint32_t)sh.l.key[tid])) : 0.0;
+            double all;
+            const double incl = w.block_scan(v, all);
+            const int at = w.block_min(v > 0.0 && incl > (double)u * S ? tid : INT_MAX);
+            const int last = w.block_max(v > 0.0 ? tid : 0);
             act = (int)~(uint32_t)(sh.l.key[at == INT_MAX ? last : at] >> 32);
             drawn = true;
+          } else if (DRAW) {
+            int all;
+            w.kept_sums(thr, tie, all);
           }
         } else if (!cut_known) {
           thr = kLiveMin;
