@@ -132,6 +132,15 @@ __device__ __forceinline__ T scan_add(T v) {
   return v;
 }
 
+// A value that every lane has, in scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float((uint32_t)uniform((int)__float_as_uint(v))); }
+__device__ __forceinline__ double uniform(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)uniform((int)(uint32_t)u), hi = (uint32_t)uniform((int)(uint32_t)(u >> 32));
+  return __builtin_bit_cast(double, (uint64_t)lo | ((uint64_t)hi << 32));
+}
+
 template <typename F>
 __device__ __forceinline__ int wave_reduce(int v, F f) {
   v = f(v, (int)dpp_u32<0xB1>((uint32_t)v));
@@ -185,13 +194,12 @@ struct Tile {
   static constexpr int EPV = 16 / (int)sizeof(Tin), NV = kTileVecs, kWords = 64 * EPV * NV;
   u32x4 v[NV];
 
-  __device__ __forceinline__ static int col(int tile, int j, int e) {
-    return tile * kWords + (j * 64 + (threadIdx.x & 63)) * EPV + e;
+  __device__ __forceinline__ static int col(int tile, int j, int e, int lane = threadIdx.x & 63) {
+    return tile * kWords + (j * 64 + lane) * EPV + e;
   }
-  // Vector j of a tile that the row's end may cut.
-  __device__ __forceinline__ static u32x4 load_one(const Tin* row, int V, int tile, int j) {
+  // The vector at column c0, which the row's end may cut.
+  __device__ __forceinline__ static u32x4 load_one(const Tin* row, int V, int c0) {
     typedef typename VecAt<Tin>::type u32x4_any;
-    const int c0 = col(tile, j, 0);
     if (c0 + EPV <= V) return *reinterpret_cast<const u32x4_any*>(row + c0);
     u32x4 r;
 #pragma unroll
@@ -206,15 +214,15 @@ struct Tile {
     }
     return r;
   }
-  __device__ __forceinline__ void load(const Tin* row, int V, int tile) {
+  __device__ __forceinline__ void load(const Tin* row, int V, int tile, int lane = threadIdx.x & 63) {
     typedef typename VecAt<Tin>::type u32x4_any;
-    if ((tile + 1) * kWords <= V) {
+    if (__all((tile + 1) * kWords <= V)) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) v[j] = *reinterpret_cast<const u32x4_any*>(row + col(tile, j, 0));
+      for (int j = 0; j < NV; ++j) v[j] = *reinterpret_cast<const u32x4_any*>(row + col(tile, j, 0, lane));
     } else {
 #pragma unroll 1
       for (int j = 0; j < NV; ++j) {
-        const u32x4 r = load_one(row, V, tile, j);
+        const u32x4 r = load_one(row, V, col(tile, j, 0, lane));
 #pragma unroll
         for (int i = 0; i < NV; ++i)
           if (i == j) v[i] = r;
@@ -401,6 +409,7 @@ struct RowShared {
     } v;
   };
   float sub[kMaxSubs];
+  uint16_t block[kMaxSubs];
   double wd[2][kMaxNW];
   int wi[2][kMaxNW];
   float wf[2][kMaxNW];
@@ -430,36 +439,36 @@ struct RowWork {
   float m;   // the row's maximum
   double c;  // log2(e) / tau
   float x_lo;  // words below it are not looked at
+  bool fine;   // sh.sub holds every tile's partial maxima
 
   int turn = 0;  // which of the two sets of sh.w* the next reduction takes
 
   // ---- over the workgroup: the same value in every thread.  One barrier each: a set is written again after the next
   // reduction's barrier, when every wave has read it. ----
   __device__ __forceinline__ double block_sum(double v) {
-    const int b = turn;
+    const int b = turn, lane = threadIdx.x & 63;
     turn ^= 1;
     v = wave_sum_dpp(v);
-    if ((threadIdx.x & 63) == 0) sh.wd[b][threadIdx.x >> 6] = v;
+    if (lane == 0) sh.wd[b][threadIdx.x >> 6] = v;
     __syncthreads();
-    double r = 0.0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) r += sh.wd[b][i];
-    return r;
+    return readlane_f64(row16_sum(lane < NW ? sh.wd[b][lane] : 0.0), 0);
   }
   template <typename F>
-  __device__ __forceinline__ int block_reduce(int v, F f) {
-    const int b = turn;
+  __device__ __forceinline__ int block_reduce(int v, F f) {  // f(a, a) = a
+    const int b = turn, lane = threadIdx.x & 63;
     turn ^= 1;
     v = wave_reduce(v, f);
-    if ((threadIdx.x & 63) == 0) sh.wi[b][threadIdx.x >> 6] = v;
+    if (lane == 0) sh.wi[b][threadIdx.x >> 6] = v;
     __syncthreads();
-    int r = sh.wi[b][0];
-#pragma unroll
-    for (int i = 1; i < NW; ++i) r = f(r, sh.wi[b][i]);
-    return r;
+    return wave_reduce(sh.wi[b][lane & (NW - 1)], f);
   }
   __device__ __forceinline__ int block_sum(int v) {
-    return block_reduce(v, [](int a, int b) { return a + b; });
+    const int b = turn, lane = threadIdx.x & 63;
+    turn ^= 1;
+    v = scan_add(v);
+    if (lane == 63) sh.wi[b][threadIdx.x >> 6] = v;
+    __syncthreads();
+    return __builtin_amdgcn_readlane(scan_add(lane < NW ? sh.wi[b][lane] : 0), 63);
   }
   __device__ __forceinline__ int block_min(int v) {
     return block_reduce(v, [](int a, int b) { return min(a, b); });
@@ -478,21 +487,15 @@ struct RowWork {
       sh.wd[b][wv] = v;
     }
     __syncthreads();
-    double before = 0.0;
-    int n_before = 0;
-    all_n = 0;
-    all_v = 0.0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      if (i == wv) {
-        before = all_v;
-        n_before = all_n;
-      }
-      all_n += sh.wi[b][i];
-      all_v += sh.wd[b][i];
+    const int lane = threadIdx.x & 63, w = uniform(wv);
+    const int wn = scan_add(lane < NW ? sh.wi[b][lane] : 0);
+    const double wd = scan_add(lane < NW ? sh.wd[b][lane] : 0.0);
+    all_n = __builtin_amdgcn_readlane(wn, 63);
+    all_v = readlane_f64(wd, 63);
+    if (w > 0) {
+      n += __builtin_amdgcn_readlane(wn, w - 1);
+      v += readlane_f64(wd, w - 1);
     }
-    n += n_before;
-    v += before;
   }
   __device__ __forceinline__ double block_scan(double v, double& all) {
     int n = 0, all_n;
@@ -509,17 +512,16 @@ struct RowWork {
       while (t < tiles && !want(t)) t += NW;
       return t;
     };
-    int tile = next(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    int tile = tiles, after = next(uniform((int)(threadIdx.x >> 6)));
     Tile<Tin> x;
-    if (tile < tiles) x.load(row, V, tile);
-    while (tile < tiles) {
-      const int after = next(tile + NW);
+    do {
       Tile<Tin> y;
       if (after < tiles) y.load(row, V, after);
-      f(x, tile);
+      if (tile < tiles) f(x, tile);
       x = y;
       tile = after;
-    }
+      after = next(after + NW);
+    } while (tile < tiles);
   }
 
   // The same with f(vector, tile, j) for each of their vectors, then done(tile).
@@ -540,48 +542,55 @@ struct RowWork {
 
   // ---- a list of words in LDS ----
 
-  // The words of [lo, hi] appended to the list while it has room; returns how many there are, or more than kCap.
+  // The words of [lo, hi] in the list, in no order; returns how many there are, or more than kCap.  Eight lanes read the
+  // words of one partial maximum, only of those that reach lo; without partial maxima, of every tile that does.
   __device__ __forceinline__ int gather(float lo, float hi) {
     const int tid = threadIdx.x, lane = tid & 63;
     __syncthreads();
-    if (tid == 0) sh.n = 0;
+    if (tid == 0) sh.n = sh.bin = 0;
     __syncthreads();
-    each_tile(
-        [&](int tile) {
-          return rec.max[tile] >= lo && __builtin_amdgcn_readfirstlane(*(volatile int*)&sh.n) <= kCap;
-        },
-        [&](const Tile<Tin>& x, int tile) {
-          int all = 0;
-#pragma unroll 1
-          for (int j = 0; j < NV; ++j) {
-            const u32x4 v = x.vec(j);
-            if (!__any(vec_max<Tin>(v, -INFINITY) >= lo)) continue;
+    int blocks = tiles * kSubs;
+    if (fine) {
+      for (int i = tid; i < blocks; i += NT)
+        if (sh.sub[i] >= lo) sh.block[atomicAdd(&sh.bin, 1)] = (uint16_t)i;
+      __syncthreads();
+      blocks = uniform(sh.bin);
+    }
+    for (int g0 = 0; g0 < blocks; g0 += NT / kSubs) {
+      const int g = g0 + tid / kSubs;
+      const int block = g < blocks ? (fine ? sh.block[g] : g) : -1;
+      const int tile = block >= 0 ? block / kSubs : 0, own = (block & (kSubs - 1)) * 8 + (tid & 7);
+      if (uniform(*(volatile int*)&sh.n) > kCap) break;
+      const bool some = block >= 0 && rec.max[tile] >= lo;
+      if (!__any(some)) continue;
+      Tile<Tin> x;
+      x.load(row, V, tile, own);
+      int mine = 0;
 #pragma unroll
-            for (int e = 0; e < EPV; ++e) all += __popcll(__ballot(elem<Tin>(v, e) >= lo && elem<Tin>(v, e) <= hi));
-          }
-          if (all == 0) return;
-          int at = 0;
-          if (lane == 0) at = atomicAdd(&sh.n, all);
-          at = __builtin_amdgcn_readfirstlane(at);
-          if (at + all > kCap) return;
-#pragma unroll 1
-          for (int j = 0; j < NV; ++j) {
-            const u32x4 v = x.vec(j);
-            if (!__any(vec_max<Tin>(v, -INFINITY) >= lo)) continue;
+      for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int e = 0; e < EPV; ++e) {
-              const float z = elem<Tin>(v, e);
-              const bool in = z >= lo && z <= hi;
-              const uint64_t mask = __ballot(in);
-              if (in)
-                sh.l.key[at + (int)__popcll(mask & ((1ull << lane) - 1))] =
-                    ((unsigned long long)order_key(z) << 32) | (uint32_t)~x.col(tile, j, e);
-              at += __popcll(mask);
-            }
+        for (int e = 0; e < EPV; ++e) mine += x.at(j, e) >= lo && x.at(j, e) <= hi;
+      mine = some ? mine : 0;
+      const int incl = scan_add(mine), all = __builtin_amdgcn_readlane(incl, 63);
+      if (all == 0) continue;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&sh.n, all);
+      at = uniform(at);
+      if (at + all > kCap) break;
+      at += incl - mine;
+      if (mine > 0) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) {
+            const float z = x.at(j, e);
+            if (z >= lo && z <= hi)
+              sh.l.key[at++] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e, own);
           }
-        });
+      }
+    }
     __syncthreads();
-    return sh.n;
+    return uniform(sh.n);
   }
 
   // Sorts the n keys in sh.l.key, all different, largest first.
@@ -720,7 +729,7 @@ struct RowWork {
       if (lane == 0) sh.i0 = col;
     }
     __syncthreads();
-    const int col = sh.i0;
+    const int col = uniform(sh.i0);
     __syncthreads();
     return col;
   }
@@ -831,10 +840,10 @@ struct RowWork {
       }
     }
     __syncthreads();
-    const int b = sh.bin;
-    count0 = sh.i0;
-    mass0 = sh.d0;
-    in_bin = sh.n;
+    const int b = uniform(sh.bin);
+    count0 = uniform(sh.i0);
+    mass0 = uniform(sh.d0);
+    in_bin = uniform(sh.n);
     __syncthreads();
     return b;
   }
@@ -888,9 +897,9 @@ struct RowWork {
     sort_list(n);
     scan_list(n, mass0);
     const int r = by_mass ? first_reaching(n, target) : max(1, min(k - count0, n));
-    cut.thr = list_value(r - 1);
-    cut.tie = list_index(r - 1);
-    cut.mass = sh.l.cum[r - 1];
+    cut.thr = uniform(list_value(r - 1));
+    cut.tie = uniform(list_index(r - 1));
+    cut.mass = uniform(sh.l.cum[r - 1]);
     cut.count = count0 + r;
     __syncthreads();
     return cut;
@@ -978,47 +987,56 @@ struct RowWork {
     // each thread kEach bins, from the largest value down; the last one holds the masked words
     const double mid = (double)sh.v.mid * 0x1p-44 * exp2_neg(mid_top);
     auto bin_at = [&](int i) { return kValues - 1 - (tid * kEach + i); };
-    int cn = 0;
-    double cm = 0.0;
+    int q[kEach], my_n = 0;
+    double w[kEach], my_m = 0.0;  // counts, weights of the bins
+#pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int b = bin_at(i);
-      if (b < 1) continue;
-      const int q = (int)sh.v.count[b];
-      const double w = q > 0 && b != kMid ? weight(bin_value(b)) : 0.0;
-      sh.v.weight[b] = w;
-      cn += q;
-      cm += b == kMid ? mid : (double)q * w;
+      q[i] = b >= 1 ? (int)sh.v.count[b] : 0;
     }
-    const int my_n = cn;
-    const double my_m = cm;
-    int all_n;
-    double all_m;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int b = bin_at(i);
+      w[i] = 0.0;
+      if (b >= 0) {
+        const double one = q[i] > 0 && b != kMid ? weight(bin_value(b)) : 0.0;
+        sh.v.weight[b] = one;
+        w[i] = b == kMid ? mid : (double)q[i] * one;
+      }
+      my_n += q[i];
+      my_m += w[i];
+    }
+    int cn = my_n, all_n;
+    double cm = my_m, all_m;
     block_scan(cn, cm, all_n, all_m);
     const int n0 = cn - my_n;
     const double m0 = cm - my_m;
     // the first bin up to which the counts (weights) reach the target
-    auto find = [&](bool by_mass, int k_, double target, int& count0, double& mass0) {
-      if (tid == 0) sh.bin = -1;
+    auto find = [&](bool by_mass, int k_, double target, int& count0, double& mass0, int& have) {
       const int first = block_min(my_n > 0 && (by_mass ? m0 + my_m >= target : n0 + my_n >= k_) ? tid : INT_MAX);
-      if (tid == (first == INT_MAX ? 0 : first)) {
+      if (first == INT_MAX) return -1;
+      if (tid == first) {
         int a = n0;
-        double w = m0;
+        double v = m0;
+        bool over = false;
+#pragma unroll
         for (int i = 0; i < kEach; ++i) {
-          const int b = bin_at(i);
-          if (b < 1 || sh.v.count[b] == 0) continue;
-          const double q = b == kMid ? mid : (double)sh.v.count[b] * sh.v.weight[b];
-          sh.bin = b;  // the last one with a word, where rounding leaves the target above them
-          sh.i0 = a;
-          sh.d0 = w;
-          if (by_mass ? w + q >= target : a + (int)sh.v.count[b] >= k_) break;
-          a += (int)sh.v.count[b];
-          w += q;
+          if (q[i] > 0 && !over) {
+            sh.bin = bin_at(i);  // the last one with a word, where the sum in another order does not reach
+            sh.i0 = a;
+            sh.d0 = v;
+            sh.n = q[i];
+            a += q[i];
+            v += w[i];
+            over = by_mass ? v >= target : a >= k_;
+          }
         }
       }
       __syncthreads();
-      const int b = first == INT_MAX ? -1 : sh.bin;
-      count0 = sh.i0;
-      mass0 = sh.d0;
+      count0 = uniform(sh.i0);
+      mass0 = uniform(sh.d0);
+      have = uniform(sh.n);
+      const int b = uniform(sh.bin);
       __syncthreads();
       return b;
     };
@@ -1030,31 +1048,32 @@ struct RowWork {
     for (int by_mass = 0; by_mass < 2; ++by_mass) {
       if (by_mass ? !p_on : !(k_on && k < all_n)) continue;
       const double target = p * S;
-      int count0;
+      int count0, have;
       double mass0;
-      const int b = find(by_mass, k, target, count0, mass0);
+      const int b = find(by_mass, k, target, count0, mass0, have);
       if (b == kMid) return false;
       if (b < 0) continue;  // rounding left the target above all words
-      const double w = sh.v.weight[b];
-      const int have = (int)sh.v.count[b];
+      const double one = uniform(sh.v.weight[b]);
       int need = k - count0;
-      if (by_mass) need = w > 0.0 ? max(1, (int)fmin(ceil((target - mass0) / w), (double)have)) : have;
+      if (by_mass) need = one > 0.0 ? max(1, (int)fmin(ceil((target - mass0) / one), (double)have)) : have;
       if (count0 + need >= n) continue;
       thr = bin_value(b);
       cnt = have;
       r = need;
       n = count0 + need;
-      S = mass0 + (double)need * w;
+      S = mass0 + (double)need * one;
     }
     if (z_min > thr) {
       if (fabsf(z_min) < bin_value(kMid + 1)) return false;
       int qn = 0;
       double qm = 0.0;
+#pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int b = bin_at(i);
-        if (b < 1 || !(bin_value(b) >= z_min)) continue;
-        qn += (int)sh.v.count[b];
-        qm += b == kMid ? mid : (double)sh.v.count[b] * sh.v.weight[b];
+        if (b >= 1 && bin_value(b) >= z_min) {
+          qn += q[i];
+          qm += w[i];
+        }
       }
       n = block_sum(qn);
       S = block_sum(qm);
@@ -1140,7 +1159,7 @@ struct RowWork {
       if (at != INT_MAX) {
         if (i == at) sh.d0 = left - (incl - v);
         __syncthreads();
-        left = sh.d0;
+        left = uniform(sh.d0);
         tile = at;
       } else {
         left -= total;
@@ -1151,31 +1170,33 @@ struct RowWork {
       left = INFINITY;
     }
     const int col0 = tile * Tile<Tin>::kWords + tid * kEach;
-    auto word = [&](int e) {
-      const int col = col0 + e;
-      if (tid * kEach + e >= Tile<Tin>::kWords || col >= V) return 0.0;
-      const float z = load_elem(row + col);
-      return kept(z, col, thr, tie) ? weight(z) : 0.0;
-    };
+    float z[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+      z[e] = tid * kEach + e < Tile<Tin>::kWords && col0 + e < V ? load_elem(row + col0 + e) : -INFINITY;
+    auto word = [&](int e) { return z[e] >= kLiveMin && kept(z[e], col0 + e, thr, tie) ? weight(z[e]) : 0.0; };
     double s = 0.0;
-#pragma unroll 1
+#pragma unroll
     for (int e = 0; e < kEach; ++e) s += word(e);
     const double incl = block_scan(s, total);
     const int first = block_min(s > 0.0 && incl > left ? tid : INT_MAX), end = block_max(s > 0.0 ? tid : -1);
     if (tid == (first != INT_MAX ? first : end)) {
       double run = incl - s;
       int col = col0;
-#pragma unroll 1
+      bool over = false;
+#pragma unroll
       for (int e = 0; e < kEach; ++e) {
         const double v = word(e);
         run += v;
-        if (v > 0.0) col = col0 + e;  // the last one where the sum in another order does not pass
-        if (v > 0.0 && run > left) break;
+        if (v > 0.0 && !over) {
+          col = col0 + e;  // the last one where the sum in another order does not pass
+          over = run > left;
+        }
       }
       sh.i0 = col;
     }
     __syncthreads();
-    return sh.i0;
+    return uniform(sh.i0);
   }
 
   // ---- bounds ----
@@ -1212,8 +1233,8 @@ struct RowWork {
         }
       }
       __syncthreads();
-      t = sh.key;
-      k -= sh.i0;
+      t = (uint32_t)uniform((int)sh.key);
+      k -= uniform(sh.i0);
     }
     return t > order_key(kLiveMin) ? key_value(t) : kLiveMin;
   }
@@ -1233,7 +1254,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
   extern __shared__ double tile_mem[];
   typedef RowWork<Tin, NT> Work;
   constexpr int NW = NT / 64;
-  const int t = row0 + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int t = row0 + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const Tin* row = static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld;
   const Settings st = load_settings(a.par, t);
   float u = 0.f;
@@ -1251,7 +1272,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
   const bool fine = a.tiles * kSubs <= kMaxSubs;
   const RowTiles rec{tile_mem, reinterpret_cast<float*>(tile_mem + a.tiles),
                      reinterpret_cast<int*>(tile_mem + a.tiles) + a.tiles};
-  Work w{sh, rec, row, a.V, a.tiles, 0.f, st.c, kLiveMin};
+  Work w{sh, rec, row, a.V, a.tiles, 0.f, st.c, kLiveMin, fine};
 
   // the tiles' records
   float m = -INFINITY, lo = INFINITY;
@@ -1312,15 +1333,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
       sh.wi[1][wv] = any_bad;
     }
     __syncthreads();
-    live = 0;
-    bad = false;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      m = fmaxf(m, sh.wf[0][i]);
-      lo = fminf(lo, sh.wf[1][i]);
-      live += sh.wi[0][i];
-      bad |= sh.wi[1][i] != 0;
-    }
+    const int q = lane & (NW - 1);
+    m = uniform(row16_max(sh.wf[0][q]));
+    lo = uniform(-row16_max(-sh.wf[1][q]));
+    live = __builtin_amdgcn_readlane(scan_add(lane < NW ? sh.wi[0][lane] : 0), 63);
+    bad = __any(sh.wi[1][q] != 0);
     __syncthreads();  // both sets are free again
   }
   w.m = m;
@@ -1359,7 +1376,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
       }
       __syncthreads();
       thr = m;
-      tie = sh.i0;
+      tie = uniform(sh.i0);
       n = 1;
       S = 1.0;
       if (DRAW) act = tie;
@@ -1436,10 +1453,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
               n = min(n, w.block_sum(c));
             }
             n = max(n, 1);
-            S = sh.l.cum[n - 1];
+            S = uniform(sh.l.cum[n - 1]);
           }
-          thr = w.list_value(n - 1);
-          tie = w.list_index(n - 1);
+          thr = uniform(w.list_value(n - 1));
+          tie = uniform(w.list_index(n - 1));
           __syncthreads();
           if (DRAW && n <= kRankSort) {
             // the kept words in the order of their indices, smallest first: keys that fall as the index grows
@@ -1453,7 +1470,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
             const double incl = w.block_scan(v, all);
             const int at = w.block_min(v > 0.0 && incl > (double)u * S ? tid : INT_MAX);
             const int last = w.block_max(v > 0.0 ? tid : 0);
-            act = (int)~(uint32_t)(sh.l.key[at == INT_MAX ? last : at] >> 32);
+            act = uniform((int)~(uint32_t)(sh.l.key[at == INT_MAX ? last : at] >> 32));
             drawn = true;
           } else if (DRAW) {
             int all;
