@@ -14,13 +14,14 @@
 // workgroup per row works on the tiles' records and re-reads only the tiles that it needs:
 //   nothing cut     a draw picks its tile by the tiles' sums and re-reads that one;
 //   few candidates  a lower bound of the threshold (the k-th largest of the partial maxima; for top-p, the weight below
-//                   which all live words together weigh less than (1 - p) S; min-p's own) leaves at most kCap words:
-//                   they are gathered in LDS, sorted, and the cut read off their prefix sums;
+//                   which all live words together weigh less than (1 - p) S; min-p's own) leaves at most kCap words: they
+//                   are gathered in LDS, and the cut is read off the sorted words' prefix sums (up to kSorted), or found
+//                   as in the last case, in the list instead of the row;
 //   many, bf16      a count of each value (bf16 logits below 64 in size have 5,377 that are told apart); counts times weights,
 //                   summed from the top, give the cut, and a table of the values' weights the tiles' kept sums;
-//   many, else      histograms: words fall into kBins bins of a quarter of a power of two of weight, each bin's count
-//                   and weight are summed, the bin that holds the cut is split again by the bits of its logits until at
-//                   most kCap words (gathered and sorted) or one repeated value are left.
+//   many, else      histograms: words fall into kBins bins of 1/32 of a power of two of weight, each bin's count and weight
+//                   are summed, the bin that holds the cut is split again by the bits of its logits until at most kSorted
+//                   words (gathered and sorted) or one repeated value are left.
 // Histogram weights are integers (weight relative to the bin's top, in 2^-44), so that atomics in any order give one sum.
 #include <hip/hip_runtime.h>
 #include <float.h>
@@ -37,9 +38,9 @@ namespace grpo {
 constexpr int kTileVecs = 4;       // a tile: 4 vectors of 16 bytes per lane, 2,048 bf16 words or 1,024 of fp32
 constexpr int kSubs = 8;           // partial maxima of a tile, each over 8 lanes' words
 constexpr int kMaxSubs = 1280;     // partial maxima (or tiles' maxima) that bound the k-th largest word
-constexpr int kCap = 2048;         // words that are sorted in LDS
-constexpr int kBins = 1024, kCols = 4;  // bins of 1/32 of a power of two of weight, each in kCols copies
-constexpr int kRankSort = 256;     // words that are sorted by counting
+constexpr int kCap = 2048;         // words that a list in LDS holds
+constexpr int kSorted = 256;       // words that are sorted
+constexpr int kBins = 1024, kCols = 2;  // bins of 1/32 of a power of two of weight, each in kCols copies
 constexpr int kMaxNW = 16;
 constexpr float kLimit = 64.f;     // logits that the count of values takes: below it in size
 constexpr float kLiveMin = -99999992.f;  // the smallest float above -1e8: the lowest live logit
@@ -383,6 +384,12 @@ __device__ __forceinline__ float bin_value(int bin) {
   return i == 0 ? 0.f : __uint_as_float(((uint32_t)mag << 16) | (i < 0 ? 0x80000000u : 0u));
 }
 
+// The bin of a logit below kLimit in size, less kMid.
+__device__ __forceinline__ int bin_index(float z) {
+  const int mag = (int)((__float_as_uint(z) & 0x7fffffffu) >> 16), i = max(0, mag - (kStepLo - 1));
+  return z < 0.f ? -i : i;
+}
+
 struct Cut {
   float thr;    // kept: z > thr, or z == thr and index <= tie
   int tie;
@@ -393,15 +400,15 @@ struct Cut {
 struct RowShared {
   union {
     struct {
-      unsigned long long mass[kBins * kCols];  // the list lies over it
+      unsigned long long mass[kBins * kCols];
       uint32_t count[kBins * kCols];
       double bin_mass[kBins];
       int bin_count[kBins];
+      unsigned long long key[kCap];      // a list of words: order_key, ~index
+      unsigned long long some[kSorted];  // a few of them
+      unsigned long long sorted[kSorted];
+      double cum[kSorted];               // prefix sums of the sorted ones' weights
     } h;
-    struct {
-      unsigned long long key[kCap];
-      double cum[kCap];
-    } l;
     struct {
       double weight[kValues];
       uint32_t count[kValues];
@@ -542,9 +549,9 @@ struct RowWork {
 
   // ---- a list of words in LDS ----
 
-  // The words of [lo, hi] in the list, in no order; returns how many there are, or more than kCap.  Eight lanes read the
-  // words of one partial maximum, only of those that reach lo; without partial maxima, of every tile that does.
-  __device__ __forceinline__ int gather(float lo, float hi) {
+  // The words of [lo, hi] in `list`, in no order; returns how many there are, or more than it has room for.  Eight lanes
+  // read the words of one partial maximum, only of those that reach lo; without partial maxima, of every tile that does.
+  __device__ __forceinline__ int gather(unsigned long long* list, int room, float lo, float hi) {
     const int tid = threadIdx.x, lane = tid & 63;
     __syncthreads();
     if (tid == 0) sh.n = sh.bin = 0;
@@ -560,7 +567,7 @@ struct RowWork {
       const int g = g0 + tid / kSubs;
       const int block = g < blocks ? (fine ? sh.block[g] : g) : -1;
       const int tile = block >= 0 ? block / kSubs : 0, own = (block & (kSubs - 1)) * 8 + (tid & 7);
-      if (uniform(*(volatile int*)&sh.n) > kCap) break;
+      if (uniform(*(volatile int*)&sh.n) > room) break;
       const bool some = block >= 0 && rec.max[tile] >= lo;
       if (!__any(some)) continue;
       Tile<Tin> x;
@@ -576,7 +583,7 @@ struct RowWork {
       int at = 0;
       if (lane == 0) at = atomicAdd(&sh.n, all);
       at = uniform(at);
-      if (at + all > kCap) break;
+      if (at + all > room) break;
       at += incl - mine;
       if (mine > 0) {
 #pragma unroll
@@ -585,7 +592,7 @@ struct RowWork {
           for (int e = 0; e < EPV; ++e) {
             const float z = x.at(j, e);
             if (z >= lo && z <= hi)
-              sh.l.key[at++] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e, own);
+              list[at++] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e, own);
           }
       }
     }
@@ -593,70 +600,39 @@ struct RowWork {
     return uniform(sh.n);
   }
 
-  // Sorts the n keys in sh.l.key, all different, largest first.
-  __device__ __forceinline__ void sort_list(int n) {
-    const int tid = threadIdx.x;
-    if (n <= kRankSort) {  // a word's place is the number of larger ones: kRanks threads count them for each
-      constexpr int kRanks = NT / kRankSort;
-      const int i = tid / kRanks;
-      const unsigned long long mine = i < n ? sh.l.key[i] : 0ull;
-      int rank = 0;
-      if (i < n)
-        for (int q = tid % kRanks; q < n; q += kRanks) rank += sh.l.key[q] > mine;
+  __device__ __forceinline__ static float word_of(unsigned long long key) { return key_value((uint32_t)(key >> 32)); }
+  __device__ __forceinline__ static int index_of(unsigned long long key) { return (int)~(uint32_t)key; }
+
+  // `to` = the n <= kSorted keys of `from`, all different, largest first; by_index: by the index alone, lowest first.  A
+  // key's place is the number of larger ones, which kEach threads count.
+  template <bool BY_INDEX>
+  __device__ __forceinline__ void sort_words(const unsigned long long* from, unsigned long long* to, int n) const {
+    constexpr int kEach = NT / kSorted;
+    const int tid = threadIdx.x, i = tid / kEach;
+    const unsigned long long mine = i < n ? from[i] : 0ull;
+    int place = 0;
+    if (i < n)
+      for (int q = tid % kEach; q < n; q += kEach)
+        place += BY_INDEX ? (uint32_t)from[q] > (uint32_t)mine : from[q] > mine;
 #pragma unroll
-      for (int o = 1; o < kRanks; o <<= 1) rank += __shfl_xor(rank, o, 64);
-      __syncthreads();
-      if (i < n && tid % kRanks == 0) sh.l.key[rank] = mine;
-      __syncthreads();
-      return;
-    }
-    int P = 2 * kRankSort;  // a bitonic sort, padded with zeros
-    while (P < n) P <<= 1;
-    for (int i = n + tid; i < P; i += NT) sh.l.key[i] = 0ull;
-    __syncthreads();
-    // Pairs at most 64 apart lie within the 128 keys of 64 neighbouring comparisons, which one wave makes: between such
-    // stages its own LDS accesses are in order and no other wave's matter.
-    for (int k = 2; k <= P; k <<= 1) {
-      for (int j = k >> 1; j > 0; j >>= 1) {
-        for (int q = tid; q < (P >> 1); q += NT) {
-          const int i = ((q & ~(j - 1)) << 1) | (q & (j - 1));
-          const unsigned long long x = sh.l.key[i], y = sh.l.key[i | j];
-          if ((x < y) == ((i & k) == 0)) {
-            sh.l.key[i] = y;
-            sh.l.key[i | j] = x;
-          }
-        }
-        if (j > 64 || (j == 1 && k >= 128)) __syncthreads();
-        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      }
-    }
+    for (int o = 1; o < kEach; o <<= 1) place += __shfl_xor(place, o, 64);
+    if (i < n && tid % kEach == 0) to[place] = mine;
     __syncthreads();
   }
 
-  __device__ __forceinline__ float list_value(int i) const { return key_value((uint32_t)(sh.l.key[i] >> 32)); }
-  __device__ __forceinline__ int list_index(int i) const { return (int)~(uint32_t)sh.l.key[i]; }
-
-  // sh.l.cum = the prefix sums of the list's weights, from `base` on.
-  __device__ __forceinline__ void scan_list(int n, double base) {
-    for (int i0 = 0; i0 < n; i0 += NT) {
-      const int i = i0 + threadIdx.x;
-      double total;
-      const double v = block_scan(i < n ? weight(list_value(i)) : 0.0, total);
-      if (i < n) sh.l.cum[i] = base + v;
-      base += total;
-    }
+  // sh.h.cum = the prefix sums of the n sorted words' weights, from `base` on.
+  __device__ __forceinline__ void scan_sorted(int n, double base) {
+    const int tid = threadIdx.x;
+    double total;
+    const double v = block_scan(tid < n ? weight(word_of(sh.h.sorted[tid])) : 0.0, total);
+    if (tid < n) sh.h.cum[tid] = base + v;
     __syncthreads();
   }
 
   // The least r >= 1 with cum[r - 1] >= target, or n.
   __device__ __forceinline__ int first_reaching(int n, double target) {
-    int r = n;
-    for (int i = threadIdx.x; i < n; i += NT)
-      if (sh.l.cum[i] >= target) {
-        r = i + 1;
-        break;
-      }
-    return block_min(r);
+    const int tid = threadIdx.x;
+    return block_min(tid < n && sh.h.cum[tid] >= target ? tid + 1 : n);
   }
 
   // ---- one value's words ----
@@ -737,69 +713,94 @@ struct RowWork {
   // ---- histograms of weight ----
 
   static constexpr double kPerOctave = 32.0;
-  __device__ __forceinline__ int bin_of(double t) const {
-    const double q = -kPerOctave * t;
-    return q < (double)(kBins - 1) ? (int)q : kBins - 1;
+  // How many 1/kPerOctave of an octave a word lies below the maximum.
+  __device__ __forceinline__ double steps(float z) const { return ((double)m - (double)z) * (c * kPerOctave); }
+  __device__ __forceinline__ int bin_of(float z) const { return (int)fmin(steps(z), (double)(kBins - 1)); }
+
+  // A weight w <= 1 in 2^-44: the low bits of 256 + w.
+  __device__ __forceinline__ static unsigned long long fixed(double y) {
+    return __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull;
   }
 
-  // The words of [lo, hi] counted and weighed, by bins of 1/kPerOctave power of two of weight (top = 0), or by the bits of
-  // their keys below `top`, `shift` bits to a bin; into sh.h.bin_count and bin_mass.  Weights are added relative to the
-  // bin's top, in 2^-44.  The last bin by weight, which has no lower end and may hold most of a row, is added up in
-  // registers.
-  __device__ __forceinline__ void histogram(float lo, float hi, uint32_t top, int shift) {
+  // The words of [lo, hi], of the row or of its list (listed >= 0), counted and weighed by bins of 1/kPerOctave octave of
+  // weight (TOP), or by the bits of their keys below `top`, `shift` bits to a bin; into sh.h.bin_count and bin_mass.
+  // Weights are added relative to the bin's top.  The last bin by weight, which has no lower end and may hold most of a
+  // row, is added up in registers.
+  template <bool TOP>
+  __device__ __forceinline__ void histogram(int listed, float lo, float hi, uint32_t top, int shift) {
     const int tid = threadIdx.x, copy = tid & (kCols - 1);
+    __syncthreads();
     for (int i = tid; i < kBins * kCols; i += NT) {
       sh.h.mass[i] = 0ull;
       sh.h.count[i] = 0u;
     }
     __syncthreads();
-    const double t_top = top ? t2(key_value(top)) : 0.0;
+    const double t_top = TOP ? 0.0 : t2(key_value(top));
     int rest = 0;
     double rest_mass = 0.0;
-    each_vector(
-        [&](int tile) { return rec.max[tile] >= lo; },
-        [&](const u32x4& x, int, int) {
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) {
-            const float z = elem<Tin>(x, e);
-            if (z >= lo && z <= hi) {
-              const double t = t2(z);
-              int b;
-              double rel;
-              if (top) {
-                b = min((int)((top - order_key(z)) >> shift), kBins - 1);
-                rel = t - t_top;
-              } else {
-                b = bin_of(t);
-                rel = b == kBins - 1 ? t : fma((double)b, 1.0 / kPerOctave, t);
-              }
-              const double r = exp2_neg(fmin(rel, 0.0));
-              if (!top && b == kBins - 1) {
-                ++rest;
-                rest_mass += r;
-              } else {
-                const double y = r + 256.0;  // the weight in 2^-44 in the low bits
-                atomicAdd(&sh.h.mass[b * kCols + copy], __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
-                atomicAdd(&sh.h.count[b * kCols + copy], 1u);
-              }
-            }
+    auto add = [&](float z) {
+      int b;
+      double y;
+      if constexpr (TOP) {
+        // 2^(-x / 32) for the rest x of the steps, by its interpolant of degree 5: off by 1.2e-16
+        const double q = steps(z);
+        b = (int)fmin(q, (double)(kBins - 1));
+        const double x = q - (double)b;
+        y = fma(x, -3.930921700473334e-11, 9.172082236776783e-09);
+        y = fma(x, y, -1.6938507235263203e-06);
+        y = fma(x, y, 0.00023459619814393515);
+        y = fma(x, y, -0.021660849392493294);
+        y = fma(x, y, 257.0);
+        if (b == kBins - 1) {
+          const double r = exp2_neg(x * (-1.0 / kPerOctave));
+          if (listed < 0) {
+            ++rest;
+            rest_mass += r;
+            return;
           }
-        },
-        [](int) {});
+          y = r + 256.0;
+        }
+      } else {
+        b = min((int)((top - order_key(z)) >> shift), kBins - 1);
+        y = exp2_neg(fmin(t2(z) - t_top, 0.0)) + 256.0;
+      }
+      atomicAdd(&sh.h.mass[b * kCols + copy], fixed(y));
+      atomicAdd(&sh.h.count[b * kCols + copy], 1u);
+    };
+    if (listed >= 0) {
+      for (int i = tid; i < listed; i += NT) {
+        const float z = word_of(sh.h.key[i]);
+        if (z >= lo && z <= hi) add(z);
+      }
+    } else {
+      each_vector(
+          [&](int tile) { return rec.max[tile] >= lo; },
+          [&](const u32x4& x, int, int) {
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) {
+              const float z = elem<Tin>(x, e);
+              if (z >= lo && (TOP || z <= hi)) add(z);
+            }
+          },
+          [](int) {});
+    }
     __syncthreads();
     rest = block_sum(rest);
     rest_mass = block_sum(rest_mass);
     for (int b = tid; b < kBins; b += NT) {
-      double mass = 0.0;
       int count = 0;
+      double mass = 0.0;
 #pragma unroll
       for (int i = 0; i < kCols; ++i) {
         mass += (double)sh.h.mass[b * kCols + i] * 0x1p-44;
         count += (int)sh.h.count[b * kCols + i];
       }
-      const bool last = !top && b == kBins - 1;
-      sh.h.bin_mass[b] = last ? rest_mass : mass * exp2_neg(top ? t_top : (double)b * (-1.0 / kPerOctave));
-      sh.h.bin_count[b] = last ? rest : count;
+      if (TOP && b == kBins - 1) {
+        mass += rest_mass;
+        count += rest;
+      }
+      sh.h.bin_mass[b] = mass * exp2_neg(TOP ? (double)b * (-1.0 / kPerOctave) : t_top);
+      sh.h.bin_count[b] = count;
     }
     __syncthreads();
   }
@@ -848,8 +849,9 @@ struct RowWork {
     return b;
   }
 
-  // The cut after the k-th word, or after the shortest prefix of weight `target`, among the words from x_lo up.
-  __device__ __forceinline__ Cut select(bool by_mass, int k, double target) {
+  // The cut after the k-th word, or after the shortest prefix of weight `target`, among the words from x_lo up (all in the
+  // list where listed >= 0), whose histogram<true> is made.
+  __device__ __forceinline__ Cut select(int listed, bool by_mass, int k, double target) {
     int count0 = 0, cnt;
     double mass0 = 0.0;
     const int b = find_bin(by_mass, count0, mass0, k, target, cnt);
@@ -858,7 +860,7 @@ struct RowWork {
       uint32_t lo = order_key(x_lo), hi = order_key(m);
       while (lo < hi) {
         const uint32_t step = (hi - lo) / 64 + 1, key = lo + (threadIdx.x & 63) * step;
-        const uint64_t mask = __ballot(key >= hi || bin_of(t2(key_value(key))) <= bin);
+        const uint64_t mask = __ballot(key >= hi || bin_of(key_value(key)) <= bin);
         const uint32_t l = mask ? (uint32_t)__ffsll((unsigned long long)mask) - 1 : 64;
         if (l < 64) hi = min(hi, lo + l * step);
         if (l > 0) lo = lo + (l - 1) * step + 1;
@@ -867,19 +869,20 @@ struct RowWork {
     };
     constexpr uint32_t kMinusZero = 0x7fffffffu;  // the key that no word has: -0 counts as 0
     uint32_t klo = lowest(b), khi = b == 0 ? order_key(m) : lowest(b - 1) - 1;
-    while (cnt > kCap && klo < khi) {
+    while (cnt > kSorted && klo < khi) {
       const int bits = 32 - __clz((int)(khi - klo));
       const int shift = max(0, bits - 10);  // at most kBins
-      histogram(key_value(klo), key_value(khi), khi, shift);
+      histogram<false>(listed, key_value(klo), key_value(khi), khi, shift);
       const int q = find_bin(by_mass, count0, mass0, k, target, cnt);
       khi -= (uint32_t)q << shift;
       klo = max(klo, khi - ((1u << shift) - 1));
       khi -= khi == kMinusZero;  // as a bound it would let the zeros in
     }
     Cut cut;
-    if (cnt > kCap) {  // one value, more often than the list holds
-      cut.thr = key_value(klo);
-      const double w = weight(cut.thr);
+    const float lo = key_value(klo), hi = key_value(khi);
+    if (cnt > kSorted) {  // one value
+      cut.thr = lo;
+      const double w = weight(lo);
       int r = cnt;
       if (!by_mass) r = k - count0;
       else if (w > 0.0) r = (int)fmin(ceil((target - mass0) / w), (double)cnt);
@@ -888,38 +891,68 @@ struct RowWork {
       cut.count = count0 + r;
       cut.tie = V;
       if (r < cnt) {
-        count_equal(cut.thr);
-        cut.tie = tie_index(cut.thr, r);
+        count_equal(lo);
+        cut.tie = tie_index(lo, r);
       }
       return cut;
     }
-    const int n = gather(key_value(klo), key_value(khi));
-    sort_list(n);
-    scan_list(n, mass0);
+    int n;
+    if (listed >= 0) {
+      const int tid = threadIdx.x;
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      for (int i = tid; i < listed; i += NT) {
+        const unsigned long long key = sh.h.key[i];
+        const float z = word_of(key);
+        if (z >= lo && z <= hi) sh.h.some[min(atomicAdd(&sh.n, 1), kSorted - 1)] = key;
+      }
+      __syncthreads();
+      n = min(uniform(sh.n), kSorted);
+    } else {
+      n = gather(sh.h.some, kSorted, lo, hi);
+    }
+    sort_words<false>(sh.h.some, sh.h.sorted, n);
+    scan_sorted(n, mass0);
     const int r = by_mass ? first_reaching(n, target) : max(1, min(k - count0, n));
-    cut.thr = uniform(list_value(r - 1));
-    cut.tie = uniform(list_index(r - 1));
-    cut.mass = uniform(sh.l.cum[r - 1]);
+    const unsigned long long last = sh.h.sorted[r - 1];
+    cut.thr = uniform(word_of(last));
+    cut.tie = uniform(index_of(last));
+    cut.mass = uniform(sh.h.cum[r - 1]);
     cut.count = count0 + r;
     __syncthreads();
     return cut;
   }
 
-  // rec.sum = the tiles' kept weights; their sum, and the number of kept words.
+  // rec.sum = the tiles' kept weights; their sum, and the number of kept words.  In a tile before the last kept one's all
+  // words that equal the threshold are kept, after it none; in its own they are added by their index.
   __device__ __forceinline__ double kept_sums(float thr, int tie, int& n) {
+    const int tie_tile = tie < 0 ? -1 : tie / Tile<Tin>::kWords;
+    const float above = nextafterf(thr, INFINITY);
+    const double w_thr = weight(thr);
+    const bool far = t2(thr) < -1000.0;
     int here = 0;
     double s = 0.0;
     for (int i = threadIdx.x; i < tiles; i += NT)
       if (!(rec.max[i] >= thr)) rec.sum[i] = 0.0;
     each_vector([&](int tile) { return rec.max[tile] >= thr; },
                 [&](const u32x4& x, int tile, int j) {
+                  const float least = tile < tie_tile ? thr : above;
 #pragma unroll
                   for (int e = 0; e < EPV; ++e) {
                     const float z = elem<Tin>(x, e);
-                    if (kept(z, Tile<Tin>::col(tile, j, e), thr, tie)) {
-                      s += weight(z);
+                    if (z >= least) {
+                      const double t = t2(z), w = exp2_neg<false>(far ? fmax(t, -1022.0) : t);
+                      s += far && t < -1021.0 ? 0.0 : w;
                       ++here;
                     }
+                  }
+                  if (tile == tie_tile) {
+#pragma unroll
+                    for (int e = 0; e < EPV; ++e)
+                      if (elem<Tin>(x, e) == thr && Tile<Tin>::col(tile, j, e) <= tie) {
+                        s += w_thr;
+                        ++here;
+                      }
                   }
                 },
                 [&](int tile) {
@@ -1109,23 +1142,27 @@ struct RowWork {
         rec.sum[i] = 0.0;
         rec.count[i] = 0;
       }
+    // words below the cut all read one place, the bin below it: no bank has to answer twice for them
+    const int at = thr > -kLimit ? bin_index(thr) : 1 - kMid;
+    const s16x2 floor2 = (s16x2)(short)(at - 1), at2 = (s16x2)(short)at;
     each_tile([&](int tile) { return rec.max[tile] >= thr; },
               [&](const Tile<Tin>& x, int tile) {
                 double s = 0.0;
-                int same = 0;
-                u16x2 least = (u16x2)(unsigned short)1;
+                u16x2 least = (u16x2)(unsigned short)1, other = (u16x2)(unsigned short)0;
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
                   for (int q = 0; q < 4; ++q) {
-                    const s16x2 b = value_bins(x.v[j][q], least);
+                    s16x2 b = value_bins(x.v[j][q], least);
+                    if (partial)
+                      other += __builtin_elementwise_min(__builtin_bit_cast(u16x2, b ^ at2), (u16x2)(unsigned short)1);
+                    b = __builtin_elementwise_max(b, floor2);
                     s += sh.v.weight[kMid + b.x];
                     s += sh.v.weight[kMid + b.y];
-                    if (partial)
-                      same += __popcll(__ballot(bf16_lo(x.v[j][q]) == thr)) + __popcll(__ballot(bf16_hi(x.v[j][q]) == thr));
                   }
                 if (mid_kept) each_mid(x, least, [&](float z) { s += weight(z); });
                 s = wave_sum_dpp(s);
+                const int same = __builtin_amdgcn_readlane(scan_add(EPV * NV - (int)other.x - (int)other.y), 63);
                 if (lane == 0) {
                   rec.sum[tile] = s;
                   rec.count[tile] = same;
@@ -1178,6 +1215,7 @@ struct RowWork {
     double s = 0.0;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) s += word(e);
+    if (tid == 0) sh.i0 = min(tile * Tile<Tin>::kWords, V - 1);  // a place in the row, whatever the sums
     const double incl = block_scan(s, total);
     const int first = block_min(s > 0.0 && incl > left ? tid : INT_MAX), end = block_max(s > 0.0 ? tid : -1);
     if (tid == (first != INT_MAX ? first : end)) {
@@ -1407,7 +1445,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
         }
         w.x_lo = x_lo;
         int listed = -1;
-        if (mode != kCount) listed = x_lo > kLiveMin || live <= kCap ? w.gather(x_lo, INFINITY) : live;
+        if (mode != kCount) listed = x_lo > kLiveMin || live <= kCap ? w.gather(sh.h.key, kCap, x_lo, INFINITY) : live;
         bool cut_known = false;
         if constexpr (Work::kByValue) {
           if ((mode == kCount || listed > kCap) && m < kLimit && lo > -kLimit) {
@@ -1422,59 +1460,46 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
               thr = cut.thr;
               n = cut.n;
               S = cut.S;
-              if (n - cut.r + cut.of <= kRankSort) listed = w.gather(thr, INFINITY);
+              if (n - cut.r + cut.of <= kSorted) listed = w.gather(sh.h.key, kCap, thr, INFINITY);
               else if (DRAW) tie = w.value_sums(cut);
               else tie = w.value_tie(cut);
             }
           }
         }
-        if (listed >= 0 && listed <= kCap) {
-          w.sort_list(listed);
+        if (listed > kCap) listed = -1;
+        const bool exact = mode == kSum64;  // S
+        const double p_lo = exact || k_on ? p : p * (1.0 - kSum32Error), p_hi = exact || k_on ? p : p * (1.0 + kSum32Error);
+        if (listed >= 0 && listed <= kSorted) {
+          w.template sort_words<false>(sh.h.key, sh.h.sorted, listed);
           if (!cut_known) {
-            w.scan_list(listed, 0.0);
+            w.scan_sorted(listed, 0.0);
             n = k_on ? min(k, listed) : listed;
             if (p_on) {
-              int np;
-              if (k_on || mode == kSum64) {
-                np = w.first_reaching(listed, p * (k_on ? sh.l.cum[n - 1] : S));
-              } else {
-                np = w.first_reaching(listed, p * (S * (1.0 - kSum32Error)));
-                if (np != w.first_reaching(listed, p * (S * (1.0 + kSum32Error)))) {
-                  int all;
-                  S = w.kept_sums(kLiveMin, a.V, all);
-                  np = w.first_reaching(listed, p * S);
-                }
+              if (k_on) S = uniform(sh.h.cum[n - 1]);
+              int np = w.first_reaching(listed, p_lo * S);
+              if (!(uniform(sh.h.cum[np - 1]) >= p_hi * S) && p_lo < p_hi) {
+                int all;
+                S = w.kept_sums(kLiveMin, a.V, all);
+                np = w.first_reaching(listed, p * S);
               }
               n = min(n, np);
             }
-            if (m_on) {
-              int c = 0;
-              for (int i = tid; i < listed; i += NT) c += w.list_value(i) >= z_min;
-              n = min(n, w.block_sum(c));
-            }
+            if (m_on) n = min(n, w.block_sum((int)(tid < listed && Work::word_of(sh.h.sorted[tid]) >= z_min)));
             n = max(n, 1);
-            S = uniform(sh.l.cum[n - 1]);
+            S = uniform(sh.h.cum[n - 1]);
           }
-          thr = uniform(w.list_value(n - 1));
-          tie = uniform(w.list_index(n - 1));
-          __syncthreads();
-          if (DRAW && n <= kRankSort) {
-            // the kept words in the order of their indices, smallest first: keys that fall as the index grows
-            const unsigned long long q = tid < n ? sh.l.key[tid] : 0ull;
-            __syncthreads();
-            if (tid < n) sh.l.key[tid] = (q << 32) | (q >> 32);
-            __syncthreads();
-            w.sort_list(n);
-            const double v = tid < n ? w.weight(key_value((uint32_t)sh.l.key[tid])) : 0.0;
+          const unsigned long long last_word = sh.h.sorted[n - 1];
+          thr = uniform(Work::word_of(last_word));
+          tie = uniform(Work::index_of(last_word));
+          if (DRAW) {  // the kept words in the order of their indices
+            w.template sort_words<true>(sh.h.sorted, sh.h.some, n);
+            const double v = tid < n ? w.weight(Work::word_of(sh.h.some[tid])) : 0.0;
             double all;
             const double incl = w.block_scan(v, all);
             const int at = w.block_min(v > 0.0 && incl > (double)u * S ? tid : INT_MAX);
             const int last = w.block_max(v > 0.0 ? tid : 0);
-            act = uniform((int)~(uint32_t)(sh.l.key[at == INT_MAX ? last : at] >> 32));
+            act = uniform(Work::index_of(sh.h.some[at == INT_MAX ? last : at]));
             drawn = true;
-          } else if (DRAW) {
-            int all;
-            w.kept_sums(thr, tie, all);
           }
         } else if (!cut_known) {
           thr = kLiveMin;
@@ -1486,19 +1511,26 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
             }
           };
           if (k_on || p_on) {
-            const bool sum_all = p_on && !k_on && mode != kSum64;  // S from the histogram: all live words
+            const bool sum_all = p_on && !k_on && !exact && listed < 0;  // S from the histogram: all live words
             if (sum_all) w.x_lo = x_lo = kLiveMin;
             double Sk = S;
 #pragma unroll 1
-            for (int by_mass = 0; by_mass < 2; ++by_mass) {
-              if (by_mass ? !p_on : !k_on) continue;
-              w.histogram(x_lo, INFINITY, 0u, 0);
+            for (int by_mass = !k_on, again = 0; by_mass <= (int)p_on; ++by_mass) {
+              w.template histogram<true>(listed, x_lo, INFINITY, 0u, 0);
               if (sum_all) {
                 double q = 0.0;
                 for (int i = tid; i < kBins; i += NT) q += sh.h.bin_mass[i];
                 Sk = w.block_sum(q);
               }
-              const Cut cut = w.select(by_mass, k, p * Sk);
+              const bool sure = sum_all || again;
+              const Cut cut = w.select(listed, by_mass, k, (sure ? p : p_lo) * Sk);
+              if (by_mass && !sure && p_lo < p_hi && !(cut.mass >= p_hi * Sk)) {  // S has to be exact: once more
+                int all;
+                Sk = w.kept_sums(kLiveMin, a.V, all);
+                again = 1;
+                --by_mass;
+                continue;
+              }
               narrow(cut.thr, cut.tie);
               Sk = S = cut.mass;
               n = cut.count;
