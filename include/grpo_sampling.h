@@ -57,7 +57,8 @@ typedef struct {
   float logp;        /* the action's log-prob                                        */
 } grpo_sampling_row;
 
-/* Bytes of device workspace grpo_sample and grpo_sampled_logp need; 0 for invalid sizes. */
+/* Bytes of device workspace grpo_sample and grpo_sampled_logp need: 0 from 192 rows on or up to 16,384 words (ws may then
+ * be NULL), and for invalid sizes. */
 size_t grpo_sampling_workspace_bytes(int64_t T, int64_t V);
 
 /*

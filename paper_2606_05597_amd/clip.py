@@ -5,9 +5,9 @@ import ctypes
 
 import torch
 
-from . import _check, _lib, _placed, _ptr
+from . import _check, _lib, _meta, _placed
 from ._lib import GRPO_BF16, GRPO_F32, GRPO_GRAD_PARTIALS
-from .sampling import _on
+from .sampling import _at, _on
 
 _CODES = {torch.float32: GRPO_F32, torch.bfloat16: GRPO_BF16}
 
@@ -53,9 +53,10 @@ class GradList:
         size = int(lib.grpo_grad_table_bytes(n))
         table = torch.zeros(max(size, 8), dtype=torch.uint8)
         self._layout = _lib.GradLayout()
-        _check(lib.grpo_grad_table(recs, n, _ptr(table), size, ctypes.byref(self._layout)), "grpo_grad_table")
+        _check(lib.grpo_grad_table(recs, n, table.data_ptr(), size, ctypes.byref(self._layout)), "grpo_grad_table")
         self._places = [s.data_ptr() for s in self._storages]
         self._table = table.to(self.device)
+        self._c_args = ctypes.byref(self._layout), self._table.data_ptr()
 
     def __len__(self):
         return int(self._layout.n)
@@ -63,7 +64,7 @@ class GradList:
     def _args(self):
         if [s.data_ptr() for s in self._storages] != self._places:
             raise ValueError("the memory of a tensor in the list has moved since the list was made")
-        return ctypes.byref(self._layout), _ptr(self._table)
+        return self._c_args
 
 
 def _grad_list(grads, out=None):
@@ -83,18 +84,33 @@ def _partials(partials, device):
     _placed(device, partials=partials)
 
 
+def _flags(error_flags, device):
+    _meta(error_flags, "error_flags", torch.int32, n=1, optional=True)
+    _placed(device, error_flags=error_flags)
+
+
+def _sumsq(grads, partials, s):
+    if partials is None:
+        partials = torch.empty(GRPO_GRAD_PARTIALS, dtype=torch.float64, device=grads.device)
+    _check(_lib.load().grpo_grad_sumsq(*grads._args(), partials.data_ptr(), s), "grpo_grad_sumsq")
+    return partials
+
+
+def _clip(grads, partials, max_norm, error_flags, s):
+    norm = torch.empty((), dtype=torch.float32, device=grads.device)
+    st = _lib.load().grpo_grad_clip(*grads._args(), partials.data_ptr(), float(max_norm), norm.data_ptr(),
+                                    _at(error_flags), s)
+    _check(st, "grpo_grad_clip")
+    return norm
+
+
 def grpo_grad_sumsq(grads, *, partials: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The sum of squares of all gradients (a GradList, or tensors) as fp64 [GRPO_GRAD_PARTIALS] slots that add up to it;
     devices that hold different gradients of one model add their slots before each clips its own."""
     grads = _grad_list(grads)
     if partials is not None:
         _partials(partials, grads.device)
-    with _on(grads.device, stream) as s:
-        if partials is None:
-            partials = torch.empty(GRPO_GRAD_PARTIALS, dtype=torch.float64, device=grads.device)
-        st = _lib.load().grpo_grad_sumsq(*grads._args(), _ptr(partials), s)
-    _check(st, "grpo_grad_sumsq")
-    return partials
+    return _on(grads.device, stream, lambda s: _sumsq(grads, partials, s))
 
 
 def grpo_grad_clip(grads, partials: torch.Tensor, max_norm: float, *, out=None,
@@ -104,16 +120,8 @@ def grpo_grad_clip(grads, partials: torch.Tensor, max_norm: float, *, out=None,
     GRPO_FLAG_NONFINITE).  Returns the norm, a 0-dim fp32 tensor."""
     grads = _grad_list(grads, out)
     _partials(partials, grads.device)
-    if error_flags is not None:
-        if error_flags.dtype != torch.int32 or error_flags.numel() < 1:
-            raise TypeError("error_flags must be an int32 tensor of at least 1 element")
-        _placed(grads.device, error_flags=error_flags)
-    with _on(grads.device, stream) as s:
-        norm = torch.empty((), dtype=torch.float32, device=grads.device)
-        st = _lib.load().grpo_grad_clip(*grads._args(), _ptr(partials), float(max_norm), _ptr(norm),
-                                        _ptr(error_flags), s)
-    _check(st, "grpo_grad_clip")
-    return norm
+    _flags(error_flags, grads.device)
+    return _on(grads.device, stream, lambda s: _clip(grads, partials, max_norm, error_flags, s))
 
 
 def grpo_clip_grad_norm_(grads, max_norm: float, *, out=None, error_flags: torch.Tensor | None = None,
@@ -121,5 +129,5 @@ def grpo_clip_grad_norm_(grads, max_norm: float, *, out=None, error_flags: torch
     """The gradients' common norm, and the gradients clipped to ``max_norm``: ``grpo_grad_sumsq``, then
     ``grpo_grad_clip``.  Returns the norm, a 0-dim fp32 tensor; nothing waits for the device."""
     grads = _grad_list(grads, out)
-    return grpo_grad_clip(grads, grpo_grad_sumsq(grads, stream=stream), max_norm, error_flags=error_flags,
-                          stream=stream)
+    _flags(error_flags, grads.device)
+    return _on(grads.device, stream, lambda s: _clip(grads, _sumsq(grads, None, s), max_norm, error_flags, s))

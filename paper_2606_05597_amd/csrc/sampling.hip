@@ -1664,7 +1664,7 @@ __global__ void k_clear_sampling_flag(int32_t* f) { *f = 0; }
 // ---- host -----------------------------------------------------------------------
 
 // Whether the tiles are reduced by a launch of their own.
-static bool split_rows(int64_t T, int64_t V) { return T < 192 && V > 16384; }
+static bool split_rows(int64_t T, int64_t V) { return T > 0 && T < 192 && V > 16384; }
 
 static int tile_count(int64_t V, bool bf16) {
   const int words = bf16 ? Tile<uint16_t>::kWords : Tile<float>::kWords;
@@ -1720,7 +1720,7 @@ static int sample_call(const void* logits, int32_t dtype, int64_t T, int64_t V, 
   if (!aligned(logits, dtype == GRPO_BF16 ? 2 : 4) || !aligned(u, 4) || !aligned(actions, 4) || !aligned(actions_out, 4) ||
       !aligned(logp, 4) || !aligned(n_kept, 4) || !aligned(rows, 8) || !aligned(flags, 4))
     return GRPO_ERR_ALIGN;
-  if (T > 0 && split_rows(T, V)) {
+  if (split_rows(T, V)) {
     if (!ws || ws_bytes < grpo_sampling_workspace_bytes(T, V)) return GRPO_ERR_WORKSPACE;
     if (!aligned(ws, 16)) return GRPO_ERR_ALIGN;
   }
@@ -1740,8 +1740,7 @@ using namespace grpo;
 
 extern "C" size_t grpo_sampling_workspace_bytes(int64_t T, int64_t V) {
   if (bad_shape(T, V, V)) return 0;
-  const size_t recs = split_rows(T, V) ? sizeof(TileRec) * (size_t)T * (size_t)tile_count(V, false) : 0;
-  return align_up(std::max(recs, (size_t)1));
+  return split_rows(T, V) ? align_up(sizeof(TileRec) * (size_t)T * (size_t)tile_count(V, false)) : 0;
 }
 
 extern "C" int grpo_sample(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,

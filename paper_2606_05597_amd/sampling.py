@@ -6,50 +6,52 @@ Each setting is a number for all rows or a GPU tensor [T] with one value per row
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
 
-from . import _check, _dlogits_arg, _lib, _logits2d, _meta, _nbytes, _placed, _ptr, _workspace
+from . import _check, _dlogits_arg, _lib, _logits2d, _meta, _nbytes, _placed, _workspace
 from ._lib import GRPO_SAMPLING_MAX_V
 
 SAMPLING_ROW_BYTES = 32  # one grpo_sampling_row
 
-_SETTINGS = (("temperature", torch.float32, 1.0), ("top_k", torch.int32, 0), ("top_p", torch.float32, 1.0),
-             ("min_p", torch.float32, 0.0))
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
-@contextlib.contextmanager
-def _on(device, stream):
-    """The tensors' device made current and the call's raw stream on it: the caller's, or that device's current one.
-    Memory allocated inside belongs to that stream."""
-    if stream is not None and stream.device != device:
-        raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            yield ctypes.c_void_p(stream.cuda_stream)
-    elif torch._C._cuda_getDevice() == device.index:
-        yield ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(device.index))
-    else:
+def _on(device, stream, call):
+    """call(the raw stream) with the tensors' device current: the caller's stream, or that device's current one.  Memory
+    allocated in `call` belongs to that stream."""
+    if stream is None:
+        if torch._C._cuda_getDevice() == device.index:
+            return call(torch._C._cuda_getCurrentRawStream(device.index))
         with torch.cuda.device(device):
-            yield ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(device.index))
+            return call(torch._C._cuda_getCurrentRawStream(device.index))
+    if stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
+    with torch.cuda.stream(stream):
+        return call(stream.cuda_stream)
 
 
-def _sampling(T, given):
+def _setting(v, name, dtype, T, tensors):
+    """A setting's pointer (None where it is a number)."""
+    if isinstance(v, torch.Tensor):
+        _meta(v, name, dtype, shape=(T,))
+        tensors[name] = v
+        return v.data_ptr()
+    return None
+
+
+def _sampling(T, temperature, top_k, top_p, min_p):
     """The settings as a grpo_sampling struct, and the tensors among them by name."""
-    par, tensors = _lib.Sampling(), {}
-    for name, dtype, off in _SETTINGS:
-        v = given[name]
-        if isinstance(v, torch.Tensor):
-            _meta(v, name, dtype, shape=(T,))
-            tensors[name] = v
-            setattr(par, name, v.data_ptr())
-        else:
-            v = off if v is None else v
-            if name == "top_k":
-                v = max(min(int(v), 2**31 - 1), 0)
-            setattr(par, name + "_all", v)
+    tensors = {}
+    f32 = torch.float32
+    at = (_setting(temperature, "temperature", f32, T, tensors), _setting(top_k, "top_k", torch.int32, T, tensors),
+          _setting(top_p, "top_p", f32, T, tensors), _setting(min_p, "min_p", f32, T, tensors))
+    par = _lib.Sampling(*at, 1.0 if temperature is None or at[0] else temperature,
+                        0 if top_k is None or at[1] else max(min(int(top_k), 2**31 - 1), 0),
+                        1.0 if top_p is None or at[2] else top_p, 0.0 if min_p is None or at[3] else min_p)
     return par, tensors
 
 
@@ -57,6 +59,16 @@ def _columns(logits, V):
     dt, T, ld = _logits2d(logits)
     V = logits.shape[1] if V is None else int(V)
     return dt, T, V, ld
+
+
+def _scratch(workspace, T, V, device):
+    """The caller's workspace, or a new one where the call needs one."""
+    if workspace is None:
+        need = _lib.load().grpo_sampling_workspace_bytes(T, V)
+        if need == 0:
+            return None, 0
+    workspace = _workspace(workspace, 0 if workspace is not None else need, device)
+    return workspace, _nbytes(workspace)
 
 
 def grpo_sample(logits: torch.Tensor, u: torch.Tensor, *, temperature=None, top_k=None, top_p=None, min_p=None,
@@ -68,19 +80,23 @@ def grpo_sample(logits: torch.Tensor, u: torch.Tensor, *, temperature=None, top_
     distribution (a NaN, +inf, nothing above -1e8, a setting out of range) gets action -1 and n_kept 0."""
     dt, T, V, ld = _columns(logits, V)
     _meta(u, "u", torch.float32, shape=(T,))
-    par, tensors = _sampling(T, dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p))
+    par, tensors = _sampling(T, temperature, top_k, top_p, min_p)
     _meta(error_flags, "error_flags", torch.int32, n=1, optional=True)
     dev = logits.device
     _placed(dev, strided=("logits",), logits=logits, u=u, error_flags=error_flags, **tensors)
-    lib = _lib.load()
-    with _on(dev, stream) as s:
-        workspace = _workspace(workspace, lib.grpo_sampling_workspace_bytes(T, V), dev)
-        out = torch.empty((3, T), dtype=torch.int32, device=dev)
-        actions, logp, n_kept = out[0], out[1].view(torch.float32), out[2]
-        st = lib.grpo_sample(_ptr(logits), dt, T, V, ld, ctypes.byref(par), _ptr(u), _ptr(actions), _ptr(logp),
-                             _ptr(n_kept), _ptr(error_flags), _ptr(workspace), _nbytes(workspace), s)
-    _check(st, "grpo_sample")
-    return actions, logp, n_kept
+
+    def call(s):
+        ws, ws_bytes = _scratch(workspace, T, V, dev)
+        actions = torch.empty(T, dtype=torch.int32, device=dev)
+        logp = torch.empty(T, dtype=torch.float32, device=dev)
+        n_kept = torch.empty(T, dtype=torch.int32, device=dev)
+        st = _lib.load().grpo_sample(logits.data_ptr(), dt, T, V, ld, ctypes.byref(par), u.data_ptr(),
+                                     actions.data_ptr(), logp.data_ptr(), n_kept.data_ptr(), _at(error_flags), _at(ws),
+                                     ws_bytes, s)
+        _check(st, "grpo_sample")
+        return actions, logp, n_kept
+
+    return _on(dev, stream, call)
 
 
 def grpo_sampled_logp(logits: torch.Tensor, actions: torch.Tensor, *, temperature=None, top_k=None, top_p=None,
@@ -90,20 +106,23 @@ def grpo_sampled_logp(logits: torch.Tensor, actions: torch.Tensor, *, temperatur
     action is not kept; n_kept int32 [T]; rows uint8 [T, 32], what ``grpo_sampled_logp_bwd`` takes)."""
     dt, T, V, ld = _columns(logits, V)
     _meta(actions, "actions", torch.int32, shape=(T,))
-    par, tensors = _sampling(T, dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p))
+    par, tensors = _sampling(T, temperature, top_k, top_p, min_p)
     _meta(error_flags, "error_flags", torch.int32, n=1, optional=True)
     dev = logits.device
     _placed(dev, strided=("logits",), logits=logits, actions=actions, error_flags=error_flags, **tensors)
-    lib = _lib.load()
-    with _on(dev, stream) as s:
-        workspace = _workspace(workspace, lib.grpo_sampling_workspace_bytes(T, V), dev)
+
+    def call(s):
+        ws, ws_bytes = _scratch(workspace, T, V, dev)
         logp = torch.empty(T, dtype=torch.float32, device=dev)
         n_kept = torch.empty(T, dtype=torch.int32, device=dev)
         rows = torch.empty((T, SAMPLING_ROW_BYTES), dtype=torch.uint8, device=dev)
-        st = lib.grpo_sampled_logp(_ptr(logits), dt, T, V, ld, ctypes.byref(par), _ptr(actions), _ptr(logp),
-                                   _ptr(n_kept), _ptr(rows), _ptr(error_flags), _ptr(workspace), _nbytes(workspace), s)
-    _check(st, "grpo_sampled_logp")
-    return logp, n_kept, rows
+        st = _lib.load().grpo_sampled_logp(logits.data_ptr(), dt, T, V, ld, ctypes.byref(par), actions.data_ptr(),
+                                           logp.data_ptr(), n_kept.data_ptr(), rows.data_ptr(), _at(error_flags),
+                                           _at(ws), ws_bytes, s)
+        _check(st, "grpo_sampled_logp")
+        return logp, n_kept, rows
+
+    return _on(dev, stream, call)
 
 
 def grpo_sampled_logp_bwd(logits: torch.Tensor, actions: torch.Tensor, rows: torch.Tensor, dlogp: torch.Tensor, *,
@@ -117,13 +136,17 @@ def grpo_sampled_logp_bwd(logits: torch.Tensor, actions: torch.Tensor, rows: tor
     _meta(dlogp, "dlogp", torch.float32, shape=(T,))
     if dlogits is None or dlogits is False:
         raise ValueError("dlogits must be True or a tensor")
-    dlogits = _dlogits_arg(dlogits, logits) if dlogits is not True else True
+    if dlogits is not True:
+        _dlogits_arg(dlogits, logits)
     dev = logits.device
     _placed(dev, strided=("logits", "dlogits"), logits=logits, dlogits=None if dlogits is True else dlogits,
             actions=actions, rows=rows, dlogp=dlogp)
-    with _on(dev, stream) as s:
-        dlogits = _dlogits_arg(dlogits, logits)
-        st = _lib.load().grpo_sampled_logp_bwd(_ptr(logits), dt, T, V, ld, _ptr(actions), _ptr(rows), _ptr(dlogp),
-                                               _ptr(dlogits), s)
-    _check(st, "grpo_sampled_logp_bwd")
-    return dlogits
+
+    def call(s):
+        out = _dlogits_arg(dlogits, logits)
+        st = _lib.load().grpo_sampled_logp_bwd(logits.data_ptr(), dt, T, V, ld, actions.data_ptr(), rows.data_ptr(),
+                                               dlogp.data_ptr(), out.data_ptr(), s)
+        _check(st, "grpo_sampled_logp_bwd")
+        return out
+
+    return _on(dev, stream, call)
