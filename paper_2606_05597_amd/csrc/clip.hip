@@ -47,17 +47,20 @@ typedef GRPO_GLOBAL float* gf32o;
 typedef GRPO_GLOBAL uint16_t* gbf16o;
 
 // Eight elements at any element-aligned address, as fp32.
+template <bool STREAM>
 __device__ __forceinline__ void load8(gf32 p, float (&x)[8]) {
-  const u32x4 a = __builtin_nontemporal_load((const GRPO_GLOBAL u32x4_a4*)p);
-  const u32x4 b = __builtin_nontemporal_load((const GRPO_GLOBAL u32x4_a4*)(p + 4));
+  const GRPO_GLOBAL u32x4_a4* q = (const GRPO_GLOBAL u32x4_a4*)p;
+  const u32x4 a = STREAM ? __builtin_nontemporal_load(q) : q[0], b = STREAM ? __builtin_nontemporal_load(q + 1) : q[1];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[e] = __uint_as_float(a[e]);
     x[4 + e] = __uint_as_float(b[e]);
   }
 }
+template <bool STREAM>
 __device__ __forceinline__ void load8(gbf16 p, float (&x)[8]) {
-  const u32x4 a = __builtin_nontemporal_load((const GRPO_GLOBAL u32x4_a2*)p);
+  const GRPO_GLOBAL u32x4_a2* q = (const GRPO_GLOBAL u32x4_a2*)p;
+  const u32x4 a = STREAM ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[2 * e] = bf16_lo(a[e]);
@@ -88,32 +91,31 @@ __device__ __forceinline__ float load1(gbf16 p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ void store1(gf32o p, float v) { *p = v; }
 __device__ __forceinline__ void store1(gbf16o p, float v) { *p = (uint16_t)(pack_bf16(v, 0.f) & 0xffffu); }
 
+constexpr int kVecs = kUnit / kClipNT / 8;  // of 8 elements, to a thread
+
 // Sums one unit's squares: fp32 squares can pass fp32's range at both ends, fp64 ones cannot.
 template <typename P>
 __device__ __forceinline__ double unit_sumsq(P p, int n) {
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, nv = n / 8;
+  float x[kVecs][8];
   double s = 0.0;
   if (n == kUnit) {
-    float x[kUnit / kClipNT / 8][8];
 #pragma unroll
-    for (int q = 0; q < kUnit / kClipNT / 8; ++q) load8(p + (q * kClipNT + tid) * 8, x[q]);
-#pragma unroll
-    for (int q = 0; q < kUnit / kClipNT / 8; ++q)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fma((double)x[q][e], (double)x[q][e], s);
+    for (int q = 0; q < kVecs; ++q) load8<false>(p + (q * kClipNT + tid) * 8, x[q]);
   } else {
-    const int nv = n / 8;
-    for (int v = tid; v < nv; v += kClipNT) {
-      float x[8];
-      load8(p + v * 8, x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fma((double)x[e], (double)x[e], s);
+    for (int q = 0; q < kVecs; ++q) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[q][e] = 0.f;
+      if (q * kClipNT + tid < nv) load8<false>(p + (q * kClipNT + tid) * 8, x[q]);
     }
-    if (tid < n - nv * 8) {
-      const double x = (double)load1(p + nv * 8 + tid);
-      s = fma(x, x, s);
-    }
+    const float edge = tid < n - nv * 8 ? load1(p + nv * 8 + tid) : 0.f;
+    s = (double)edge * (double)edge;
   }
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fma((double)x[q][e], (double)x[q][e], s);
   return s;
 }
 
@@ -139,32 +141,38 @@ __global__ __launch_bounds__(kClipNT) void k_grad_sumsq(const GradEntry* __restr
     partials[i] = 0.0;
 }
 
-template <typename Pi, typename Po>
+template <bool STREAM, typename Pi, typename Po>
 __device__ __forceinline__ void unit_scale(Pi p, Po o, int n, float f) {
-  const int tid = threadIdx.x;
-  const int nv = n / 8;
+  const int tid = threadIdx.x, nv = n / 8;
+  float x[kVecs][8];
   if (n == kUnit) {
-    float x[kUnit / kClipNT / 8][8];
 #pragma unroll
-    for (int q = 0; q < kUnit / kClipNT / 8; ++q) load8(p + (q * kClipNT + tid) * 8, x[q]);
+    for (int q = 0; q < kVecs; ++q) load8<STREAM>(p + (q * kClipNT + tid) * 8, x[q]);
 #pragma unroll
-    for (int q = 0; q < kUnit / kClipNT / 8; ++q) {
+    for (int q = 0; q < kVecs; ++q) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[q][e] *= f;
       store8(o + (q * kClipNT + tid) * 8, x[q]);
     }
     return;
   }
-  for (int v = tid; v < nv; v += kClipNT) {
-    float x[8];
-    load8(p + v * 8, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= f;
-    store8(o + v * 8, x);
-  }
-  if (tid < n - nv * 8) store1(o + nv * 8 + tid, load1(p + nv * 8 + tid) * f);
+  for (int q = 0; q < kVecs; ++q)
+    if (q * kClipNT + tid < nv) load8<STREAM>(p + (q * kClipNT + tid) * 8, x[q]);
+  const float edge = tid < n - nv * 8 ? load1(p + nv * 8 + tid) : 0.f;
+#pragma unroll
+  for (int q = 0; q < kVecs; ++q)
+    if (q * kClipNT + tid < nv) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[q][e] *= f;
+      store8(o + (q * kClipNT + tid) * 8, x[q]);
+    }
+  if (tid < n - nv * 8) store1(o + nv * 8 + tid, edge * f);
 }
 
+// BIG: more gradients than the memory-side cache holds.  They are then taken from the last unit back, so that what the
+// sum of squares read last is still there, and past the caches otherwise; fewer are read from that cache as they lie.
+template <bool BIG>
 __global__ __launch_bounds__(kClipNT) void k_grad_clip(const GradEntry* __restrict__ tab, int n_tab, int64_t units,
                                                        bool in_place, const double* __restrict__ partials,
                                                        double max_norm, float* __restrict__ norm_out,
@@ -185,24 +193,24 @@ __global__ __launch_bounds__(kClipNT) void k_grad_clip(const GradEntry* __restri
     if (flags) *flags = finite ? 0 : GRPO_FLAG_NONFINITE;
   }
   if (in_place && f == 1.f) return;
-  int at = 0;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    at = entry_of(tab, at, n_tab, u);
-    const GradEntry e = tab[at];
+  for (int64_t v = blockIdx.x; v < units; v += gridDim.x) {
+    const int64_t u = BIG ? units - 1 - v : v;
+    const GradEntry e = tab[entry_of(tab, 0, n_tab, u)];
     const int64_t first = (u - e.unit0) * kUnit;
     const int n = (int)min((int64_t)kUnit, e.n - first);
     if (e.data == e.out && f == 1.f) continue;
     if (e.dtype == GRPO_F32) {
-      if (e.out_dtype == GRPO_F32) unit_scale((gf32)e.data + first, (gf32o)e.out + first, n, f);
-      else unit_scale((gf32)e.data + first, (gbf16o)e.out + first, n, f);
+      if (e.out_dtype == GRPO_F32) unit_scale<BIG>((gf32)e.data + first, (gf32o)e.out + first, n, f);
+      else unit_scale<BIG>((gf32)e.data + first, (gbf16o)e.out + first, n, f);
     } else {
-      if (e.out_dtype == GRPO_F32) unit_scale((gbf16)e.data + first, (gf32o)e.out + first, n, f);
-      else unit_scale((gbf16)e.data + first, (gbf16o)e.out + first, n, f);
+      if (e.out_dtype == GRPO_F32) unit_scale<BIG>((gbf16)e.data + first, (gf32o)e.out + first, n, f);
+      else unit_scale<BIG>((gbf16)e.data + first, (gbf16o)e.out + first, n, f);
     }
   }
 }
 
 constexpr int64_t kMaxGrads = 1 << 20;
+constexpr int64_t kCacheBytes = 256 << 20;  // the memory-side cache
 
 static unsigned clip_grid(int64_t units) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(units, GRPO_GRAD_PARTIALS)); }
 
@@ -295,8 +303,8 @@ extern "C" int grpo_grad_clip(const grpo_grad_layout* layout, const void* table,
   if (st != GRPO_OK) return st;
   if (!(max_norm >= 0.0)) return GRPO_ERR_ARG;
   if (!aligned(norm_out, 4) || !aligned(error_flags, 4)) return GRPO_ERR_ALIGN;
-  hipLaunchKernelGGL(k_grad_clip, dim3(clip_grid(layout->units)), dim3(kClipNT), 0, s,
-                     static_cast<const GradEntry*>(table), layout->n, layout->units, layout->in_place != 0, partials,
-                     max_norm, norm_out, error_flags);
+  const auto kernel = layout->units * kUnit * 4 > kCacheBytes ? k_grad_clip<true> : k_grad_clip<false>;
+  hipLaunchKernelGGL(kernel, dim3(clip_grid(layout->units)), dim3(kClipNT), 0, s, static_cast<const GradEntry*>(table),
+                     layout->n, layout->units, layout->in_place != 0, partials, max_norm, norm_out, error_flags);
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
 }
