@@ -563,38 +563,49 @@ struct RowWork {
       __syncthreads();
       blocks = uniform(sh.bin);
     }
-    for (int g0 = 0; g0 < blocks; g0 += NT / kSubs) {
+    // this thread's block of round g0: its tile and the lane whose words it reads, or -1
+    auto block_at = [&](int g0) {
       const int g = g0 + tid / kSubs;
-      const int block = g < blocks ? (fine ? sh.block[g] : g) : -1;
-      const int tile = block >= 0 ? block / kSubs : 0, own = (block & (kSubs - 1)) * 8 + (tid & 7);
+      if (g >= blocks) return -1;
+      const int b = fine ? sh.block[g] : g;
+      return rec.max[b / kSubs] >= lo ? b : -1;
+    };
+    auto lane_of = [&](int b) { return (b & (kSubs - 1)) * 8 + (tid & 7); };
+    Tile<Tin> x, y;
+    int block = block_at(0);
+    if (__any(block >= 0)) x.load(row, V, max(block, 0) / kSubs, lane_of(block));
+    for (int g0 = 0; g0 < blocks; g0 += NT / kSubs) {
       if (uniform(*(volatile int*)&sh.n) > room) break;
-      const bool some = block >= 0 && rec.max[tile] >= lo;
-      if (!__any(some)) continue;
-      Tile<Tin> x;
-      x.load(row, V, tile, own);
+      const int next = block_at(g0 + NT / kSubs);
+      if (__any(next >= 0)) y.load(row, V, max(next, 0) / kSubs, lane_of(next));
       int mine = 0;
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) mine += x.at(j, e) >= lo && x.at(j, e) <= hi;
-      mine = some ? mine : 0;
-      const int incl = scan_add(mine), all = __builtin_amdgcn_readlane(incl, 63);
-      if (all == 0) continue;
-      int at = 0;
-      if (lane == 0) at = atomicAdd(&sh.n, all);
-      at = uniform(at);
-      if (at + all > room) break;
-      at += incl - mine;
-      if (mine > 0) {
+      if (block >= 0) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-          for (int e = 0; e < EPV; ++e) {
-            const float z = x.at(j, e);
-            if (z >= lo && z <= hi)
-              list[at++] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e, own);
-          }
+          for (int e = 0; e < EPV; ++e) mine += x.at(j, e) >= lo && x.at(j, e) <= hi;
       }
+      const int incl = scan_add(mine), all = __builtin_amdgcn_readlane(incl, 63);
+      if (all > 0) {
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&sh.n, all);
+        at = uniform(at);
+        if (at + all > room) break;
+        at += incl - mine;
+        if (mine > 0) {
+          const int tile = block / kSubs, own = lane_of(block);
+#pragma unroll
+          for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) {
+              const float z = x.at(j, e);
+              if (z >= lo && z <= hi)
+                list[at++] = ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e, own);
+            }
+        }
+      }
+      x = y;
+      block = next;
     }
     __syncthreads();
     return uniform(sh.n);
@@ -1192,7 +1203,6 @@ struct RowWork {
       const double v = i < tiles ? rec.sum[i] : 0.0;
       const double incl = block_scan(v, total);
       const int at = block_min(v > 0.0 && incl > left ? i : INT_MAX);
-      last = max(last, block_max(v > 0.0 ? i : -1));
       if (at != INT_MAX) {
         if (i == at) sh.d0 = left - (incl - v);
         __syncthreads();
@@ -1200,6 +1210,7 @@ struct RowWork {
         tile = at;
       } else {
         left -= total;
+        last = max(last, block_max(v > 0.0 ? i : -1));
       }
     }
     if (tile < 0) {
@@ -1217,8 +1228,9 @@ struct RowWork {
     for (int e = 0; e < kEach; ++e) s += word(e);
     if (tid == 0) sh.i0 = min(tile * Tile<Tin>::kWords, V - 1);  // a place in the row, whatever the sums
     const double incl = block_scan(s, total);
-    const int first = block_min(s > 0.0 && incl > left ? tid : INT_MAX), end = block_max(s > 0.0 ? tid : -1);
-    if (tid == (first != INT_MAX ? first : end)) {
+    int at = block_min(s > 0.0 && incl > left ? tid : INT_MAX);
+    if (at == INT_MAX) at = block_max(s > 0.0 ? tid : -1);
+    if (tid == at) {
       double run = incl - s;
       int col = col0;
       bool over = false;
@@ -1285,6 +1297,18 @@ struct RowWork {
     return z;
   }
 };
+
+// A row's outputs; an action outside the vocabulary has log-prob 0.
+__device__ __forceinline__ void write_row(const RowArgs& a, int t, grpo_sampling_row out, bool act_ok, int flag) {
+  if (!act_ok) {
+    out.logp = 0.f;
+    flag |= GRPO_FLAG_ACTION;
+  }
+  if (a.logp) a.logp[t] = out.logp;
+  if (a.n_kept) a.n_kept[t] = out.n_kept;
+  if (a.rows) a.rows[t] = out;
+  if (a.flags && flag) atomicOr(a.flags, flag);
+}
 
 template <typename Tin, bool FUSED, bool DRAW, int NT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_sample_row(const RowArgs a, int row0) {
@@ -1496,9 +1520,9 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
             const double v = tid < n ? w.weight(Work::word_of(sh.h.some[tid])) : 0.0;
             double all;
             const double incl = w.block_scan(v, all);
-            const int at = w.block_min(v > 0.0 && incl > (double)u * S ? tid : INT_MAX);
-            const int last = w.block_max(v > 0.0 ? tid : 0);
-            act = uniform(Work::index_of(sh.h.some[at == INT_MAX ? last : at]));
+            int at = w.block_min(v > 0.0 && incl > (double)u * S ? tid : INT_MAX);
+            if (at == INT_MAX) at = w.block_max(v > 0.0 ? tid : 0);
+            act = uniform(Work::index_of(sh.h.some[at]));
             drawn = true;
           }
         } else if (!cut_known) {
@@ -1555,16 +1579,112 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
     }
   }
   if (tid == 0) {
-    if (!act_ok) {
-      out.logp = 0.f;
-      flag |= GRPO_FLAG_ACTION;
-    }
     if (DRAW) a.actions_out[t] = out.n_kept > 0 ? act : -1;
-    if (a.logp) a.logp[t] = out.logp;
-    if (a.n_kept) a.n_kept[t] = out.n_kept;
-    if (a.rows) a.rows[t] = out;
-    if (a.flags && flag) atomicOr(a.flags, flag);
+    write_row(a, t, out, act_ok, flag);
   }
+}
+
+// ---- log-probs of rows with nothing cut -------------------------------------------
+// One workgroup to a row, read once: a thread's 32 (bf16) or 16 weights at a time summed in fp32, relative to its running
+// maximum, and these sums in fp64.  HBM-bound.
+template <typename Tin>
+__global__ __launch_bounds__(256) void k_tempered_logp(const RowArgs a, int row0) {
+  constexpr int NT = 256, NW = NT / 64, EPV = 16 / (int)sizeof(Tin), U = 4;
+  typedef typename VecAt<Tin>::type u32x4_any;
+  __shared__ float sh_m[NW];
+  __shared__ double sh_s[NW];
+  __shared__ int sh_n[NW], sh_bad[NW];
+  const int t = row0 + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const Tin* row = static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld;
+  const int act = a.actions[t], nvec = a.V / EPV;
+  const bool act_ok = act >= 0 && act < a.V;
+  const float act_z = act_ok ? load_elem(row + act) : 0.f;
+  const float tau = a.par.temperature_all;
+  const double c = kLog2e64 / (double)tau;
+  const float c32 = (float)c;
+  float m = kLiveMin;
+  double s = 0.0;
+  int dead = 0;
+  bool nan = false;
+  auto raise = [&](float z) {  // the running maximum
+    s *= exp2_neg(((double)m - (double)z) * c);
+    m = z;
+  };
+  auto one = [&](float z) {  // a word by itself
+    nan |= z != z;
+    if (!(z >= kLiveMin)) {
+      ++dead;
+      return;
+    }
+    if (z > m) raise(z);
+    s += (double)__builtin_amdgcn_exp2f((z - m) * c32);
+  };
+  for (int base = tid; base < nvec; base += NT * U) {
+    u32x4 x[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int v = min(base + i * NT, nvec - 1);
+      x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + (int64_t)v * EPV));
+    }
+    float hi = -INFINITY, lo = INFINITY;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < EPV; e += 2) {
+        const float p = elem<Tin>(x[i], e), q = elem<Tin>(x[i], e + 1);
+        nan |= __builtin_isunordered(p, q);
+        hi = max3f(hi, p, q);
+        lo = min3f(lo, p, q);
+      }
+    const bool whole = base + (U - 1) * NT < nvec;
+    if (__all(whole && lo >= kLiveMin)) {
+      if (hi > m) raise(hi);
+      float some = 0.f;
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) some += __builtin_amdgcn_exp2f((elem<Tin>(x[i], e) - m) * c32);
+      s += (double)some;
+    } else {
+      for (int v = base; v < min(base + U * NT, nvec); v += NT)
+        for (int e = 0; e < EPV; ++e) one(load_elem(row + (int64_t)v * EPV + e));
+    }
+  }
+  if (tid < a.V - nvec * EPV) one(load_elem(row + nvec * EPV + tid));
+  const float mw = wave_max_dpp(m);
+  const double sw = wave_sum_dpp(s * exp2_neg(((double)m - (double)mw) * c));
+  dead = __builtin_amdgcn_readlane(scan_add(dead), 63);
+  const bool bad = __any(nan) || mw == INFINITY;
+  if (lane == 0) {
+    sh_m[wv] = mw;
+    sh_s[wv] = sw;
+    sh_n[wv] = dead;
+    sh_bad[wv] = bad;
+  }
+  __syncthreads();
+  if (tid != 0) return;
+  float M = sh_m[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) M = fmaxf(M, sh_m[i]);
+  double S = 0.0;
+  int n = a.V, any_bad = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    S += sh_s[i] * exp2_neg(((double)sh_m[i] - (double)M) * c);
+    n -= sh_n[i];
+    any_bad |= sh_bad[i];
+  }
+  grpo_sampling_row out;
+  out.max = M;
+  out.temperature = tau;
+  out.threshold = n > 0 && !any_bad ? -1e8f : INFINITY;
+  out.tie = -1;
+  out.n_kept = any_bad ? 0 : n;
+  out.sum = any_bad ? (double)NAN : n > 0 ? S : 0.0;
+  out.logp = any_bad ? NAN : -INFINITY;
+  if (n > 0 && !any_bad && act_ok && act_z >= kLiveMin)
+    out.logp = (float)(((double)act_z - (double)M) / (double)tau - log(S));
+  write_row(a, t, out, act_ok, any_bad || n == 0 ? GRPO_FLAG_NONFINITE : 0);
 }
 
 // ---- the gradient ---------------------------------------------------------------
@@ -1691,7 +1811,7 @@ static void launch_row_kernel(const RowArgs& a, int64_t T, hipStream_t s) {
   // one workgroup to a CU: twice the waves
   const bool wide = T <= 256 && a.V > 16384;
   const auto k = wide ? k_sample_row<Tin, FUSED, DRAW, 1024> : k_sample_row<Tin, FUSED, DRAW, 512>;
-  constexpr int64_t kRows = 1 << 20;  // a launch's threads stay below 2^32
+  constexpr int64_t kRows = 1 << 20;
   for (int64_t r = 0; r < T; r += kRows)
     hipLaunchKernelGGL(k, dim3((unsigned)std::min(kRows, T - r)), dim3(wide ? 1024 : 512),
                        row_tile_bytes(a.tiles), s, a, (int)r);
@@ -1699,7 +1819,14 @@ static void launch_row_kernel(const RowArgs& a, int64_t T, hipStream_t s) {
 
 template <typename Tin, bool DRAW>
 static void launch_rows(const RowArgs& a, int64_t T, hipStream_t s) {
-  if (split_rows(T, a.V)) {
+  const grpo_sampling& p = a.par;
+  constexpr int64_t kRows = 1 << 20;  // a launch's threads stay below 2^32
+  // Nothing cut anywhere, which the host sees where no setting is an array.
+  if (!DRAW && !p.temperature && !p.top_k && !p.top_p && !p.min_p && p.temperature_all > 0.f &&
+      (p.top_k_all <= 0 || p.top_k_all >= a.V) && p.top_p_all == 1.f && p.min_p_all == 0.f && !split_rows(T, a.V)) {
+    for (int64_t r = 0; r < T; r += kRows)
+      hipLaunchKernelGGL(k_tempered_logp<Tin>, dim3((unsigned)std::min(kRows, T - r)), dim3(256), 0, s, a, (int)r);
+  } else if (split_rows(T, a.V)) {
     const int waves = (int)T * a.tiles;
     hipLaunchKernelGGL(k_sample_tiles<Tin>, dim3((unsigned)(waves + 3) / 4), dim3(256), 0, s, a, waves, DRAW);
     launch_row_kernel<Tin, false, DRAW>(a, T, s);
