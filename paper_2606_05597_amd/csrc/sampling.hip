@@ -180,7 +180,7 @@ constexpr double kSum32Error = 1e-5;
 __device__ __forceinline__ SumMode sum_mode(const Settings& s, int V, bool draw, bool fused, bool by_value, int subs) {
   if (!s.ok || s.greedy) return kNoSum;
   const bool k_on = s.k > 0 && s.k < V;
-  if (fused && by_value && (k_on ? s.k > subs : s.p < 1.f)) return kCount;
+  if (fused && by_value && (k_on ? s.k > subs : s.p < 1.f || s.min_p > 0.f)) return kCount;
   if (k_on) return kNoSum;
   if (s.p < 1.f) return fused ? kSum32 : kSum64;
   if (s.min_p > 0.f) return kNoSum;
@@ -423,7 +423,7 @@ struct RowShared {
   uint32_t radix[256];
   // broadcast
   int n, bin, i0;
-  uint32_t key;
+  uint32_t key, key2;
   double d0;
 };
 
@@ -728,7 +728,7 @@ struct RowWork {
   __device__ __forceinline__ double steps(float z) const { return ((double)m - (double)z) * (c * kPerOctave); }
   __device__ __forceinline__ int bin_of(float z) const { return (int)fmin(steps(z), (double)(kBins - 1)); }
 
-  // A weight w <= 1 in 2^-44: the low bits of 256 + w.
+  // The low bits of y in [1, 2) or [256, 512): of 256 + w, a weight w <= 1 in 2^-44.
   __device__ __forceinline__ static unsigned long long fixed(double y) {
     return __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull;
   }
@@ -860,11 +860,58 @@ struct RowWork {
     return b;
   }
 
+  // The words of [lo, hi] in sh.h.some, and rec.sum = the tiles' weights of the words above hi; returns how many there are
+  // (at most kSorted, as the caller knows).
+  __device__ __forceinline__ int gather_and_sum(float lo, float hi) {
+    double s = 0.0;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = 0;
+    for (int i = threadIdx.x; i < tiles; i += NT)
+      if (!(rec.max[i] >= lo)) rec.sum[i] = 0.0;
+    __syncthreads();
+    each_vector([&](int tile) { return rec.max[tile] >= lo; },
+                [&](const u32x4& x, int tile, int j) {
+#pragma unroll
+                  for (int e = 0; e < EPV; ++e) {
+                    const float z = elem<Tin>(x, e);
+                    if (z > hi) s += weight(z);
+                    else if (z >= lo)
+                      sh.h.some[min(atomicAdd(&sh.n, 1), kSorted - 1)] =
+                          ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e);
+                  }
+                },
+                [&](int tile) {
+                  s = wave_sum_dpp(s);
+                  if ((threadIdx.x & 63) == 0) rec.sum[tile] = s;
+                  s = 0.0;
+                });
+    __syncthreads();
+    return min(uniform(sh.n), kSorted);
+  }
+
+  // rec.sum += the weights of the first r sorted words, each in its tile, in their order.
+  __device__ __forceinline__ void add_sorted(int r) {
+    const int tid = threadIdx.x;
+    double* w = reinterpret_cast<double*>(sh.h.some);
+    if (tid < r) w[tid] = weight(word_of(sh.h.sorted[tid]));
+    __syncthreads();
+    for (int i = tid; i < tiles; i += NT) {
+      double s = rec.sum[i];
+      for (int q = 0; q < r; ++q)
+        if (index_of(sh.h.sorted[q]) / Tile<Tin>::kWords == i) s += w[q];
+      rec.sum[i] = s;
+    }
+    __syncthreads();
+  }
+
   // The cut after the k-th word, or after the shortest prefix of weight `target`, among the words from x_lo up (all in the
-  // list where listed >= 0), whose histogram<true> is made.
-  __device__ __forceinline__ Cut select(int listed, bool by_mass, int k, double target) {
+  // list where listed >= 0), whose histogram<true> is made.  `sums`: rec.sum is wanted too, and true comes back in it where
+  // it holds the tiles' kept weights.
+  __device__ __forceinline__ Cut select(int listed, bool by_mass, int k, double target, bool& sums) {
     int count0 = 0, cnt;
     double mass0 = 0.0;
+    const bool want = sums && listed < 0;
+    sums = false;
     const int b = find_bin(by_mass, count0, mass0, k, target, cnt);
     // the keys that fall into bin b: bin_of only falls as the key grows; each lane tries one of 64 between the ends
     auto lowest = [&](int bin) {
@@ -879,7 +926,15 @@ struct RowWork {
       return lo;
     };
     constexpr uint32_t kMinusZero = 0x7fffffffu;  // the key that no word has: -0 counts as 0
-    uint32_t klo = lowest(b), khi = b == 0 ? order_key(m) : lowest(b - 1) - 1;
+    if (threadIdx.x < 64) {
+      const uint32_t from = lowest(b), to = b == 0 ? order_key(m) : lowest(b - 1) - 1;
+      if (threadIdx.x == 0) {
+        sh.key = from;
+        sh.key2 = to;
+      }
+    }
+    __syncthreads();
+    uint32_t klo = (uint32_t)uniform((int)sh.key), khi = (uint32_t)uniform((int)sh.key2);
     while (cnt > kSorted && klo < khi) {
       const int bits = 32 - __clz((int)(khi - klo));
       const int shift = max(0, bits - 10);  // at most kBins
@@ -919,6 +974,8 @@ struct RowWork {
       }
       __syncthreads();
       n = min(uniform(sh.n), kSorted);
+    } else if (want) {
+      n = gather_and_sum(lo, hi);
     } else {
       n = gather(sh.h.some, kSorted, lo, hi);
     }
@@ -931,7 +988,46 @@ struct RowWork {
     cut.mass = uniform(sh.h.cum[r - 1]);
     cut.count = count0 + r;
     __syncthreads();
+    if (want) {
+      add_sorted(r);
+      sums = true;
+    }
     return cut;
+  }
+
+  // rec.sum = the tiles' kept weights, all kept words in the list; their sum and number.  Added as integers.
+  __device__ __forceinline__ double list_sums(int listed, float thr, int tie, int& n) {
+    const int tid = threadIdx.x;
+    unsigned long long* sum = reinterpret_cast<unsigned long long*>(rec.sum);
+    for (int i = tid; i < tiles; i += NT) sum[i] = 0ull;
+    __syncthreads();
+    int here = 0;
+    for (int i = tid; i < listed; i += NT) {
+      const unsigned long long key = sh.h.key[i];
+      const float z = word_of(key);
+      const int col = index_of(key);
+      if (kept(z, col, thr, tie)) {
+        const double w = weight(z);  // in 2^-51, at least one of them if it is not 0
+        atomicAdd(sum + col / Tile<Tin>::kWords, max(fixed(fma(w, 0.5, 1.0)), (unsigned long long)(w > 0.0)));
+        ++here;
+      }
+    }
+    __syncthreads();
+    double s = 0.0;
+    for (int i = tid; i < tiles; i += NT) {
+      const double v = (double)sum[i] * 0x1p-51;
+      rec.sum[i] = v;
+      s += v;
+    }
+    n = block_sum(here);
+    return block_sum(s);
+  }
+
+  // The sum of rec.sum.
+  __device__ __forceinline__ double tile_sum() {
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < tiles; i += NT) sum += rec.sum[i];
+    return block_sum(sum);
   }
 
   // rec.sum = the tiles' kept weights; their sum, and the number of kept words.  In a tile before the last kept one's all
@@ -972,11 +1068,8 @@ struct RowWork {
                   s = 0.0;
                 });
     __syncthreads();
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < tiles; i += NT) sum += rec.sum[i];
-    sum = block_sum(sum);
     n = block_sum(here);
-    return sum;
+    return tile_sum();
   }
 
   // ---- the count of bf16 values ----
@@ -1190,6 +1283,18 @@ struct RowWork {
   }
 
   // ---- draws ----
+
+  // The same among the first n sorted words.
+  __device__ __forceinline__ int draw_sorted(int n, double target) {
+    const int tid = threadIdx.x;
+    sort_words<true>(sh.h.sorted, sh.h.some, n);
+    const double v = tid < n ? weight(word_of(sh.h.some[tid])) : 0.0;
+    double all;
+    const double incl = block_scan(v, all);
+    int at = block_min(v > 0.0 && incl > target ? tid : INT_MAX);
+    if (at == INT_MAX) at = block_max(v > 0.0 ? tid : 0);
+    return uniform(index_of(sh.h.some[at]));
+  }
 
   // The first kept word at which the kept weights pass `target`, from the tiles' sums in rec.sum: its tile, then its
   // words, a few to a thread; the last kept word where rounding leaves none.
@@ -1515,14 +1620,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
           const unsigned long long last_word = sh.h.sorted[n - 1];
           thr = uniform(Work::word_of(last_word));
           tie = uniform(Work::index_of(last_word));
-          if (DRAW) {  // the kept words in the order of their indices
-            w.template sort_words<true>(sh.h.sorted, sh.h.some, n);
-            const double v = tid < n ? w.weight(Work::word_of(sh.h.some[tid])) : 0.0;
-            double all;
-            const double incl = w.block_scan(v, all);
-            int at = w.block_min(v > 0.0 && incl > (double)u * S ? tid : INT_MAX);
-            if (at == INT_MAX) at = w.block_max(v > 0.0 ? tid : 0);
-            act = uniform(Work::index_of(sh.h.some[at]));
+          if (DRAW) {
+            act = w.draw_sorted(n, (double)u * S);
             drawn = true;
           }
         } else if (!cut_known) {
@@ -1534,10 +1633,12 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
               tie = i;
             }
           };
+          bool summed = false;  // rec.sum holds the tiles' kept weights
           if (k_on || p_on) {
             const bool sum_all = p_on && !k_on && !exact && listed < 0;  // S from the histogram: all live words
             if (sum_all) w.x_lo = x_lo = kLiveMin;
             double Sk = S;
+            bool sums = false;
 #pragma unroll 1
             for (int by_mass = !k_on, again = 0; by_mass <= (int)p_on; ++by_mass) {
               w.template histogram<true>(listed, x_lo, INFINITY, 0u, 0);
@@ -1547,7 +1648,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
                 Sk = w.block_sum(q);
               }
               const bool sure = sum_all || again;
-              const Cut cut = w.select(listed, by_mass, k, (sure ? p : p_lo) * Sk);
+              sums = DRAW && by_mass == (int)p_on;
+              const Cut cut = w.select(listed, by_mass, k, (sure ? p : p_lo) * Sk, sums);
               if (by_mass && !sure && p_lo < p_hi && !(cut.mass >= p_hi * Sk)) {  // S has to be exact: once more
                 int all;
                 Sk = w.kept_sums(kLiveMin, a.V, all);
@@ -1559,9 +1661,16 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
               Sk = S = cut.mass;
               n = cut.count;
             }
+            summed = sums;
           }
-          if (m_on) narrow(z_min, a.V);
-          if (DRAW || m_on) S = w.kept_sums(thr, tie, n);
+          if (m_on && (z_min > thr || !(k_on || p_on))) {
+            narrow(z_min, a.V);
+            summed = false;
+            n = INT_MAX;
+          }
+          if (listed >= 0 && (DRAW || n == INT_MAX)) S = w.list_sums(listed, thr, tie, n);
+          else if (summed) S = w.tile_sum();
+          else if (DRAW || n == INT_MAX) S = w.kept_sums(thr, tie, n);
         }
       }
       if (!drawn) act = w.draw((double)u * S, thr, tie);
