@@ -535,8 +535,16 @@ struct RowWork {
   template <typename P, typename F, typename G>
   __device__ __forceinline__ void each_vector(P want, F f, G done) const {
     each_tile(want, [&](const Tile<Tin>& x, int tile) {
+      if constexpr (EPV == 8) {
 #pragma unroll 1
-      for (int j = 0; j < NV; ++j) f(x.vec(j), tile, j);
+        for (int j = 0; j < NV; ++j) f(x.vec(j), tile, j);
+      } else {  // two at a time: eight words to overlap
+#pragma unroll 1
+        for (int j = 0; j < NV; j += 2) {
+          f(x.vec(j), tile, j);
+          f(x.vec(j + 1), tile, j + 1);
+        }
+      }
       done(tile);
     });
   }
@@ -863,6 +871,7 @@ struct RowWork {
   // The words of [lo, hi] in sh.h.some, and rec.sum = the tiles' weights of the words above hi; returns how many there are
   // (at most kSorted, as the caller knows).
   __device__ __forceinline__ int gather_and_sum(float lo, float hi) {
+    const bool far = t2(hi) < -1000.0;
     double s = 0.0;
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0;
@@ -874,8 +883,9 @@ struct RowWork {
 #pragma unroll
                   for (int e = 0; e < EPV; ++e) {
                     const float z = elem<Tin>(x, e);
-                    if (z > hi) s += weight(z);
-                    else if (z >= lo)
+                    const double t = t2(z), w = exp2_neg<false>(far ? fmax(t, -1022.0) : t);
+                    if (z > hi) s += far && t < -1021.0 ? 0.0 : w;
+                    if (z >= lo && z <= hi)
                       sh.h.some[min(atomicAdd(&sh.n, 1), kSorted - 1)] =
                           ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e);
                   }
@@ -889,18 +899,25 @@ struct RowWork {
     return min(uniform(sh.n), kSorted);
   }
 
-  // rec.sum += the weights of the first r sorted words, each in its tile, in their order.
+  // A weight w <= 1 in 2^-51, at least one of them if it is not 0: sums of up to 4,096 fit 64 bits, in any order.
+  __device__ __forceinline__ static unsigned long long fine_fixed(double w) {
+    return max(fixed(fma(w, 0.5, 1.0)), (unsigned long long)(w > 0.0));
+  }
+
+  // rec.sum += the weights of the first r sorted words, each in its tile.  The histograms' memory is free by now.
   __device__ __forceinline__ void add_sorted(int r) {
+    static_assert(sizeof(sh.h.mass) + sizeof(sh.h.count) + sizeof(sh.h.bin_mass) + sizeof(sh.h.bin_count) >=
+                      8 * (GRPO_SAMPLING_MAX_V / Tile<Tin>::kWords), "an integer for each tile");
     const int tid = threadIdx.x;
-    double* w = reinterpret_cast<double*>(sh.h.some);
-    if (tid < r) w[tid] = weight(word_of(sh.h.sorted[tid]));
+    unsigned long long* sum = sh.h.mass;
+    for (int i = tid; i < tiles; i += NT) sum[i] = 0ull;
     __syncthreads();
-    for (int i = tid; i < tiles; i += NT) {
-      double s = rec.sum[i];
-      for (int q = 0; q < r; ++q)
-        if (index_of(sh.h.sorted[q]) / Tile<Tin>::kWords == i) s += w[q];
-      rec.sum[i] = s;
+    if (tid < r) {
+      const unsigned long long key = sh.h.sorted[tid];
+      atomicAdd(sum + index_of(key) / Tile<Tin>::kWords, fine_fixed(weight(word_of(key))));
     }
+    __syncthreads();
+    for (int i = tid; i < tiles; i += NT) rec.sum[i] += (double)sum[i] * 0x1p-51;
     __syncthreads();
   }
 
@@ -1007,8 +1024,7 @@ struct RowWork {
       const float z = word_of(key);
       const int col = index_of(key);
       if (kept(z, col, thr, tie)) {
-        const double w = weight(z);  // in 2^-51, at least one of them if it is not 0
-        atomicAdd(sum + col / Tile<Tin>::kWords, max(fixed(fma(w, 0.5, 1.0)), (unsigned long long)(w > 0.0)));
+        atomicAdd(sum + col / Tile<Tin>::kWords, fine_fixed(weight(z)));
         ++here;
       }
     }
