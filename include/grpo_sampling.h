@@ -73,7 +73,8 @@ size_t grpo_sampling_workspace_bytes(int64_t T, int64_t V);
  *                with nothing cut off
  *   n_kept       device int32 [T] or NULL
  *   error_flags  device int32 [1] or NULL, overwritten
- *   ws, ws_bytes device workspace of at least grpo_sampling_workspace_bytes(T, V), 16-byte aligned
+ *   ws, ws_bytes device workspace of at least grpo_sampling_workspace_bytes(T, V), 16-byte aligned; calls that may
+ *                overlap (on two streams, in two graphs) need one each
  * A row with a NaN or +inf: action -1, log-prob NaN, n_kept 0, GRPO_FLAG_NONFINITE.  A row with nothing above -1e8:
  * action -1, log-prob -inf, n_kept 0, GRPO_FLAG_NONFINITE.  The same inputs give the same bits.
  * Errors: GRPO_ERR_ARG (a required pointer NULL, an `_all` value out of range), GRPO_ERR_SHAPE, GRPO_ERR_DTYPE,
@@ -102,8 +103,10 @@ int grpo_sampled_logp(const void* logits, int32_t dtype, int64_t T, int64_t V, i
  * a row with a NaN or +inf has NaN throughout.
  *   rows         device [T], from grpo_sampled_logp on the same logits and actions
  *   dlogp        device fp32 [T]
- *   dlogits      device [T, ld] of `dtype`; columns >= V are not written; may be `logits` itself
- * Errors: GRPO_ERR_ARG, GRPO_ERR_SHAPE, GRPO_ERR_DTYPE, GRPO_ERR_ALIGN, GRPO_ERR_HIP.
+ *   dlogits      device [T, ld] of `dtype`; columns >= V are not written; may be `logits` itself, and otherwise shares
+ *                no element with it (rows of the two may lie in turn)
+ * Errors: GRPO_ERR_ARG (a pointer NULL, dlogits over part of logits), GRPO_ERR_SHAPE, GRPO_ERR_DTYPE, GRPO_ERR_ALIGN,
+ *   GRPO_ERR_HIP.
  */
 int grpo_sampled_logp_bwd(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
                           const int32_t* actions, const grpo_sampling_row* rows, const float* dlogp, void* dlogits,

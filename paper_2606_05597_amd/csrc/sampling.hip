@@ -1931,6 +1931,15 @@ static bool bad_shape(int64_t T, int64_t V, int64_t ld) {
   return T < 0 || T >= ((int64_t)1 << 31) || V < 1 || V > GRPO_SAMPLING_MAX_V || ld < V;
 }
 
+// Whether T rows of V elements, ld apart, at two places share memory without being the same rows.
+static bool rows_overlap(const void* a, const void* b, int64_t T, int64_t V, int64_t ld, size_t esz) {
+  const uintptr_t x = std::min((uintptr_t)a, (uintptr_t)b), y = std::max((uintptr_t)a, (uintptr_t)b);
+  const uintptr_t bytes = (uintptr_t)V * esz, step = (uintptr_t)ld * esz;
+  if (x == y || y - x >= (uintptr_t)(T - 1) * step + bytes) return false;
+  const uintptr_t r = (y - x) % step;  // a row of the second begins r bytes into one of the first
+  return r < bytes || (step - r < bytes && (y - x) / step + 1 < (uintptr_t)T);
+}
+
 template <typename Tin, bool FUSED, bool DRAW>
 static void launch_row_kernel(const RowArgs& a, int64_t T, hipStream_t s) {
   // one workgroup to a CU: twice the waves
@@ -2019,6 +2028,7 @@ extern "C" int grpo_sampled_logp_bwd(const void* logits, int32_t dtype, int64_t 
   const size_t esz = dtype == GRPO_BF16 ? 2 : 4;
   if (!aligned(logits, esz) || !aligned(dlogits, esz) || !aligned(actions, 4) || !aligned(rows, 8) || !aligned(dlogp, 4))
     return GRPO_ERR_ALIGN;
+  if (T > 0 && rows_overlap(logits, dlogits, T, V, ld, esz)) return GRPO_ERR_ARG;
   const int blocks = (int)((V + kBwdCols - 1) / kBwdCols);
   const int64_t per = std::max<int64_t>(1, ((int64_t)1 << 23) / blocks);  // a launch's threads stay below 2^32
   for (int64_t r = 0; r < T; r += per) {

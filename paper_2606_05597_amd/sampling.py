@@ -57,8 +57,11 @@ def _sampling(T, temperature, top_k, top_p, min_p):
 
 def _columns(logits, V):
     dt, T, ld = _logits2d(logits)
-    V = logits.shape[1] if V is None else int(V)
-    return dt, T, V, ld
+    cols = logits.shape[1]
+    V = cols if V is None else int(V)
+    if V > cols:
+        raise ValueError(f"V must be at most logits' {cols} columns, got {V}")
+    return dt, T, V, max(ld, cols) if T == 1 else ld
 
 
 def _scratch(workspace, T, V, device):

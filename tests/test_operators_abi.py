@@ -95,6 +95,14 @@ def test_sampling_refusals_of_one_entry(lib):
         assert f(**kw) == _lib.GRPO_ERR_ALIGN
 
 
+def test_dlogits_over_part_of_the_logits_is_refused(lib):
+    """Rows of 100 columns, bf16: shifted by a column, by a row, by a column less than the row's width."""
+    f = lambda d, ld, T=8: lib.grpo_sampled_logp_bwd(D, 1, T, 100, ld, D, D, D, ctypes.c_void_p(0x100000 + 2 * d), None)  # noqa: E731
+    for d, ld in ((1, 100), (99, 100), (100, 100), (700, 100), (-1, 100), (-100, 100), (99, 200), (101, 200), (-99, 200),
+                  (1 * 200 + 50, 200), (7 * 200 + 99, 200)):
+        assert f(d, ld) == _lib.GRPO_ERR_ARG, (d, ld)
+
+
 def test_sampling_workspace(lib):
     f = lib.grpo_sampling_workspace_bytes
     assert f(-1, 10) == 0 and f(1, 0) == 0 and f(1, (1 << 22) + 1) == 0
@@ -183,6 +191,8 @@ def test_binding_refuses_host_tensors_and_wrong_types():
             call(top_p=torch.ones(4))
     with pytest.raises(ValueError):
         grpo.grpo_sample(z, torch.zeros(2))
+    with pytest.raises(ValueError, match="columns"):
+        grpo.grpo_sample(torch.zeros(3, 16)[:, :8], u, V=9)
     with pytest.raises(TypeError):
         grpo.grpo_sample(z.half(), u)
     with pytest.raises(ValueError):
