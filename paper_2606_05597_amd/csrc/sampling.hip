@@ -36,11 +36,24 @@
 namespace grpo {
 
 constexpr int kTileVecs = 4;       // a tile: 4 vectors of 16 bytes per lane, 2,048 bf16 words or 1,024 of fp32
-constexpr int kSubs = 8;           // partial maxima of a tile, each over 8 lanes' words
-constexpr int kMaxSubs = 1280;     // partial maxima (or tiles' maxima) that bound the k-th largest word
-constexpr int kCap = 2048;         // words that a list in LDS holds
-constexpr int kSorted = 256;       // words that are sorted
-constexpr int kBins = 1024, kCols = 2;  // bins of 1/32 of a power of two of weight, each in kCols copies
+constexpr int kSubs = 8;           // partial maxima of a tile in its record, each over 8 lanes' words
+
+// What a row's workgroup of NT threads holds in LDS, and so how many rows a CU works on at once: two with 512 threads (one
+// with 1,024), four with 256 for rows of at most 16,384 words.
+template <int NT>
+struct RowShape {
+  static constexpr int kMaxSubs = 1280;  // partial maxima (or tiles' maxima) that bound the k-th largest word
+  static constexpr int kCap = 2048;      // words that a list holds
+  static constexpr int kSorted = 256;    // words that are sorted
+  static constexpr int kBins = 1024, kCols = 2;  // bins of 32 to a power of two of weight, each in kCols copies
+  static constexpr int kMaxWords = GRPO_SAMPLING_MAX_V;
+  static constexpr bool kValueTable = true;  // room for the counts of bf16 values
+};
+template <>
+struct RowShape<256> {
+  static constexpr int kMaxSubs = 1024, kCap = 1024, kSorted = 256, kBins = 512, kCols = 1, kMaxWords = 16384;
+  static constexpr bool kValueTable = false;
+};
 constexpr int kMaxNW = 16;
 constexpr float kLimit = 64.f;     // logits that the count of values takes: below it in size
 constexpr float kLiveMin = -99999992.f;  // the smallest float above -1e8: the lowest live logit
@@ -248,7 +261,8 @@ struct Tile {
 
 struct TileStats {
   double sum;   // of weights relative to max; every lane
-  float sub;    // the maximum over this lane's group of 8 lanes
+  float own;    // the maximum of this lane's words
+  float sub;    // over its group of 8 lanes
   float max;    // every lane
   float lo;     // the least live logit; every lane
   int live;     // every lane
@@ -270,6 +284,7 @@ __device__ __forceinline__ TileStats tile_stats(const Tile<Tin>& x, SumMode mode
       mx = max3f(mx, p, q);
       mn = min3f(mn, p, q);
     }
+  s.own = mx;
   float g = fmaxf(mx, dpp_f32v<0xB1>(mx));
   g = fmaxf(g, dpp_f32v<0x4E>(g));
   s.sub = fmaxf(g, dpp_f32v<0x141>(g));
@@ -397,26 +412,33 @@ struct Cut {
   int count;
 };
 
+template <bool TABLE>
+struct ValueTable {
+  double weight[kValues];
+  uint32_t count[kValues];
+  unsigned long long mid;  // the weight of the words of bin kMid, in 2^-44 of the next bin's
+};
+template <>
+struct ValueTable<false> {};
+
+template <int NT>
 struct RowShared {
+  typedef RowShape<NT> Shape;
   union {
     struct {
-      unsigned long long mass[kBins * kCols];
-      uint32_t count[kBins * kCols];
-      double bin_mass[kBins];
-      int bin_count[kBins];
-      unsigned long long key[kCap];      // a list of words: order_key, ~index
-      unsigned long long some[kSorted];  // a few of them
-      unsigned long long sorted[kSorted];
-      double cum[kSorted];               // prefix sums of the sorted ones' weights
+      unsigned long long mass[Shape::kBins * Shape::kCols];
+      uint32_t count[Shape::kBins * Shape::kCols];
+      double bin_mass[Shape::kBins];
+      int bin_count[Shape::kBins];
+      unsigned long long key[Shape::kCap];      // a list of words: order_key, ~index
+      unsigned long long some[Shape::kSorted];  // a few of them
+      unsigned long long sorted[Shape::kSorted];
+      double cum[Shape::kSorted];               // prefix sums of the sorted ones' weights
     } h;
-    struct {
-      double weight[kValues];
-      uint32_t count[kValues];
-      unsigned long long mid;  // the weight of the words of bin kMid, in 2^-44 of `mid_top`'s
-    } v;
+    ValueTable<Shape::kValueTable> v;
   };
-  float sub[kMaxSubs];
-  uint16_t block[kMaxSubs];
+  float sub[Shape::kMaxSubs];
+  uint16_t block[Shape::kMaxSubs];
   double wd[2][kMaxNW];
   int wi[2][kMaxNW];
   float wf[2][kMaxNW];
@@ -437,16 +459,20 @@ __host__ __device__ constexpr size_t row_tile_bytes(int tiles) { return (size_t)
 
 template <typename Tin, int NT>
 struct RowWork {
+  typedef RowShape<NT> Shape;
   static constexpr int NW = NT / 64, NV = Tile<Tin>::NV, EPV = Tile<Tin>::EPV;
-  static constexpr bool kByValue = sizeof(Tin) == 2;
-  RowShared& sh;
+  static constexpr int kBins = Shape::kBins, kCols = Shape::kCols, kCap = Shape::kCap, kSorted = Shape::kSorted;
+  static constexpr int kMaxTiles = (Shape::kMaxWords + Tile<Tin>::kWords - 1) / Tile<Tin>::kWords;
+  static constexpr bool kByValue = sizeof(Tin) == 2 && Shape::kValueTable;
+  RowShared<NT>& sh;
   RowTiles rec;
   const Tin* row;
   int V, tiles;
   float m;   // the row's maximum
   double c;  // log2(e) / tau
   float x_lo;  // words below it are not looked at
-  bool fine;   // sh.sub holds every tile's partial maxima
+  int per;     // partial maxima of a tile: 64, 8 or 1, each over 64 / per lanes' words
+  bool fine;   // sh.sub holds them
 
   int turn = 0;  // which of the two sets of sh.w* the next reduction takes
 
@@ -557,14 +583,16 @@ struct RowWork {
 
   // ---- a list of words in LDS ----
 
-  // The words of [lo, hi] in `list`, in no order; returns how many there are, or more than it has room for.  Eight lanes
-  // read the words of one partial maximum, only of those that reach lo; without partial maxima, of every tile that does.
+  // The words of [lo, hi] in `list`, in no order; returns how many there are, or more than it has room for.  As many lanes
+  // as a partial maximum is over read their words again, only of those that reach lo; without partial maxima, of every
+  // tile that does.
   __device__ __forceinline__ int gather(unsigned long long* list, int room, float lo, float hi) {
     const int tid = threadIdx.x, lane = tid & 63;
     __syncthreads();
     if (tid == 0) sh.n = sh.bin = 0;
     __syncthreads();
-    int blocks = tiles * kSubs;
+    const int wide = 64 / per;  // lanes that read a block
+    int blocks = tiles * per;
     if (fine) {
       for (int i = tid; i < blocks; i += NT)
         if (sh.sub[i] >= lo) sh.block[atomicAdd(&sh.bin, 1)] = (uint16_t)i;
@@ -573,19 +601,19 @@ struct RowWork {
     }
     // this thread's block of round g0: its tile and the lane whose words it reads, or -1
     auto block_at = [&](int g0) {
-      const int g = g0 + tid / kSubs;
+      const int g = g0 + tid / wide;
       if (g >= blocks) return -1;
       const int b = fine ? sh.block[g] : g;
-      return rec.max[b / kSubs] >= lo ? b : -1;
+      return rec.max[b / per] >= lo ? b : -1;
     };
-    auto lane_of = [&](int b) { return (b & (kSubs - 1)) * 8 + (tid & 7); };
+    auto lane_of = [&](int b) { return max(b, 0) % per * wide + tid % wide; };
     Tile<Tin> x, y;
     int block = block_at(0);
-    if (__any(block >= 0)) x.load(row, V, max(block, 0) / kSubs, lane_of(block));
-    for (int g0 = 0; g0 < blocks; g0 += NT / kSubs) {
+    if (__any(block >= 0)) x.load(row, V, max(block, 0) / per, lane_of(block));
+    for (int g0 = 0; g0 < blocks; g0 += NT / wide) {
       if (uniform(*(volatile int*)&sh.n) > room) break;
-      const int next = block_at(g0 + NT / kSubs);
-      if (__any(next >= 0)) y.load(row, V, max(next, 0) / kSubs, lane_of(next));
+      const int next = block_at(g0 + NT / wide);
+      if (__any(next >= 0)) y.load(row, V, max(next, 0) / per, lane_of(next));
       int mine = 0;
       if (block >= 0) {
 #pragma unroll
@@ -601,7 +629,7 @@ struct RowWork {
         if (at + all > room) break;
         at += incl - mine;
         if (mine > 0) {
-          const int tile = block / kSubs, own = lane_of(block);
+          const int tile = block / per, own = lane_of(block);
 #pragma unroll
           for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -731,8 +759,8 @@ struct RowWork {
 
   // ---- histograms of weight ----
 
-  static constexpr double kPerOctave = 32.0;
-  // How many 1/kPerOctave of an octave a word lies below the maximum.
+  static constexpr double kPerOctave = kBins / 32;
+  // How many 1/kPerOctave of an octave (a power of two of weight) a word lies below the maximum.
   __device__ __forceinline__ double steps(float z) const { return ((double)m - (double)z) * (c * kPerOctave); }
   __device__ __forceinline__ int bin_of(float z) const { return (int)fmin(steps(z), (double)(kBins - 1)); }
 
@@ -761,15 +789,18 @@ struct RowWork {
       int b;
       double y;
       if constexpr (TOP) {
-        // 2^(-x / 32) for the rest x of the steps, by its interpolant of degree 5: off by 1.2e-16
         const double q = steps(z);
         b = (int)fmin(q, (double)(kBins - 1));
         const double x = q - (double)b;
-        y = fma(x, -3.930921700473334e-11, 9.172082236776783e-09);
-        y = fma(x, y, -1.6938507235263203e-06);
-        y = fma(x, y, 0.00023459619814393515);
-        y = fma(x, y, -0.021660849392493294);
-        y = fma(x, y, 257.0);
+        if constexpr (kBins == 1024) {  // 2^(-x / 32) for the rest x, by its interpolant of degree 5: off by 1.2e-16
+          y = fma(x, -3.930921700473334e-11, 9.172082236776783e-09);
+          y = fma(x, y, -1.6938507235263203e-06);
+          y = fma(x, y, 0.00023459619814393515);
+          y = fma(x, y, -0.021660849392493294);
+          y = fma(x, y, 257.0);
+        } else {
+          y = exp2_neg(x * (-1.0 / kPerOctave)) + 256.0;
+        }
         if (b == kBins - 1) {
           const double r = exp2_neg(x * (-1.0 / kPerOctave));
           if (listed < 0) {
@@ -907,7 +938,7 @@ struct RowWork {
   // rec.sum += the weights of the first r sorted words, each in its tile.  The histograms' memory is free by now.
   __device__ __forceinline__ void add_sorted(int r) {
     static_assert(sizeof(sh.h.mass) + sizeof(sh.h.count) + sizeof(sh.h.bin_mass) + sizeof(sh.h.bin_count) >=
-                      8 * (GRPO_SAMPLING_MAX_V / Tile<Tin>::kWords), "an integer for each tile");
+                      8 * kMaxTiles, "an integer for each tile");
     const int tid = threadIdx.x;
     unsigned long long* sum = sh.h.mass;
     for (int i = tid; i < tiles; i += NT) sum[i] = 0ull;
@@ -954,7 +985,8 @@ struct RowWork {
     uint32_t klo = (uint32_t)uniform((int)sh.key), khi = (uint32_t)uniform((int)sh.key2);
     while (cnt > kSorted && klo < khi) {
       const int bits = 32 - __clz((int)(khi - klo));
-      const int shift = max(0, bits - 10);  // at most kBins
+      constexpr int kBinBits = 31 - __builtin_clz(kBins);
+      const int shift = max(0, bits - kBinBits);
       histogram<false>(listed, key_value(klo), key_value(khi), khi, shift);
       const int q = find_bin(by_mass, count0, mass0, k, target, cnt);
       khi -= (uint32_t)q << shift;
@@ -1339,13 +1371,14 @@ struct RowWork {
       left = INFINITY;
     }
     const int col0 = tile * Tile<Tin>::kWords + tid * kEach;
-    float z[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      z[e] = tid * kEach + e < Tile<Tin>::kWords && col0 + e < V ? load_elem(row + col0 + e) : -INFINITY;
-    auto word = [&](int e) { return z[e] >= kLiveMin && kept(z[e], col0 + e, thr, tie) ? weight(z[e]) : 0.0; };
+    auto word = [&](int e) {
+      const int col = col0 + e;
+      if (tid * kEach + e >= Tile<Tin>::kWords || col >= V) return 0.0;
+      const float z = load_elem(row + col);
+      return z >= kLiveMin && kept(z, col, thr, tie) ? weight(z) : 0.0;
+    };
     double s = 0.0;
-#pragma unroll
+#pragma unroll 4
     for (int e = 0; e < kEach; ++e) s += word(e);
     if (tid == 0) sh.i0 = min(tile * Tile<Tin>::kWords, V - 1);  // a place in the row, whatever the sums
     const double incl = block_scan(s, total);
@@ -1354,15 +1387,12 @@ struct RowWork {
     if (tid == at) {
       double run = incl - s;
       int col = col0;
-      bool over = false;
-#pragma unroll
+#pragma unroll 1
       for (int e = 0; e < kEach; ++e) {
         const double v = word(e);
         run += v;
-        if (v > 0.0 && !over) {
-          col = col0 + e;  // the last one where the sum in another order does not pass
-          over = run > left;
-        }
+        if (v > 0.0) col = col0 + e;  // the last one where the sum in another order does not pass
+        if (v > 0.0 && run > left) break;
       }
       sh.i0 = col;
     }
@@ -1379,7 +1409,7 @@ struct RowWork {
     uint32_t t = 0;
 #pragma unroll 1
     for (int shift = 24; shift >= 16; shift -= 8) {
-      if (tid < 256) sh.radix[tid] = 0u;
+      for (int i = tid; i < 256; i += NT) sh.radix[i] = 0u;
       __syncthreads();
       for (int i = tid; i < n; i += NT) {
         const uint32_t key = order_key(sh.sub[i]);
@@ -1433,7 +1463,7 @@ __device__ __forceinline__ void write_row(const RowArgs& a, int t, grpo_sampling
 
 template <typename Tin, bool FUSED, bool DRAW, int NT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_sample_row(const RowArgs a, int row0) {
-  __shared__ RowShared sh;
+  __shared__ RowShared<NT> sh;
   extern __shared__ double tile_mem[];
   typedef RowWork<Tin, NT> Work;
   constexpr int NW = NT / 64;
@@ -1451,11 +1481,13 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
   }
   const bool act_ok = DRAW || (act >= 0 && act < a.V);
   const bool k_on = st.k > 0 && st.k < a.V, p_on = st.p < 1.f, m_on = st.min_p > 0.f;
-  const int subs = a.tiles * kSubs <= kMaxSubs ? a.tiles * kSubs : a.tiles <= kMaxSubs ? a.tiles : 0;
-  const bool fine = a.tiles * kSubs <= kMaxSubs;
+  constexpr int kMaxSubs = Work::Shape::kMaxSubs, kCap = Work::kCap, kSorted = Work::kSorted, kBins = Work::kBins;
+  const int per = FUSED && a.tiles * 64 <= kMaxSubs ? 64 : a.tiles * kSubs <= kMaxSubs ? kSubs : 1;
+  const bool fine = a.tiles * per <= kMaxSubs;
+  const int subs = fine ? a.tiles * per : 0;
   const RowTiles rec{tile_mem, reinterpret_cast<float*>(tile_mem + a.tiles),
                      reinterpret_cast<int*>(tile_mem + a.tiles) + a.tiles};
-  Work w{sh, rec, row, a.V, a.tiles, 0.f, st.c, kLiveMin, fine};
+  Work w{sh, rec, row, a.V, a.tiles, 0.f, st.c, kLiveMin, per, fine};
 
   // the tiles' records
   float m = -INFINITY, lo = INFINITY;
@@ -1472,9 +1504,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
                     if (mode == kCount) w.count_values(x);
                   }
                   const TileStats s = tile_stats<Tin>(x, mode, st.c);
-                  if (fine && (lane & 7) == 0) sh.sub[tile * kSubs + (lane >> 3)] = s.sub;
+                  if (per == 64) sh.sub[tile * 64 + lane] = s.own;
+                  else if (per == kSubs && (lane & 7) == 0) sh.sub[tile * kSubs + (lane >> 3)] = s.sub;
                   if (lane == 0) {
-                    if (!fine && subs) sh.sub[tile] = s.max;
+                    if (per == 1 && fine) sh.sub[tile] = s.max;
                     rec.sum[tile] = s.sum;
                     rec.max[tile] = s.max;
                   }
@@ -1490,10 +1523,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
       float mx = r.sub[0];
 #pragma unroll
       for (int q = 1; q < kSubs; ++q) mx = fmaxf(mx, r.sub[q]);
-      if (fine) {
+      if (per == kSubs) {
 #pragma unroll
         for (int q = 0; q < kSubs; ++q) sh.sub[i * kSubs + q] = r.sub[q];
-      } else if (subs) {
+      } else if (fine) {
         sh.sub[i] = mx;
       }
       rec.sum[i] = r.sum;
@@ -1940,32 +1973,47 @@ static bool rows_overlap(const void* a, const void* b, int64_t T, int64_t V, int
   return r < bytes || (step - r < bytes && (y - x) / step + 1 < (uintptr_t)T);
 }
 
-template <typename Tin, bool FUSED, bool DRAW>
+constexpr int64_t kRowsPerLaunch = 1 << 20;  // a launch's threads stay below 2^32
+
+template <typename Tin, bool FUSED, bool DRAW, int NT>
 static void launch_row_kernel(const RowArgs& a, int64_t T, hipStream_t s) {
-  // one workgroup to a CU: twice the waves
-  const bool wide = T <= 256 && a.V > 16384;
-  const auto k = wide ? k_sample_row<Tin, FUSED, DRAW, 1024> : k_sample_row<Tin, FUSED, DRAW, 512>;
-  constexpr int64_t kRows = 1 << 20;
-  for (int64_t r = 0; r < T; r += kRows)
-    hipLaunchKernelGGL(k, dim3((unsigned)std::min(kRows, T - r)), dim3(wide ? 1024 : 512),
+  for (int64_t r = 0; r < T; r += kRowsPerLaunch)
+    hipLaunchKernelGGL((k_sample_row<Tin, FUSED, DRAW, NT>), dim3((unsigned)std::min(kRowsPerLaunch, T - r)), dim3(NT),
                        row_tile_bytes(a.tiles), s, a, (int)r);
+}
+
+// Whether rows go to workgroups of 256 threads, four on a CU, and not to ones of 512 or 1,024.  Up to 16,384 words a top-k
+// is found among the partial maxima that such a workgroup holds (us, 256 against 512 threads, bf16, k = 50 with p = 0.95:
+// V = 2,000 T = 4 12 and 13, T = 3,000 37 and 76; V = 16,384 T = 4 13 and 14, T = 3,000 49 and 85).  A top-p alone goes
+// through more of the row, which few rows do faster with more threads (V = 16,384, T = 200: bf16 44 and 29, fp32 43 and
+// 34) and many with more rows at once (T = 3,000: V = 2,048 bf16 57 and 104; V = 8,000 bf16 103 and 128; V = 16,384
+// fp32 144 and 177), but for bf16 rows beyond 8,192 words, whose values the large workgroup counts (141 and 120).
+template <typename Tin>
+static bool short_rows(const RowArgs& a, int64_t T) {
+  if (a.V > RowShape<256>::kMaxWords) return false;
+  if (a.par.top_k || a.par.top_k_all > 0 || a.V <= 2048) return true;
+  return T > 512 && (a.V <= 8192 || sizeof(Tin) == 4);
 }
 
 template <typename Tin, bool DRAW>
 static void launch_rows(const RowArgs& a, int64_t T, hipStream_t s) {
   const grpo_sampling& p = a.par;
-  constexpr int64_t kRows = 1 << 20;  // a launch's threads stay below 2^32
   // Nothing cut anywhere, which the host sees where no setting is an array.
   if (!DRAW && !p.temperature && !p.top_k && !p.top_p && !p.min_p && p.temperature_all > 0.f &&
       (p.top_k_all <= 0 || p.top_k_all >= a.V) && p.top_p_all == 1.f && p.min_p_all == 0.f && !split_rows(T, a.V)) {
-    for (int64_t r = 0; r < T; r += kRows)
-      hipLaunchKernelGGL(k_tempered_logp<Tin>, dim3((unsigned)std::min(kRows, T - r)), dim3(256), 0, s, a, (int)r);
+    for (int64_t r = 0; r < T; r += kRowsPerLaunch)
+      hipLaunchKernelGGL(k_tempered_logp<Tin>, dim3((unsigned)std::min(kRowsPerLaunch, T - r)), dim3(256), 0, s, a,
+                         (int)r);
   } else if (split_rows(T, a.V)) {
     const int waves = (int)T * a.tiles;
     hipLaunchKernelGGL(k_sample_tiles<Tin>, dim3((unsigned)(waves + 3) / 4), dim3(256), 0, s, a, waves, DRAW);
-    launch_row_kernel<Tin, false, DRAW>(a, T, s);
+    launch_row_kernel<Tin, false, DRAW, 1024>(a, T, s);
+  } else if (short_rows<Tin>(a, T)) {
+    launch_row_kernel<Tin, true, DRAW, 256>(a, T, s);
+  } else if (a.V > RowShape<256>::kMaxWords && T <= 256) {
+    launch_row_kernel<Tin, true, DRAW, 1024>(a, T, s);
   } else {
-    launch_row_kernel<Tin, true, DRAW>(a, T, s);
+    launch_row_kernel<Tin, true, DRAW, 512>(a, T, s);
   }
 }
 
