@@ -1941,7 +1941,7 @@ __global__ void k_clear_sampling_flag(int32_t* f) { *f = 0; }
 
 // ---- host -----------------------------------------------------------------------
 
-// Whether the tiles are reduced by a launch of their own.
+// Whether the tiles may be reduced by a launch of their own, which needs a workspace.
 static bool split_rows(int64_t T, int64_t V) { return T > 0 && T < 192 && V > 16384; }
 
 static int tile_count(int64_t V, bool bf16) {
@@ -1995,22 +1995,42 @@ static bool short_rows(const RowArgs& a, int64_t T) {
   return T > 512 && (a.V <= 8192 || sizeof(Tin) == 4);
 }
 
+// Whether nothing is cut anywhere, which the host sees where no setting is an array.
+static bool nothing_cut(const grpo_sampling& p, int V) {
+  return !p.temperature && !p.top_k && !p.top_p && !p.min_p && p.temperature_all > 0.f &&
+         (p.top_k_all <= 0 || p.top_k_all >= V) && p.top_p_all == 1.f && p.min_p_all == 0.f;
+}
+
+// Whether the tiles are reduced by a launch of their own, which spreads a row over the chip but lets the row's workgroup
+// see each tile's record alone.  Where nothing is cut that is all it needs (us, two launches against one: V = 17,000
+// bf16 T = 1 14 and 15; V = 152,064 T = 1 13 and 38, T = 64 21 and 39, T = 191 36 and 41).  A cut reads the row again:
+// two launches pay for the longest of few rows (fp32 top-p: V = 50,000 T = 64 62 and 60; V = 152,064 T = 1 130 and 141,
+// T = 191 164 and 150; bf16 k = 50 with p = 0.95: T = 1 17 and 21, T = 128 25 and 24), and not for a bf16 row with a top-p
+// alone, which one launch counts by value as it reads it first (T = 1 49 and 43, T = 64 57 and 44).
+template <typename Tin>
+static bool split_now(const RowArgs& a, int64_t T) {
+  const grpo_sampling& p = a.par;
+  if (!split_rows(T, a.V)) return false;
+  if (nothing_cut(p, a.V)) return true;
+  const bool counted = sizeof(Tin) == 2 && (p.top_k || p.top_k_all <= 0) && (p.top_p || p.top_p_all < 1.f);
+  return T <= 64 && a.V > 65536 && !counted;
+}
+
 template <typename Tin, bool DRAW>
 static void launch_rows(const RowArgs& a, int64_t T, hipStream_t s) {
-  const grpo_sampling& p = a.par;
-  // Nothing cut anywhere, which the host sees where no setting is an array.
-  if (!DRAW && !p.temperature && !p.top_k && !p.top_p && !p.min_p && p.temperature_all > 0.f &&
-      (p.top_k_all <= 0 || p.top_k_all >= a.V) && p.top_p_all == 1.f && p.min_p_all == 0.f && !split_rows(T, a.V)) {
-    for (int64_t r = 0; r < T; r += kRowsPerLaunch)
-      hipLaunchKernelGGL(k_tempered_logp<Tin>, dim3((unsigned)std::min(kRowsPerLaunch, T - r)), dim3(256), 0, s, a,
-                         (int)r);
-  } else if (split_rows(T, a.V)) {
+  if (split_now<Tin>(a, T)) {
     const int waves = (int)T * a.tiles;
     hipLaunchKernelGGL(k_sample_tiles<Tin>, dim3((unsigned)(waves + 3) / 4), dim3(256), 0, s, a, waves, DRAW);
     launch_row_kernel<Tin, false, DRAW, 1024>(a, T, s);
+  } else if (!DRAW && nothing_cut(a.par, a.V)) {
+    for (int64_t r = 0; r < T; r += kRowsPerLaunch)
+      hipLaunchKernelGGL(k_tempered_logp<Tin>, dim3((unsigned)std::min(kRowsPerLaunch, T - r)), dim3(256), 0, s, a,
+                         (int)r);
   } else if (short_rows<Tin>(a, T)) {
     launch_row_kernel<Tin, true, DRAW, 256>(a, T, s);
   } else if (a.V > RowShape<256>::kMaxWords && T <= 256) {
+    // one row per CU: all its waves for that row (us, 1,024 against 512 threads, top-p alone: V = 152,064 T = 256 bf16 48 and
+    // 54, fp32 157 and 186; T = 400 bf16 89 and 77, fp32 283 and 265; T = 1,500 bf16 251 and 198)
     launch_row_kernel<Tin, true, DRAW, 1024>(a, T, s);
   } else {
     launch_row_kernel<Tin, true, DRAW, 512>(a, T, s);

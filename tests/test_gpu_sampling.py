@@ -119,8 +119,8 @@ PARS = [
 
 @pytest.mark.parametrize("par", PARS, ids=lambda p: "-".join(f"{k}{v}" for k, v in p.items()) or "off")
 @pytest.mark.parametrize("kind", ["normal", "peaked", "ties"])
-@pytest.mark.parametrize("T,V,dtype", [(3, 1024, F32), (2, 2049, BF16), (5, 32003, F32), (2, 151936, BF16)],
-                         ids=str)
+@pytest.mark.parametrize("T,V,dtype", [(3, 1024, F32), (2, 2049, BF16), (5, 32003, F32), (2, 151936, BF16),
+                                       (2, 70001, F32), (65, 66001, BF16)], ids=str)
 def test_settings(T, V, dtype, kind, par):
     logits, z = make(kind, T, V, dtype, 7 * V + T)
     check(logits, z, par, uniform(z, par, V), V)
@@ -145,6 +145,14 @@ def test_values(V, dtype, kind):
             dict(temperature=2.5, top_k=V - 7, top_p=0.81, min_p=0.003)]
     for i, par in enumerate(pars):
         logits, z = make(kind, 2, V, dtype, V + i)
+        check(logits, z, par, uniform(z, par, V + i), V)
+
+
+@pytest.mark.parametrize("T,V,dtype", [(600, 2500, BF16), (600, 9000, BF16), (600, 9000, F32), (300, 9000, BF16),
+                                       (300, 20000, BF16), (1100, 300, F32), (64, 70000, BF16), (64, 70000, F32)], ids=str)
+def test_rows_of_every_launch(T, V, dtype):
+    for i, par in enumerate([{}, dict(top_k=40), dict(top_p=0.9), dict(top_k=3000, top_p=0.99), dict(min_p=1e-3)]):
+        logits, z = make("normal", T, V, dtype, V + T + i)
         check(logits, z, par, uniform(z, par, V + i), V)
 
 
