@@ -900,22 +900,26 @@ struct RowWork {
   }
 
   // The words of [lo, hi] in sh.h.some, and rec.sum = the tiles' weights of the words above hi; returns how many there are
-  // (at most kSorted, as the caller knows).
-  __device__ __forceinline__ int gather_and_sum(float lo, float hi) {
-    const bool far = t2(hi) < -1000.0;
+  // (at most kSorted, as the caller knows).  ALL: also `all`, the weight of this thread's live words.
+  template <bool ALL>
+  __device__ __forceinline__ int gather_and_sum(float lo, float hi, double& all) {
+    const bool far = ALL || t2(hi) < -1000.0;
+    const float least = ALL ? kLiveMin : lo;
     double s = 0.0;
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0;
     for (int i = threadIdx.x; i < tiles; i += NT)
-      if (!(rec.max[i] >= lo)) rec.sum[i] = 0.0;
+      if (!(rec.max[i] >= least)) rec.sum[i] = 0.0;
     __syncthreads();
-    each_vector([&](int tile) { return rec.max[tile] >= lo; },
+    each_vector([&](int tile) { return rec.max[tile] >= least; },
                 [&](const u32x4& x, int tile, int j) {
 #pragma unroll
                   for (int e = 0; e < EPV; ++e) {
                     const float z = elem<Tin>(x, e);
                     const double t = t2(z), w = exp2_neg<false>(far ? fmax(t, -1022.0) : t);
-                    if (z > hi) s += far && t < -1021.0 ? 0.0 : w;
+                    const double v = far && t < -1021.0 ? 0.0 : w;
+                    if (ALL && z >= kLiveMin) all += v;
+                    if (z > hi) s += v;
                     if (z >= lo && z <= hi)
                       sh.h.some[min(atomicAdd(&sh.n, 1), kSorted - 1)] =
                           ((unsigned long long)order_key(z) << 32) | (uint32_t)~Tile<Tin>::col(tile, j, e);
@@ -952,6 +956,160 @@ struct RowWork {
     __syncthreads();
   }
 
+  static constexpr uint32_t kMinusZero = 0x7fffffffu;  // the key that no word has: -0 counts as 0
+
+  // The keys, from `least`'s up, that `bin` takes to b0 .. b1; it only falls as the key grows.  Waves 0 and 1 look for one
+  // end each, a lane trying one of 64 keys between the ends.
+  template <typename F>
+  __device__ __forceinline__ void keys_of(int b0, int b1, float least, F bin, uint32_t& klo, uint32_t& khi) {
+    if (threadIdx.x < 128) {
+      const bool top = uniform((int)(threadIdx.x >> 6));
+      uint32_t lo = order_key(least), hi = order_key(m);
+      if (top && b0 == 0) lo = ++hi;
+      while (lo < hi) {
+        const uint32_t step = (hi - lo) / 64 + 1, key = lo + (threadIdx.x & 63) * step;
+        const uint64_t mask = __ballot(key >= hi || bin(key_value(key)) <= (top ? b0 - 1 : b1));
+        const uint32_t l = mask ? (uint32_t)__ffsll((unsigned long long)mask) - 1 : 64;
+        if (l < 64) hi = min(hi, lo + l * step);
+        if (l > 0) lo = lo + (l - 1) * step + 1;
+      }
+      if ((threadIdx.x & 63) == 0) *(top ? &sh.key2 : &sh.key) = top ? lo - 1 : lo;
+    }
+    __syncthreads();
+    klo = (uint32_t)uniform((int)sh.key);
+    khi = (uint32_t)uniform((int)sh.key2);
+  }
+
+  // ---- a cut by counts alone ----
+  // The row's words are counted by fine bins of weight.  Counts say exactly where the k-th word is.  For a weight, the
+  // bins' counts times their middles say where the words below the cut, all lighter than it, weigh what is to be left out:
+  // within a bin or so, since no heavy word adds to the error.  One pass then gathers these bins' words and sums the ones
+  // above them in fp64, and the cut is accepted if the sums confirm that it lies among them.
+
+  static constexpr int kFine = 2 * kBins * kCols;  // bins, in the histograms' memory
+  __device__ __forceinline__ int fine_of(float z, float cf) const {
+    return (int)fminf((m - z) * cf, (float)(kFine - 1));
+  }
+
+  // The last bin, without a lower end, is not counted.
+  __device__ __forceinline__ void count_fine(float cf) {
+    uint32_t* bins = reinterpret_cast<uint32_t*>(sh.h.mass);
+    __syncthreads();
+    for (int i = threadIdx.x; i < kFine; i += NT) bins[i] = 0u;
+    __syncthreads();
+    each_vector([&](int tile) { return rec.max[tile] >= kLiveMin; },
+                [&](const u32x4& x, int, int) {
+#pragma unroll
+                  for (int e = 0; e < EPV; ++e) {
+                    const float z = elem<Tin>(x, e);
+                    const int b = fine_of(z, cf);
+                    if (z >= kLiveMin && b < kFine - 1) atomicAdd(bins + b, 1u);
+                  }
+                },
+                [](int) {});
+    __syncthreads();
+  }
+
+  // The bins b0 .. b1 that hold the k-th word, or the word with what weighs `left_out` below it among the words that weigh
+  // `whole` by the middles of their bins (0: all of them); the words before them and in them.  By k, `whole` comes back as
+  // what the first k words weigh.  False where the cut is below the counted bins or too many words are in these.
+  __device__ __forceinline__ bool find_fine(bool by_mass, int k, double left_out, double octave, double& whole, int& b0,
+                                            int& b1, int& before, int& cnt) {
+    constexpr int kEach = kFine / NT;
+    const uint32_t* bins = reinterpret_cast<const uint32_t*>(sh.h.mass);
+    const int tid = threadIdx.x;
+    const double w0 = exp2_neg((tid * kEach + 0.5) * -octave), step = exp2_neg(-octave);
+    int n = 0, all_n;
+    double e = 0.0, all_e, w = w0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i, w *= step) {
+      const int q = (int)bins[tid * kEach + i];
+      n += q;
+      e += q * w;
+    }
+    const int mine = n;
+    const double my_e = e;
+    block_scan(n, e, all_n, all_e);
+    const double target = (whole > 0.0 ? whole : all_e) - left_out;
+    const int at = block_min(mine > 0 && (by_mass ? e >= target : n >= k) ? tid : INT_MAX);
+    if (at == INT_MAX) return false;
+    if (tid == at) {
+      n -= mine;
+      e -= my_e;
+      w = w0;
+#pragma unroll 1
+      for (int i = 0; i < kEach; ++i, w *= step) {
+        const int q = (int)bins[tid * kEach + i];
+        if (q == 0) continue;
+        sh.bin = tid * kEach + i;
+        sh.i0 = n;
+        sh.d0 = by_mass ? (target - e) / (q * w) : e + (k - n) * w;  // how far into the bin; the first k words' weight
+        n += q;
+        e += q * w;
+        if (by_mass ? e >= target : n >= k) break;
+      }
+    }
+    __syncthreads();
+    const double d = uniform(sh.d0);
+    b0 = b1 = uniform(sh.bin);
+    before = uniform(sh.i0);
+    cnt = (int)bins[b0];
+    if (!by_mass) whole = d;
+    if (by_mass && d < 0.25 && b0 > 0) {
+      const int q = (int)bins[--b0];
+      before -= q;
+      cnt += q;
+    }
+    if (by_mass && d > 0.75) cnt += (int)bins[min(++b1, kFine - 1)];
+    cnt = uniform(cnt);
+    before = uniform(before);
+    return b1 < kFine - 1 && cnt <= kSorted;
+  }
+
+  // The cut after k words, and among these (k_on; else all words, which weigh about S, 0 where that is not known) after
+  // the share p of their weight; `least` is the row's least live word.  sums: rec.sum = the tiles' kept weights.  False where counts do not find it.
+  __device__ __forceinline__ bool fine_cut(float least, bool k_on, int k, bool p_on, double p, double S, bool exact, bool sums,
+                                           Cut& cut) {
+    // A count may end anywhere: the bins go down to the row's least live word.  Words lighter than 2^-32 of the first are
+    // not what a share depends on.
+    const double down = -t2(least) + 0.01, octave = (k_on ? down : fmin(down, 32.0)) / (kFine - 2);  // of a bin
+    const float cf = (float)(c / octave);
+    double whole = 0.0, Sk = S;
+    int r = 0;
+    count_fine(cf);
+#pragma unroll 1
+    for (int by_mass = !k_on; by_mass <= (int)p_on; ++by_mass) {
+      int b0, b1, before, cnt;
+      if (!find_fine(by_mass, k, (1.0 - p) * Sk, octave, whole, b0, b1, before, cnt)) return false;
+      uint32_t klo, khi;
+      keys_of(b0, b1, kLiveMin, [&](float z) { return fine_of(z, cf); }, klo, khi);
+      khi -= khi == kMinusZero;
+      const float lo = key_value(klo), hi = key_value(khi);
+      const bool total = by_mass && !k_on && !exact;
+      double all = 0.0;
+      const int n = total ? gather_and_sum<true>(lo, hi, all) : gather_and_sum<false>(lo, hi, all);
+      if (total) Sk = block_sum(all);
+      const double above = tile_sum(), target = p * Sk;
+      sort_words<false>(sh.h.some, sh.h.sorted, n);
+      scan_sorted(n, above);
+      if (by_mass) {
+        if (before > 0 && !(above < target)) return false;
+        r = first_reaching(n, target);
+        if (!(uniform(sh.h.cum[r - 1]) >= target)) return false;
+      } else {
+        r = k - before;
+      }
+      const unsigned long long last = sh.h.sorted[r - 1];
+      cut.thr = uniform(word_of(last));
+      cut.tie = uniform(index_of(last));
+      cut.mass = Sk = uniform(sh.h.cum[r - 1]);
+      cut.count = before + r;
+      __syncthreads();
+    }
+    if (sums) add_sorted(r);
+    return true;
+  }
+
   // The cut after the k-th word, or after the shortest prefix of weight `target`, among the words from x_lo up (all in the
   // list where listed >= 0), whose histogram<true> is made.  `sums`: rec.sum is wanted too, and true comes back in it where
   // it holds the tiles' kept weights.
@@ -961,28 +1119,8 @@ struct RowWork {
     const bool want = sums && listed < 0;
     sums = false;
     const int b = find_bin(by_mass, count0, mass0, k, target, cnt);
-    // the keys that fall into bin b: bin_of only falls as the key grows; each lane tries one of 64 between the ends
-    auto lowest = [&](int bin) {
-      uint32_t lo = order_key(x_lo), hi = order_key(m);
-      while (lo < hi) {
-        const uint32_t step = (hi - lo) / 64 + 1, key = lo + (threadIdx.x & 63) * step;
-        const uint64_t mask = __ballot(key >= hi || bin_of(key_value(key)) <= bin);
-        const uint32_t l = mask ? (uint32_t)__ffsll((unsigned long long)mask) - 1 : 64;
-        if (l < 64) hi = min(hi, lo + l * step);
-        if (l > 0) lo = lo + (l - 1) * step + 1;
-      }
-      return lo;
-    };
-    constexpr uint32_t kMinusZero = 0x7fffffffu;  // the key that no word has: -0 counts as 0
-    if (threadIdx.x < 64) {
-      const uint32_t from = lowest(b), to = b == 0 ? order_key(m) : lowest(b - 1) - 1;
-      if (threadIdx.x == 0) {
-        sh.key = from;
-        sh.key2 = to;
-      }
-    }
-    __syncthreads();
-    uint32_t klo = (uint32_t)uniform((int)sh.key), khi = (uint32_t)uniform((int)sh.key2);
+    uint32_t klo, khi;
+    keys_of(b, b, x_lo, [&](float z) { return bin_of(z); }, klo, khi);
     while (cnt > kSorted && klo < khi) {
       const int bits = 32 - __clz((int)(khi - klo));
       constexpr int kBinBits = 31 - __builtin_clz(kBins);
@@ -1024,7 +1162,8 @@ struct RowWork {
       __syncthreads();
       n = min(uniform(sh.n), kSorted);
     } else if (want) {
-      n = gather_and_sum(lo, hi);
+      double none = 0.0;
+      n = gather_and_sum<false>(lo, hi, none);
     } else {
       n = gather(sh.h.some, kSorted, lo, hi);
     }
@@ -1683,7 +1822,13 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
             }
           };
           bool summed = false;  // rec.sum holds the tiles' kept weights
-          if (k_on || p_on) {
+          Cut fine;
+          if ((k_on || p_on) && listed < 0 && w.fine_cut(lo, k_on, k, p_on, p, S, exact, DRAW, fine)) {
+            narrow(fine.thr, fine.tie);
+            S = fine.mass;
+            n = fine.count;
+            summed = DRAW;
+          } else if (k_on || p_on) {
             const bool sum_all = p_on && !k_on && !exact && listed < 0;  // S from the histogram: all live words
             if (sum_all) w.x_lo = x_lo = kLiveMin;
             double Sk = S;
