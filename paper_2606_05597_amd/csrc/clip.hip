@@ -119,6 +119,8 @@ __device__ __forceinline__ double unit_sumsq(P p, int n) {
   return s;
 }
 
+// HBM-bound, or by the memory-side cache where the gradients fit it: 545 M fp32 elements in 0.35 ms = 6.2 TB/s, 60 M in
+// 37 us = 6.6 TB/s; 24 small tensors in 3.7 us.
 __global__ __launch_bounds__(kClipNT) void k_grad_sumsq(const GradEntry* __restrict__ tab, int n_tab, int64_t units,
                                                         double* __restrict__ partials) {
   __shared__ double sh[kClipNT / 64];
@@ -172,6 +174,8 @@ __device__ __forceinline__ void unit_scale(Pi p, Po o, int n, float f) {
 
 // BIG: more gradients than the memory-side cache holds.  They are then taken from the last unit back, so that what the
 // sum of squares read last is still there, and past the caches otherwise; fewer are read from that cache as they lie.
+// Norm and clipping, both ways (us): 545 M elements, fp32 to bf16, 938 so and 955 in order through the caches (the clipping
+// 0.58 ms = 5.6 TB/s); 60 M 124 so and 99 in order (57 = 6.3 TB/s).
 template <bool BIG>
 __global__ __launch_bounds__(kClipNT) void k_grad_clip(const GradEntry* __restrict__ tab, int n_tab, int64_t units,
                                                        bool in_place, const double* __restrict__ partials,

@@ -19,10 +19,17 @@
 //                   as in the last case, in the list instead of the row;
 //   many, bf16      a count of each value (bf16 logits below 64 in size have 5,377 that are told apart); counts times weights,
 //                   summed from the top, give the cut, and a table of the values' weights the tiles' kept sums;
-//   many, else      histograms: words fall into kBins bins of 1/32 of a power of two of weight, each bin's count and weight
-//                   are summed, the bin that holds the cut is split again by the bits of its logits until at most kSorted
-//                   words (gathered and sorted) or one repeated value are left.
+//   many, else      counts by fine bins of weight say which bin holds the cut, and one more pass gathers that bin's words
+//                   and sums the words above them; where they do not (a value that repeats, one bin for many words),
+//                   histograms: words fall into kBins bins, each bin's count and weight are summed, the bin that holds the
+//                   cut is split again by the bits of its logits until at most kSorted words (gathered and sorted) or one
+//                   repeated value are left.
 // Histogram weights are integers (weight relative to the bin's top, in 2^-44), so that atomics in any order give one sum.
+//
+// A pass over a row by its own workgroup is bound by its instructions, not by memory: about 6 us for 32,003 fp32 words where
+// tiles are reduced or words counted, 13 us where each word's fp64 weight is summed, two rows on a CU (a CU's share of the
+// memory would bring them in 11 us for both).  The loops over a tile's vectors are rolled: unrolled, the kernel waits for its
+// own instructions.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <math.h>
@@ -357,7 +364,8 @@ __device__ __forceinline__ TileStats tile_stats(const Tile<Tin>& x, SumMode mode
   return s;
 }
 
-// The tiles of few rows, one wave each, spread over the whole chip.
+// The tiles of few rows, one wave each, spread over the whole chip.  bf16 [1, 151,936]: 4.5 us, a launch's latency; [64,
+// 151,936]: 14 us, bound by the fp64 weights of a row with nothing cut (19 MB: 3.5 us).
 template <typename Tin>
 __global__ __launch_bounds__(256) void k_sample_tiles(const RowArgs a, int n_waves, bool draw) {
   const int w = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -984,7 +992,9 @@ struct RowWork {
   // The row's words are counted by fine bins of weight.  Counts say exactly where the k-th word is.  For a weight, the
   // bins' counts times their middles say where the words below the cut, all lighter than it, weigh what is to be left out:
   // within a bin or so, since no heavy word adds to the error.  One pass then gathers these bins' words and sums the ones
-  // above them in fp64, and the cut is accepted if the sums confirm that it lies among them.
+  // above them in fp64, and the cut is accepted if the sums confirm that it lies among them.  A count is one 32-bit LDS
+  // atomic per word, a histogram's weight a 64-bit one besides, which bounds it (fp32 [500, 32,003], top-p 0.9, two rows on
+  // a CU: 6 us and 24 us for that pass; the whole call 62 us and 74 us).
 
   static constexpr int kFine = 2 * kBins * kCols;  // bins, in the histograms' memory
   __device__ __forceinline__ int fine_of(float z, float cf) const {
@@ -1067,7 +1077,8 @@ struct RowWork {
   }
 
   // The cut after k words, and among these (k_on; else all words, which weigh about S, 0 where that is not known) after
-  // the share p of their weight; `least` is the row's least live word.  sums: rec.sum = the tiles' kept weights.  False where counts do not find it.
+  // the share p of their weight; `least` is the row's least live word.  sums: rec.sum = the tiles' kept weights.  False
+  // where counts do not find it.
   __device__ __forceinline__ bool fine_cut(float least, bool k_on, int k, bool p_on, double p, double S, bool exact, bool sums,
                                            Cut& cut) {
     // A count may end anywhere: the bins go down to the row's least live word.  Words lighter than 2^-32 of the first are
@@ -1600,6 +1611,10 @@ __device__ __forceinline__ void write_row(const RowArgs& a, int t, grpo_sampling
   if (a.flags && flag) atomicOr(a.flags, flag);
 }
 
+// One workgroup per row.  FUSED: it reduces the row's tiles itself; else their records are there (split_now).  A few words to
+// look at: latency, a dozen steps between barriers (bf16 [1, 151,936], k = 50 with p = 0.95: 12.5 us after the tiles' 4.5);
+// many: the passes over the row (top-p 0.9: fp32 [500, 32,003] 62 us = 1.0 TB/s, bf16 [256, 151,936] 48 us = 1.6 TB/s; a
+// setting per row, log-probs: bf16 [2,000, 151,669] 0.19 ms = 3.1 TB/s).  128 VGPRs: two rows of 512 threads to a CU.
 template <typename Tin, bool FUSED, bool DRAW, int NT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_sample_row(const RowArgs a, int row0) {
   __shared__ RowShared<NT> sh;
@@ -1889,7 +1904,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
 
 // ---- log-probs of rows with nothing cut -------------------------------------------
 // One workgroup to a row, read once: a thread's 32 (bf16) or 16 weights at a time summed in fp32, relative to its running
-// maximum, and these sums in fp64.  HBM-bound.
+// maximum, and these sums in fp64.  HBM-bound: bf16 [8,000, 151,936] in 0.50 ms = 4.9 TB/s (the row kernel's own first pass
+// takes 0.51 ms for it), fp32 [192, 1,024] in 4.8 us.
 template <typename Tin>
 __global__ __launch_bounds__(256) void k_tempered_logp(const RowArgs a, int row0) {
   constexpr int NT = 256, NW = NT / 64, EPV = 16 / (int)sizeof(Tin), U = 4;
@@ -2004,7 +2020,8 @@ struct BwdArgs {
 constexpr int kBwdNT = 256, kBwdCols = 8192;
 
 // One workgroup to kBwdCols columns of a row, all loads in flight before the first store: a streaming pass, bound by
-// the 2 + 2 (bf16) or 4 + 4 bytes per word.
+// the 2 + 2 (bf16) or 4 + 4 bytes per word: bf16 [8,000, 151,936] in 0.82 ms = 5.9 TB/s, fp32 [3,001, 32,003], whose rows
+// start at any element, in 0.12 ms = 6.6 TB/s (the forward pass left part of it cached).
 template <typename Tin>
 __global__ __launch_bounds__(kBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_sampled_bwd(const BwdArgs a, int row0) {
   constexpr int EPV = 16 / (int)sizeof(Tin), U = kBwdCols / kBwdNT / EPV;
@@ -2130,9 +2147,10 @@ static void launch_row_kernel(const RowArgs& a, int64_t T, hipStream_t s) {
 // Whether rows go to workgroups of 256 threads, four on a CU, and not to ones of 512 or 1,024.  Up to 16,384 words a top-k
 // is found among the partial maxima that such a workgroup holds (us, 256 against 512 threads, bf16, k = 50 with p = 0.95:
 // V = 2,000 T = 4 12 and 13, T = 3,000 37 and 76; V = 16,384 T = 4 13 and 14, T = 3,000 49 and 85).  A top-p alone goes
-// through more of the row, which few rows do faster with more threads (V = 16,384, T = 200: bf16 44 and 29, fp32 43 and
-// 34) and many with more rows at once (T = 3,000: V = 2,048 bf16 57 and 104; V = 8,000 bf16 103 and 128; V = 16,384
-// fp32 144 and 177), but for bf16 rows beyond 8,192 words, whose values the large workgroup counts (141 and 120).
+// through more of the row, which few rows do faster with more threads (V = 16,384, T = 200: bf16 35 and 29, fp32 34 and
+// 30) and many with more rows at once (T = 3,000: V = 2,048 bf16 56 and 104; V = 8,000 bf16 90 and 127; V = 16,384 fp32
+// 118 and 161), but for bf16 rows beyond 8,192 words, whose values the large workgroup counts (126 and 120; T = 600 60 and
+// 39).
 template <typename Tin>
 static bool short_rows(const RowArgs& a, int64_t T) {
   if (a.V > RowShape<256>::kMaxWords) return false;
@@ -2149,9 +2167,9 @@ static bool nothing_cut(const grpo_sampling& p, int V) {
 // Whether the tiles are reduced by a launch of their own, which spreads a row over the chip but lets the row's workgroup
 // see each tile's record alone.  Where nothing is cut that is all it needs (us, two launches against one: V = 17,000
 // bf16 T = 1 14 and 15; V = 152,064 T = 1 13 and 38, T = 64 21 and 39, T = 191 36 and 41).  A cut reads the row again:
-// two launches pay for the longest of few rows (fp32 top-p: V = 50,000 T = 64 62 and 60; V = 152,064 T = 1 130 and 141,
-// T = 191 164 and 150; bf16 k = 50 with p = 0.95: T = 1 17 and 21, T = 128 25 and 24), and not for a bf16 row with a top-p
-// alone, which one launch counts by value as it reads it first (T = 1 49 and 43, T = 64 57 and 44).
+// two launches pay for the longest of few rows (fp32 top-p: V = 50,000 T = 64 51 and 48; V = 152,064 T = 1 89 and 93,
+// T = 191 123 and 110; bf16 k = 50 with p = 0.95: T = 1 17 and 21, T = 128 25 and 24), and not for a bf16 row with a top-p
+// alone, which one launch counts by value as it reads it first (T = 1 49 and 43, T = 64 60 and 44).
 template <typename Tin>
 static bool split_now(const RowArgs& a, int64_t T) {
   const grpo_sampling& p = a.par;
@@ -2173,9 +2191,9 @@ static void launch_rows(const RowArgs& a, int64_t T, hipStream_t s) {
                          (int)r);
   } else if (short_rows<Tin>(a, T)) {
     launch_row_kernel<Tin, true, DRAW, 256>(a, T, s);
-  } else if (a.V > RowShape<256>::kMaxWords && T <= 256) {
-    // one row per CU: all its waves for that row (us, 1,024 against 512 threads, top-p alone: V = 152,064 T = 256 bf16 48 and
-    // 54, fp32 157 and 186; T = 400 bf16 89 and 77, fp32 283 and 265; T = 1,500 bf16 251 and 198)
+  } else if (T <= 256 && (a.V > RowShape<256>::kMaxWords || sizeof(Tin) == 2)) {
+    // one row per CU: all its waves for that row (us, 1,024 against 512 threads, top-p alone: V = 8,000 T = 200 bf16 25 and
+    // 30, fp32 35 and 32; V = 152,064 T = 191 bf16 48 and 53, fp32 111 and 141; T = 400 bf16 93 and 77, fp32 212 and 194)
     launch_row_kernel<Tin, true, DRAW, 1024>(a, T, s);
   } else {
     launch_row_kernel<Tin, true, DRAW, 512>(a, T, s);
