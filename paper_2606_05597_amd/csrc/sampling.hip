@@ -1837,11 +1837,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void
             }
           };
           bool summed = false;  // rec.sum holds the tiles' kept weights
-          Cut fine;
-          if ((k_on || p_on) && listed < 0 && w.fine_cut(lo, k_on, k, p_on, p, S, exact, DRAW, fine)) {
-            narrow(fine.thr, fine.tie);
-            S = fine.mass;
-            n = fine.count;
+          Cut by_counts;
+          if ((k_on || p_on) && listed < 0 && w.fine_cut(lo, k_on, k, p_on, p, S, exact, DRAW, by_counts)) {
+            narrow(by_counts.thr, by_counts.tie);
+            S = by_counts.mass;
+            n = by_counts.count;
             summed = DRAW;
           } else if (k_on || p_on) {
             const bool sum_all = p_on && !k_on && !exact && listed < 0;  // S from the histogram: all live words

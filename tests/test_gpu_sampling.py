@@ -156,6 +156,26 @@ def test_rows_of_every_launch(T, V, dtype):
         check(logits, z, par, uniform(z, par, V + i), V)
 
 
+@pytest.mark.parametrize("T,V,dtype", [(3, 9001, F32), (3, 20011, F32), (260, 17001, F32), (3, 9001, BF16), (3, 80000, F32)],
+                         ids=str)
+def test_cuts_among_many_words(T, V, dtype):
+    """Cuts anywhere in a row: next to its end, below an outlier that takes nearly all bins of weight, beside one heavy
+    word, at temperatures that leave all weights alike or far apart."""
+    rng = np.random.default_rng(V)
+    z = rng.normal(0, 2, (T, V))
+    z[0, 7] = -9e7
+    z[1] = np.where(np.arange(V) % 3 == 0, z[1], -np.inf)
+    z[2, 11] = np.log(9 * np.exp(np.delete(z[2], 11)).sum()) + 1e-4  # a share of 0.9
+    x = torch.from_numpy(z).to(dtype)
+    z = x.double().numpy()
+    live = int((z[1] > -1e8).sum())
+    for par in (dict(top_k=V - 1), dict(top_k=V // 2, top_p=0.7), dict(top_k=live - 1, top_p=0.9999), dict(top_p=0.9),
+                dict(top_p=1 - 2.0**-24), dict(top_p=1e-30, top_k=V // 2), dict(top_p=0.0), dict(top_p=0.98, temperature=1e6),
+                dict(top_k=V // 3, top_p=0.95, temperature=1e6), dict(top_k=V // 3, top_p=0.95, temperature=0.01),
+                dict(top_k=V // 2, temperature=1e-6), dict(top_p=0.9999, temperature=30.0, min_p=0.7)):
+        check(x.cuda(), z, par, uniform(z, par, V, [0.0, 0.999, 0.9]), V)
+
+
 @pytest.mark.parametrize("T,V", [(191, 20000), (192, 20000), (200, 2500)])
 def test_own_settings_per_row(T, V):
     rng = np.random.default_rng(T)
