@@ -157,6 +157,7 @@ class SampledLogp(torch.autograd.Function):
     def backward(ctx, grad_output):
         logits, actions, rows = ctx.saved_tensors
         padded = ctx.V is not None and ctx.V < logits.shape[1]
-        dlogits = torch.zeros_like(logits) if padded else True
+        dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype,
+                                      device=logits.device).zero_() if padded else True
         d = grpo_sampled_logp_bwd(logits, actions, rows, grad_output.contiguous(), V=ctx.V, dlogits=dlogits)
         return d, None, None

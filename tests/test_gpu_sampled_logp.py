@@ -224,3 +224,19 @@ def test_graph_replays():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(d, want[0]) and torch.equal(lp, want[1]), rep
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_autograd_of_padded_columns_in_wider_rows(dtype):
+    T, cols, V, ld = 5, 700, 650, 800
+    buf = torch.randn((T, ld), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(dtype)
+    act = torch.arange(T, dtype=torch.int32, device="cuda") * 100
+    g = torch.rand(T, device="cuda") + 0.5
+
+    def grad(x):
+        x = x.detach().requires_grad_()
+        grpo.SampledLogp.apply(x, act, dict(temperature=0.7, top_k=60, V=V)).backward(g)
+        return x.grad
+
+    strided, packed = grad(buf[:, :cols]), grad(buf[:, :cols].contiguous())
+    assert torch.equal(strided, packed) and (strided[:, V:] == 0).all() and (strided[:, :V] != 0).any()
