@@ -233,10 +233,15 @@ def test_autograd_of_padded_columns_in_wider_rows(dtype):
     act = torch.arange(T, dtype=torch.int32, device="cuda") * 100
     g = torch.rand(T, device="cuda") + 0.5
 
-    def grad(x):
-        x = x.detach().requires_grad_()
-        grpo.SampledLogp.apply(x, act, dict(temperature=0.7, top_k=60, V=V)).backward(g)
-        return x.grad
+    for par in (dict(temperature=0.7, top_k=60), dict(temperature=0.7)):
 
-    strided, packed = grad(buf[:, :cols]), grad(buf[:, :cols].contiguous())
-    assert torch.equal(strided, packed) and (strided[:, V:] == 0).all() and (strided[:, :V] != 0).any()
+        def grad(x):
+            x = x.detach().requires_grad_()
+            logp = grpo.SampledLogp.apply(x, act, dict(par, V=V))
+            logp.backward(g)
+            return x.grad, torch.isfinite(logp.detach())
+
+        (strided, kept), (packed, _) = grad(buf[:, :cols]), grad(buf[:, :cols].contiguous())
+        assert torch.equal(strided, packed) and (strided[:, V:] == 0).all()
+        # rows whose action is not kept have no gradient; with nothing cut every row has one
+        assert torch.equal((strided[:, :V] != 0).any(1), kept) and (kept.all() or "top_k" in par)
