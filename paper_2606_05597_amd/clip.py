@@ -56,12 +56,16 @@ class GradList:
         _check(lib.grpo_grad_table(recs, n, table.data_ptr(), size, ctypes.byref(self._layout)), "grpo_grad_table")
         self._places = [s.data_ptr() for s in self._storages]
         self._table = table.to(self.device)
+        self._stream = torch._C._cuda_getCurrentRawStream(self.device.index)  # the stream that the table's memory belongs to
         self._c_args = ctypes.byref(self._layout), self._table.data_ptr()
 
     def __len__(self):
         return int(self._layout.n)
 
-    def _args(self):
+    def _args(self, s):
+        """The library's arguments for a call on the raw stream s, the device's current one."""
+        if s != self._stream:  # the list may go before that stream is done with its table
+            self._table.record_stream(torch.cuda.current_stream(self.device))
         if [s.data_ptr() for s in self._storages] != self._places:
             raise ValueError("the memory of a tensor in the list has moved since the list was made")
         return self._c_args
@@ -92,13 +96,13 @@ def _flags(error_flags, device):
 def _sumsq(grads, partials, s):
     if partials is None:
         partials = torch.empty(GRPO_GRAD_PARTIALS, dtype=torch.float64, device=grads.device)
-    _check(_lib.load().grpo_grad_sumsq(*grads._args(), partials.data_ptr(), s), "grpo_grad_sumsq")
+    _check(_lib.load().grpo_grad_sumsq(*grads._args(s), partials.data_ptr(), s), "grpo_grad_sumsq")
     return partials
 
 
 def _clip(grads, partials, max_norm, error_flags, s):
     norm = torch.empty((), dtype=torch.float32, device=grads.device)
-    st = _lib.load().grpo_grad_clip(*grads._args(), partials.data_ptr(), float(max_norm), norm.data_ptr(),
+    st = _lib.load().grpo_grad_clip(*grads._args(s), partials.data_ptr(), float(max_norm), norm.data_ptr(),
                                     _at(error_flags), s)
     _check(st, "grpo_grad_clip")
     return norm

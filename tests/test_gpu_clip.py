@@ -208,3 +208,26 @@ def test_graph_replays():
         gr.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out + [norm], want)), rep
+
+
+def test_table_stays_until_another_stream_is_done_with_it():
+    """Lists that the calls make for themselves, used on a stream that is still busy when they go."""
+    n = 300
+    g = [torch.full((50 + i,), 0.25, device="cuda") for i in range(n)]
+    want = (sum(x.numel() for x in g) * 0.0625) ** 0.5
+    table_bytes = 40 * n
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        x = torch.ones(4096, 4096, device="cuda")
+        for _ in range(20):
+            x = (x @ x).mul_(1 / 4096)
+    held = []
+    norm = grpo.grpo_clip_grad_norm_(g, 1e9, stream=side)
+    for _ in range(20):
+        held.append(torch.full((table_bytes,), 0, dtype=torch.uint8, device="cuda"))
+    partials = grpo.grpo_grad_sumsq(g, stream=side)
+    held.append(torch.full((table_bytes,), 0, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    assert abs(norm.item() - want) <= 2.0**-24 * want
+    assert abs(partials.sum().item() ** 0.5 - want) <= 1e-12 * want
