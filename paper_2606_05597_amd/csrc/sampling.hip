@@ -1614,7 +1614,8 @@ __device__ __forceinline__ void write_row(const RowArgs& a, int t, grpo_sampling
 // One workgroup per row.  FUSED: it reduces the row's tiles itself; else their records are there (split_now).  A few words to
 // look at: latency, a dozen steps between barriers (bf16 [1, 151,936], k = 50 with p = 0.95: 12.5 us after the tiles' 4.5);
 // many: the passes over the row (top-p 0.9: fp32 [500, 32,003] 62 us = 1.0 TB/s, bf16 [256, 151,936] 48 us = 1.6 TB/s; a
-// setting per row, log-probs: bf16 [2,000, 151,669] 0.19 ms = 3.1 TB/s).  128 VGPRs: two rows of 512 threads to a CU.
+// setting per row, log-probs: bf16 [2,000, 151,669] 0.19 ms = 3.1 TB/s).  128 VGPRs, for two rows of 512
+// threads to a CU, at the price of 7 to 47 of a thread's values in scratch.
 template <typename Tin, bool FUSED, bool DRAW, int NT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_sample_row(const RowArgs a, int row0) {
   __shared__ RowShared<NT> sh;
@@ -2020,7 +2021,7 @@ struct BwdArgs {
 constexpr int kBwdNT = 256, kBwdCols = 8192;
 
 // One workgroup to kBwdCols columns of a row, all loads in flight before the first store: a streaming pass, bound by
-// the 2 + 2 (bf16) or 4 + 4 bytes per word: bf16 [8,000, 151,936] in 0.82 ms = 5.9 TB/s, fp32 [3,001, 32,003], whose rows
+// the 2 + 2 (bf16) or 4 + 4 bytes per word: bf16 [8,000, 151,936] in 0.82-0.86 ms = 5.7-5.9 TB/s, fp32 [3,001, 32,003], whose rows
 // start at any element, in 0.12 ms = 6.6 TB/s (the forward pass left part of it cached).
 template <typename Tin>
 __global__ __launch_bounds__(kBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_sampled_bwd(const BwdArgs a, int row0) {
