@@ -24,7 +24,8 @@
 //                   histograms: words fall into kBins bins, each bin's count and weight are summed, the bin that holds the
 //                   cut is split again by the bits of its logits until at most kSorted words (gathered and sorted) or one
 //                   repeated value are left.
-// Histogram weights are integers (weight relative to the bin's top, in 2^-44), so that atomics in any order give one sum.
+// Histogram weights are integers (weight relative to the bin's top, in 2^-42 or finer), so that atomics in any order give one
+// sum.
 //
 // A pass over a row by its own workgroup is bound by its instructions, not by memory: about 6 us for 32,003 fp32 words where
 // tiles are reduced or words counted, 13 us where each word's fp64 weight is summed, two rows on a CU (a CU's share of the
@@ -54,11 +55,13 @@ struct RowShape {
   static constexpr int kSorted = 256;    // words that are sorted
   static constexpr int kBins = 1024, kCols = 2;  // bins of 32 to a power of two of weight, each in kCols copies
   static constexpr int kMaxWords = GRPO_SAMPLING_MAX_V;
+  static constexpr int kUnitBits = 42;  // a bin's weights are in 2^-kUnitBits
   static constexpr bool kValueTable = true;  // room for the counts of bf16 values
 };
 template <>
 struct RowShape<256> {
   static constexpr int kMaxSubs = 1024, kCap = 1024, kSorted = 256, kBins = 512, kCols = 1, kMaxWords = 16384;
+  static constexpr int kUnitBits = 44;
   static constexpr bool kValueTable = false;
 };
 constexpr int kMaxNW = 16;
@@ -772,7 +775,13 @@ struct RowWork {
   __device__ __forceinline__ double steps(float z) const { return ((double)m - (double)z) * (c * kPerOctave); }
   __device__ __forceinline__ int bin_of(float z) const { return (int)fmin(steps(z), (double)(kBins - 1)); }
 
-  // The low bits of y in [1, 2) or [256, 512): of 256 + w, a weight w <= 1 in 2^-44.
+  // A bin's weights are summed in 64 bits, in each copy half the row's words at most (lanes of one parity): 2^21 of weight
+  // 1 in 2^-42 are 2^63.  Rounding to 2^-42 is off by 1.2e-13 of a word's weight at most (2^-43 of 2^(-1/32)).
+  static constexpr int kUnitBits = Shape::kUnitBits;
+  static_assert((uint64_t)(Shape::kMaxWords / kCols) <= 1ull << (63 - kUnitBits), "a bin that holds all words");
+  static constexpr double kOver = (double)(1ull << (52 - kUnitBits));  // kOver + w: w in the low bits, in 2^-kUnitBits
+
+  // The low bits of y in [1, 2) or [kOver, 2 kOver).
   __device__ __forceinline__ static unsigned long long fixed(double y) {
     return __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull;
   }
@@ -805,9 +814,9 @@ struct RowWork {
           y = fma(x, y, -1.6938507235263203e-06);
           y = fma(x, y, 0.00023459619814393515);
           y = fma(x, y, -0.021660849392493294);
-          y = fma(x, y, 257.0);
+          y = fma(x, y, 1.0 + kOver);
         } else {
-          y = exp2_neg(x * (-1.0 / kPerOctave)) + 256.0;
+          y = exp2_neg(x * (-1.0 / kPerOctave)) + kOver;
         }
         if (b == kBins - 1) {
           const double r = exp2_neg(x * (-1.0 / kPerOctave));
@@ -816,11 +825,11 @@ struct RowWork {
             rest_mass += r;
             return;
           }
-          y = r + 256.0;
+          y = r + kOver;
         }
       } else {
         b = min((int)((top - order_key(z)) >> shift), kBins - 1);
-        y = exp2_neg(fmin(t2(z) - t_top, 0.0)) + 256.0;
+        y = exp2_neg(fmin(t2(z) - t_top, 0.0)) + kOver;
       }
       atomicAdd(&sh.h.mass[b * kCols + copy], fixed(y));
       atomicAdd(&sh.h.count[b * kCols + copy], 1u);
@@ -850,7 +859,7 @@ struct RowWork {
       double mass = 0.0;
 #pragma unroll
       for (int i = 0; i < kCols; ++i) {
-        mass += (double)sh.h.mass[b * kCols + i] * 0x1p-44;
+        mass += (double)sh.h.mass[b * kCols + i] * (1.0 / (double)(1ull << kUnitBits));
         count += (int)sh.h.count[b * kCols + i];
       }
       if (TOP && b == kBins - 1) {
