@@ -423,11 +423,16 @@ struct Cut {
   int count;
 };
 
+constexpr int kMidSums = 8;
+static_assert(GRPO_SAMPLING_MAX_V / kMidSums <= 1 << 19, "the words of bin kMid");
+
 template <bool TABLE>
 struct ValueTable {
   double weight[kValues];
   uint32_t count[kValues];
-  unsigned long long mid;  // the weight of the words of bin kMid, in 2^-44 of the next bin's
+  // The weight of the words of bin kMid, in 2^-44 of the next bin's: eight sums, each over the words of every eighth
+  // lane, 2^19 of a row at most and so 2^63.
+  unsigned long long mid[kMidSums];
 };
 template <>
 struct ValueTable<false> {};
@@ -1296,7 +1301,7 @@ struct RowWork {
 
   __device__ __forceinline__ void clear_values() const {
     for (int i = threadIdx.x; i < kValues; i += NT) sh.v.count[i] = 0u;
-    if (threadIdx.x == 0) sh.v.mid = 0ull;
+    if (threadIdx.x < kMidSums) sh.v.mid[threadIdx.x] = 0ull;
     __syncthreads();
   }
 
@@ -1313,7 +1318,7 @@ struct RowWork {
       }
     each_mid(x, least, [&](float z) {
       const double y = exp2_neg(((double)z - (double)bin_value(kMid + 1)) * c) + 256.0;
-      atomicAdd(&sh.v.mid, __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
+      atomicAdd(&sh.v.mid[threadIdx.x & (kMidSums - 1)], __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
     });
   }
 
@@ -1329,7 +1334,10 @@ struct RowWork {
     const int tid = threadIdx.x;
     const double mid_top = t2(bin_value(kMid + 1));
     // each thread kEach bins, from the largest value down; the last one holds the masked words
-    const double mid = (double)sh.v.mid * 0x1p-44 * exp2_neg(mid_top);
+    double mid = 0.0;
+#pragma unroll
+    for (int i = 0; i < kMidSums; ++i) mid += (double)sh.v.mid[i];
+    mid *= 0x1p-44 * exp2_neg(mid_top);
     auto bin_at = [&](int i) { return kValues - 1 - (tid * kEach + i); };
     int q[kEach], my_n = 0;
     double w[kEach], my_m = 0.0;  // counts, weights of the bins

@@ -24,6 +24,8 @@ def row(kind, V):
         return np.where(np.arange(V) % 4 == 1, 4.0, 5.0)[None]
     if kind == "close":  # words of one bin, told apart
         return rng.normal(0, 1e-3, (1, V))
+    if kind == "above_zero":  # three words in four at zero, the others likelier
+        return np.where(np.arange(V) % 4 == 1, 1.0, 0.0)[None]
     raise AssertionError(kind)
 
 
@@ -62,3 +64,13 @@ def test_many_such_rows(kind):
     got = grpo.grpo_sample(rows, torch.from_numpy(u).cuda().expand(T).contiguous(), **par)
     for a, b in zip(got, want):
         assert (a == b).all()
+
+
+@pytest.mark.parametrize("V", [1 << 21, MOST - 3, MOST])
+def test_many_zeros_below_the_cut(V):
+    """bf16 words too small to be told apart are weighed together; the cut is among likelier ones, or takes them all."""
+    logits, z = on_gpu(row("above_zero", V), BF16)
+    for par in (dict(top_p=0.4), dict(min_p=0.3), dict(top_p=0.3, min_p=0.2, temperature=2.0),
+                dict(top_k=V // 5, top_p=0.7)):
+        check(logits, z, par, uniform(z, par, 1), V)
+        check_logp(logits, z, par, actions(z, par, 2), V)
