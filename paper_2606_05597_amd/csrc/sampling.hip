@@ -1337,7 +1337,9 @@ struct RowWork {
     double mid = 0.0;
 #pragma unroll
     for (int i = 0; i < kMidSums; ++i) mid += (double)sh.v.mid[i];
-    mid *= 0x1p-44 * exp2_neg(mid_top);
+    // Without such words the maximum may lie far below them, and their bin's weight beyond the range of exp2_neg.  With
+    // one, the maximum is above -2^-15: 2^89 at most, which exp2_neg forms as well.
+    if (mid > 0.0) mid *= 0x1p-44 * exp2_neg(mid_top);
     auto bin_at = [&](int i) { return kValues - 1 - (tid * kEach + i); };
     int q[kEach], my_n = 0;
     double w[kEach], my_m = 0.0;  // counts, weights of the bins
