@@ -69,7 +69,7 @@ int grpo_grad_sumsq(const grpo_grad_layout* layout, const void* table, double* p
 /*
  * The norm from the slots, and every gradient times f, formed in fp32 and rounded once to its out's type.
  *   max_norm     >= 0 (+inf: nothing is scaled)
- *   norm_out     device fp32 [1] or NULL: the norm
+ *   norm_out     device fp32 [1] or NULL: the norm (+inf beyond fp32's range: f is formed from the fp64 norm)
  *   error_flags  device int32 [1] or NULL: overwritten with GRPO_FLAG_NONFINITE when the norm is not finite
  * A norm that is not finite leaves f at 1: the gradients are as they were, and norm_out says that the step is to be
  * skipped.  Where f = 1, gradients clipped in place are not touched.

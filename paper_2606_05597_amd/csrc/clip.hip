@@ -143,8 +143,22 @@ __global__ __launch_bounds__(kClipNT) void k_grad_sumsq(const GradEntry* __restr
     partials[i] = 0.0;
 }
 
+// A factor f 2^e: e is 0 but for factors near fp32's subnormals, which hold fewer bits than the products do.
+struct Factor {
+  float f;
+  int e;
+  __device__ __forceinline__ bool is_one() const { return f == 1.f && e == 0; }
+};
+__device__ __forceinline__ float operator*(float x, Factor k) { return __builtin_amdgcn_ldexpf(x * k.f, k.e); }
+__device__ __forceinline__ Factor factor_of(double f) {
+  if (f >= 0x1p-100 || f == 0.0) return Factor{(float)f, 0};
+  int e;
+  const double r = frexp(f, &e);  // [1/2, 1)
+  return Factor{(float)r, e};
+}
+
 template <bool STREAM, typename Pi, typename Po>
-__device__ __forceinline__ void unit_scale(Pi p, Po o, int n, float f) {
+__device__ __forceinline__ void unit_scale(Pi p, Po o, int n, Factor f) {
   const int tid = threadIdx.x, nv = n / 8;
   float x[kVecs][8];
   if (n == kUnit) {
@@ -153,7 +167,7 @@ __device__ __forceinline__ void unit_scale(Pi p, Po o, int n, float f) {
 #pragma unroll
     for (int q = 0; q < kVecs; ++q) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[q][e] *= f;
+      for (int e = 0; e < 8; ++e) x[q][e] = x[q][e] * f;
       store8(o + (q * kClipNT + tid) * 8, x[q]);
     }
     return;
@@ -166,7 +180,7 @@ __device__ __forceinline__ void unit_scale(Pi p, Po o, int n, float f) {
   for (int q = 0; q < kVecs; ++q)
     if (q * kClipNT + tid < nv) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[q][e] *= f;
+      for (int e = 0; e < 8; ++e) x[q][e] = x[q][e] * f;
       store8(o + (q * kClipNT + tid) * 8, x[q]);
     }
   if (tid < n - nv * 8) store1(o + nv * 8 + tid, edge * f);
@@ -191,18 +205,18 @@ __global__ __launch_bounds__(kClipNT) void k_grad_clip(const GradEntry* __restri
   __syncthreads();
   const double norm = sqrt((sh[0] + sh[1]) + (sh[2] + sh[3]));
   const bool finite = isfinite(norm);
-  const float f = finite ? (float)fmin(1.0, max_norm / (norm + GRPO_CLIP_EPS)) : 1.f;
+  const Factor f = factor_of(finite ? fmin(1.0, max_norm / (norm + GRPO_CLIP_EPS)) : 1.0);
   if (blockIdx.x == 0 && tid == 0) {
     if (norm_out) *norm_out = (float)norm;
     if (flags) *flags = finite ? 0 : GRPO_FLAG_NONFINITE;
   }
-  if (in_place && f == 1.f) return;
+  if (in_place && f.is_one()) return;
   for (int64_t v = blockIdx.x; v < units; v += gridDim.x) {
     const int64_t u = BIG ? units - 1 - v : v;
     const GradEntry e = tab[entry_of(tab, 0, n_tab, u)];
     const int64_t first = (u - e.unit0) * kUnit;
     const int n = (int)min((int64_t)kUnit, e.n - first);
-    if (e.data == e.out && f == 1.f) continue;
+    if (e.data == e.out && f.is_one()) continue;
     if (e.dtype == GRPO_F32) {
       if (e.out_dtype == GRPO_F32) unit_scale<BIG>((gf32)e.data + first, (gf32o)e.out + first, n, f);
       else unit_scale<BIG>((gf32)e.data + first, (gbf16o)e.out + first, n, f);
