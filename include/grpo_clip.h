@@ -38,6 +38,7 @@ typedef struct {
   int32_t n;        /* tensors in it                                      */
   int32_t in_place; /* 1 where every out is its data                      */
   int64_t units;    /* pieces of work, each of at most 8192 elements      */
+  int64_t bytes;    /* of all data                                        */
 } grpo_grad_layout;
 
 /* Bytes of the table of n tensors, 0 for n < 0 or n > 2^20. */

@@ -62,7 +62,8 @@ class Grad(ctypes.Structure):
 
 
 class GradLayout(ctypes.Structure):
-    _fields_ = [("n", ctypes.c_int32), ("in_place", ctypes.c_int32), ("units", ctypes.c_int64)]
+    _fields_ = [("n", ctypes.c_int32), ("in_place", ctypes.c_int32), ("units", ctypes.c_int64),
+                ("bytes", ctypes.c_int64)]
 
 
 class GrpoError(RuntimeError):

@@ -186,10 +186,11 @@ __device__ __forceinline__ void unit_scale(Pi p, Po o, int n, Factor f) {
   if (tid < n - nv * 8) store1(o + nv * 8 + tid, edge * f);
 }
 
-// BIG: more gradients than the memory-side cache holds.  They are then taken from the last unit back, so that what the
-// sum of squares read last is still there, and past the caches otherwise; fewer are read from that cache as they lie.
+// BIG: more bytes of gradients than the memory-side cache holds.  They are then taken from the last unit back, so that what
+// the sum of squares read last is still there, and past the caches otherwise; fewer are read from that cache as they lie.
 // Norm and clipping, both ways (us): 545 M elements, fp32 to bf16, 938 so and 955 in order through the caches (the clipping
-// 0.58 ms = 5.6 TB/s); 60 M 124 so and 99 in order (57 = 6.3 TB/s).
+// 0.58 ms = 5.6 TB/s); in place, 160 MB of fp32 84 and 76, 264 MB 136 and 120, 320 MB 165 and 174, 480 MB 254 and 286; of
+// bf16 160 MB 77 and 73, 268 MB 127 and 120, 300 MB 139 and 141, 400 MB 184 and 223.
 template <bool BIG>
 __global__ __launch_bounds__(kClipNT) void k_grad_clip(const GradEntry* __restrict__ tab, int n_tab, int64_t units,
                                                        bool in_place, const double* __restrict__ partials,
@@ -234,7 +235,7 @@ static unsigned clip_grid(int64_t units) { return (unsigned)std::max<int64_t>(1,
 
 static int check_layout(const grpo_grad_layout* l, const void* table, const double* partials) {
   if (!l || !partials || l->n < 0 || l->n > kMaxGrads || l->units < 0 || l->units >= ((int64_t)1 << 31) ||
-      (l->n > 0 && !table) || (l->n == 0 && l->units > 0))
+      l->bytes < 0 || (l->n > 0 && !table) || (l->n == 0 && l->units > 0))
     return GRPO_ERR_ARG;
   if (!aligned(table, 8) || !aligned(partials, 8)) return GRPO_ERR_ALIGN;
   return GRPO_OK;
@@ -262,7 +263,7 @@ extern "C" int grpo_grad_table(const grpo_grad* grads, int32_t n, void* table, s
   Range* ranges = new (std::nothrow) Range[2 * (size_t)std::max(n, 1)];
   if (!ranges) return GRPO_ERR_WORKSPACE;
   GradEntry* tab = static_cast<GradEntry*>(table);
-  int64_t unit = 0;
+  int64_t unit = 0, bytes = 0;
   int32_t in_place = 1;
   size_t nr = 0;
   int st = GRPO_OK;
@@ -279,6 +280,7 @@ extern "C" int grpo_grad_table(const grpo_grad* grads, int32_t n, void* table, s
       if (g.n > 0 && (!aligned(g.data, a) || !aligned(g.out, b))) st = GRPO_ERR_ALIGN;
       tab[i] = GradEntry{g.data, g.out, g.n, unit, g.dtype, g.out_dtype};
       unit += (g.n + kUnit - 1) / kUnit;
+      bytes += g.n * (int64_t)a;
       if (unit >= ((int64_t)1 << 31)) st = GRPO_ERR_SHAPE;
       if (g.n > 0) {
         const uintptr_t d = (uintptr_t)g.data, o = (uintptr_t)g.out;
@@ -304,6 +306,7 @@ extern "C" int grpo_grad_table(const grpo_grad* grads, int32_t n, void* table, s
   layout->n = n;
   layout->in_place = in_place;
   layout->units = unit;
+  layout->bytes = bytes;
   return GRPO_OK;
 }
 
@@ -321,7 +324,7 @@ extern "C" int grpo_grad_clip(const grpo_grad_layout* layout, const void* table,
   if (st != GRPO_OK) return st;
   if (!(max_norm >= 0.0)) return GRPO_ERR_ARG;
   if (!aligned(norm_out, 4) || !aligned(error_flags, 4)) return GRPO_ERR_ALIGN;
-  const auto kernel = layout->units * kUnit * 4 > kCacheBytes ? k_grad_clip<true> : k_grad_clip<false>;
+  const auto kernel = layout->bytes > kCacheBytes ? k_grad_clip<true> : k_grad_clip<false>;
   hipLaunchKernelGGL(kernel, dim3(clip_grid(layout->units)), dim3(kClipNT), 0, s, static_cast<const GradEntry*>(table),
                      layout->n, layout->units, layout->in_place != 0, partials, max_norm, norm_out, error_flags);
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
