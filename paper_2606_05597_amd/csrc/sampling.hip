@@ -1034,10 +1034,11 @@ struct RowWork {
     __syncthreads();
   }
 
-  // The bins b0 .. b1 that hold the k-th word, or the word with what weighs `left_out` below it among the words that weigh
-  // `whole` by the middles of their bins (0: all of them); the words before them and in them.  By k, `whole` comes back as
-  // what the first k words weigh.  False where the cut is below the counted bins or too many words are in these.
-  __device__ __forceinline__ bool find_fine(bool by_mass, int k, double left_out, double octave, double& whole, int& b0,
+  // The bins b0 .. b1 that hold the k-th word, or the word with the share `out` of the weight S (0: of `whole`) below it among
+  // the words that weigh `whole` by the middles of their bins (0: all of them); the words before them and in them.  By k,
+  // `whole` comes back as what the first k words weigh.  False where the cut is below the counted bins or too many words
+  // are in these.
+  __device__ __forceinline__ bool find_fine(bool by_mass, int k, double out, double S, double octave, double& whole, int& b0,
                                             int& b1, int& before, int& cnt) {
     constexpr int kEach = kFine / NT;
     const uint32_t* bins = reinterpret_cast<const uint32_t*>(sh.h.mass);
@@ -1054,7 +1055,7 @@ struct RowWork {
     const int mine = n;
     const double my_e = e;
     block_scan(n, e, all_n, all_e);
-    const double target = (whole > 0.0 ? whole : all_e) - left_out;
+    const double among = whole > 0.0 ? whole : all_e, target = among - out * (S > 0.0 ? S : among);
     const int at = block_min(mine > 0 && (by_mass ? e >= target : n >= k) ? tid : INT_MAX);
     if (at == INT_MAX) return false;
     if (tid == at) {
@@ -1105,7 +1106,7 @@ struct RowWork {
 #pragma unroll 1
     for (int by_mass = !k_on; by_mass <= (int)p_on; ++by_mass) {
       int b0, b1, before, cnt;
-      if (!find_fine(by_mass, k, (1.0 - p) * Sk, octave, whole, b0, b1, before, cnt)) return false;
+      if (!find_fine(by_mass, k, 1.0 - p, Sk, octave, whole, b0, b1, before, cnt)) return false;
       uint32_t klo, khi;
       keys_of(b0, b1, kLiveMin, [&](float z) { return fine_of(z, cf); }, klo, khi);
       khi -= khi == kMinusZero;
