@@ -139,15 +139,17 @@ class SampledLogp(torch.autograd.Function):
 
     The log-probs (fp32 [T]) of given actions under the rollout's sampling distribution, for objectives of the caller's
     own: logits [T, V] (bf16 or fp32, on the GPU), ``opts`` a dict of the keyword options of ``grpo_sampled_logp``
-    (temperature, top_k, top_p, min_p, V, error_flags, workspace).  backward reads the logits again and writes their gradient
-    (``grpo_sampled_logp_bwd``; zero in columns past V); the kept set is a constant.  An action that is not kept has
-    log-prob -inf and no gradient.
+    (temperature, top_k, top_p, min_p, V, error_flags, workspace, stream).  backward reads the logits again and writes
+    their gradient (``grpo_sampled_logp_bwd``; zero in columns past V) on the stream that was current in forward, which
+    waits for a ``stream`` of the caller's before it takes the log-probs; the kept set is a constant.  An action that is
+    not kept has log-prob -inf and no gradient.
     """
 
     @staticmethod
     def forward(ctx, logits, actions, opts=None):
         opts = dict(opts or {})
         ctx.V = opts.get("V")
+        ctx.own_stream = opts.get("stream") is None
         logp, _, rows = grpo_sampled_logp(logits.detach(), actions, **opts)
         ctx.save_for_backward(logits, actions, rows)
         return logp
@@ -159,5 +161,7 @@ class SampledLogp(torch.autograd.Function):
         padded = ctx.V is not None and ctx.V < logits.shape[1]
         dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype,
                                       device=logits.device).zero_() if padded else True
+        if not ctx.own_stream:  # their memory belongs to the forward's stream and may go before this one has read them
+            rows.record_stream(torch.cuda.current_stream(logits.device))
         d = grpo_sampled_logp_bwd(logits, actions, rows, grad_output.contiguous(), V=ctx.V, dlogits=dlogits)
         return d, None, None
