@@ -18,8 +18,8 @@ class GradList:
     ``grads``: fp32 or bf16 GPU tensors on one device, contiguous, of any shapes.  ``out``: where their clipped values
     go, a tensor of the same size for each (fp32 or bf16); None clips in place.  What is written may overlap nothing
     else.  The list holds on to the tensors' memory as it is now: gradients that are allocated anew at each step need a
-    new list (the calls take a plain list of tensors too and make one).  Making a list copies its table to the device
-    and cannot be captured into a graph; the calls that take it can.
+    new list (the calls take a plain list of tensors too and make one).  Making a list copies its table to the device and
+    waits for the current stream; while a graph is captured it raises, so a call in a graph takes a GradList made before.
     """
 
     def __init__(self, grads, out=None):
@@ -39,6 +39,9 @@ class GradList:
                 raise ValueError(f"out[{i}] must hold {grads[i].numel()} elements, got {outs[i].numel()}")
         self.device = every[0][1].device if every else torch.device("cuda", torch.cuda.current_device())
         _placed(self.device, **dict(every))
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():  # the copy below waits, which would end the capture
+                raise RuntimeError("a list of gradients cannot be made while a graph is captured: make a GradList before")
         # aliases: their memory stays, whatever becomes of the caller's tensors
         self._grads = [t.detach() for t in grads]
         self._outs = self._grads if outs is None else [t.detach() for t in outs]
