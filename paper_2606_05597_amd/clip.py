@@ -134,7 +134,8 @@ def grpo_grad_clip(grads, partials: torch.Tensor, max_norm: float, *, out=None,
 def grpo_clip_grad_norm_(grads, max_norm: float, *, out=None, error_flags: torch.Tensor | None = None,
                          stream=None) -> torch.Tensor:
     """The gradients' common norm, and the gradients clipped to ``max_norm``: ``grpo_grad_sumsq``, then
-    ``grpo_grad_clip``.  Returns the norm, a 0-dim fp32 tensor; nothing waits for the device."""
+    ``grpo_grad_clip``.  Returns the norm, a 0-dim fp32 tensor.  With a GradList nothing waits for the device; a plain list
+    of tensors is made into one first, which waits for the current stream."""
     grads = _grad_list(grads, out)
     _flags(error_flags, grads.device)
     return _on(grads.device, stream, lambda s: _clip(grads, _sumsq(grads, None, s), max_norm, error_flags, s))
