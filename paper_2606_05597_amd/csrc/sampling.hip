@@ -1329,18 +1329,25 @@ struct RowWork {
     double S;
   };
 
-  // The row's cut from the counts of values.  False where it falls among the words of bin kMid, which are not told apart.
+  // The row's cut from the counts of values.  False where it falls among the words of bin kMid, which are not told apart, or
+  // where these weigh too much for the unit that they are summed in.
   __device__ __forceinline__ bool cut_values(bool k_on, int k, bool p_on, double p, float z_min, ValueCut& out) {
     constexpr int kEach = (kValues + NT - 1) / NT;
     const int tid = threadIdx.x;
     const double mid_top = t2(bin_value(kMid + 1));
     // each thread kEach bins, from the largest value down; the last one holds the masked words
     double mid = 0.0;
+    // Without words of bin kMid the maximum may lie far below them, and their weight beyond the range of exp2_neg.  With one,
+    // the maximum is above -2^-15: 2^89 at most, which exp2_neg forms as well.
+    if (const int n_mid = uniform((int)sh.v.count[kMid])) {
+      const double unit = 0x1p-44 * exp2_neg(mid_top);
 #pragma unroll
-    for (int i = 0; i < kMidSums; ++i) mid += (double)sh.v.mid[i];
-    // Without such words the maximum may lie far below them, and their bin's weight beyond the range of exp2_neg.  With
-    // one, the maximum is above -2^-15: 2^89 at most, which exp2_neg forms as well.
-    if (mid > 0.0) mid *= 0x1p-44 * exp2_neg(mid_top);
+      for (int i = 0; i < kMidSums; ++i) mid += (double)sh.v.mid[i];
+      mid *= unit;
+      // Each is off by half a unit, which below a temperature of 2e-5 may be as much as such a word weighs; the kept words'
+      // sum is at least 1, and at least `mid` where they are kept.
+      if (n_mid * (0.5 * unit) > 0x1p-43 * fmax(1.0, mid)) return false;
+    }
     auto bin_at = [&](int i) { return kValues - 1 - (tid * kEach + i); };
     int q[kEach], my_n = 0;
     double w[kEach], my_m = 0.0;  // counts, weights of the bins
