@@ -423,16 +423,13 @@ struct Cut {
   int count;
 };
 
-constexpr int kMidSums = 8;
-static_assert(GRPO_SAMPLING_MAX_V / kMidSums <= 1 << 19, "the words of bin kMid");
+constexpr int kMidWords = 1 << 20;  // as many words of bin kMid do not fit their sum
 
 template <bool TABLE>
 struct ValueTable {
   double weight[kValues];
   uint32_t count[kValues];
-  // The weight of the words of bin kMid, in 2^-44 of the next bin's: eight sums, each over the words of every eighth
-  // lane, 2^19 of a row at most and so 2^63.
-  unsigned long long mid[kMidSums];
+  unsigned long long mid;  // the weight of the words of bin kMid, in 2^-44 of the next bin's
 };
 template <>
 struct ValueTable<false> {};
@@ -1302,7 +1299,7 @@ struct RowWork {
 
   __device__ __forceinline__ void clear_values() const {
     for (int i = threadIdx.x; i < kValues; i += NT) sh.v.count[i] = 0u;
-    if (threadIdx.x < kMidSums) sh.v.mid[threadIdx.x] = 0ull;
+    if (threadIdx.x == 0) sh.v.mid = 0ull;
     __syncthreads();
   }
 
@@ -1319,7 +1316,7 @@ struct RowWork {
       }
     each_mid(x, least, [&](float z) {
       const double y = exp2_neg(((double)z - (double)bin_value(kMid + 1)) * c) + 256.0;
-      atomicAdd(&sh.v.mid[threadIdx.x & (kMidSums - 1)], __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
+      atomicAdd(&sh.v.mid, __builtin_bit_cast(unsigned long long, y) & 0xfffffffffffffull);
     });
   }
 
@@ -1330,7 +1327,7 @@ struct RowWork {
   };
 
   // The row's cut from the counts of values.  False where it falls among the words of bin kMid, which are not told apart, or
-  // where these weigh too much for the unit that they are summed in.
+  // where these are too many for their sum or too light for its unit.
   __device__ __forceinline__ bool cut_values(bool k_on, int k, bool p_on, double p, float z_min, ValueCut& out) {
     constexpr int kEach = (kValues + NT - 1) / NT;
     const int tid = threadIdx.x;
@@ -1341,12 +1338,10 @@ struct RowWork {
     // the maximum is above -2^-15: 2^89 at most, which exp2_neg forms as well.
     if (const int n_mid = uniform((int)sh.v.count[kMid])) {
       const double unit = 0x1p-44 * exp2_neg(mid_top);
-#pragma unroll
-      for (int i = 0; i < kMidSums; ++i) mid += (double)sh.v.mid[i];
-      mid *= unit;
+      mid = (double)sh.v.mid * unit;
       // Each is off by half a unit, which below a temperature of 2e-5 may be as much as such a word weighs; the kept words'
       // sum is at least 1, and at least `mid` where they are kept.
-      if (n_mid * (0.5 * unit) > 0x1p-43 * fmax(1.0, mid)) return false;
+      if (n_mid >= kMidWords || n_mid * (0.5 * unit) > 0x1p-43 * fmax(1.0, mid)) return false;
     }
     auto bin_at = [&](int i) { return kValues - 1 - (tid * kEach + i); };
     int q[kEach], my_n = 0;
