@@ -27,6 +27,7 @@ def test_shares(T, V, kind):
         z = np.where(rng.random((T, V)) < 0.9, z * 2.0**-18, np.abs(z) * 0.1)
     x = torch.from_numpy(z).to(BF16)
     z = x.double().numpy()
-    for par in (dict(top_p=0.9), dict(top_p=0.3, temperature=1.4), dict(top_p=0.999, min_p=0.02), dict(top_k=V // 2, top_p=0.6)):
+    pars = (dict(top_p=0.9), dict(top_p=0.3, temperature=1.4), dict(top_p=0.999, min_p=0.02), dict(top_k=V // 2, top_p=0.6))
+    for par in pars if T < 10 else pars[:1]:
         check(x.cuda(), z, par, uniform(z, par, 1), V)
         check_logp(x.cuda(), z, par, actions(z, par, 2), V)

@@ -26,7 +26,8 @@ def test_all_negative(T, V, octaves):
     x = torch.from_numpy(z).to(BF16)
     z = x.double().numpy()
     assert z.max() == -1.0
-    for par in (dict(top_p=0.4), dict(top_k=V // 2, top_p=0.3), dict(min_p=0.5), dict(top_k=V - 100)):
+    pars = (dict(top_p=0.4), dict(top_k=V // 2, top_p=0.3), dict(min_p=0.5), dict(top_k=V - 100))
+    for par in pars if T < 10 else pars[:1]:
         par = dict(par, temperature=tau_of(octaves))
         check(x.cuda(), z, par, uniform(z, par, 1), V)
         check_logp(x.cuda(), z, par, actions(z, par, 2), V)
