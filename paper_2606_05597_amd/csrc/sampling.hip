@@ -1637,7 +1637,7 @@ __device__ __forceinline__ void write_row(const RowArgs& a, int t, grpo_sampling
 // look at: latency, a dozen steps between barriers (bf16 [1, 151,936], k = 50 with p = 0.95: 12.5 us after the tiles' 4.5);
 // many: the passes over the row (top-p 0.9: fp32 [500, 32,003] 62 us = 1.0 TB/s, bf16 [256, 151,936] 48 us = 1.6 TB/s; a
 // setting per row, log-probs: bf16 [2,000, 151,669] 0.19 ms = 3.1 TB/s).  128 VGPRs, for two rows of 512
-// threads to a CU, at the price of 7 to 47 of a thread's values in scratch.
+// threads to a CU, at the price of 32 to 128 bytes of scratch per lane: 7 to 47 VGPRs, and 85 to 121 SGPRs in others' lanes.
 template <typename Tin, bool FUSED, bool DRAW, int NT>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 4))) void k_sample_row(const RowArgs a, int row0) {
   __shared__ RowShared<NT> sh;
@@ -2167,13 +2167,15 @@ static void launch_row_kernel(const RowArgs& a, int64_t T, hipStream_t s) {
                        row_tile_bytes(a.tiles), s, a, (int)r);
 }
 
-// Whether rows go to workgroups of 256 threads, four on a CU, and not to ones of 512 or 1,024.  Up to 16,384 words a top-k
-// is found among the partial maxima that such a workgroup holds (us, 256 against 512 threads, bf16, k = 50 with p = 0.95:
-// V = 2,000 T = 4 12 and 13, T = 3,000 37 and 76; V = 16,384 T = 4 13 and 14, T = 3,000 49 and 85).  A top-p alone goes
+// Whether rows go to workgroups of 256 threads, four on a CU, and not to ones of 512 or 1,024.  Up to 16,384 words a small
+// top-k is found among the partial maxima that such a workgroup holds, 64 to a tile (us, 256 against 512 threads, bf16, k = 50
+// with p = 0.95: V = 2,000 T = 4 12 and 13, T = 3,000 37 and 76; V = 16,384 T = 4 13 and 14, T = 3,000 49 and 85).  A larger k
+// is not, and the rule does not look at it: V = 16,384, k = 2,000 T = 4 bf16 30 and 22, fp32 30 and 24, T = 3,000 134 and 140,
+// 142 and 184; with p = 0.95 T = 4 44 and 23, 45 and 36, T = 3,000 210 and 149, 221 and 276.  A top-p alone goes
 // through more of the row, which few rows do faster with more threads (V = 16,384, T = 200: bf16 35 and 29, fp32 34 and
 // 30) and many with more rows at once (T = 3,000: V = 2,048 bf16 56 and 104; V = 8,000 bf16 90 and 127; V = 16,384 fp32
 // 118 and 161), but for bf16 rows beyond 8,192 words, whose values the large workgroup counts (126 and 120; T = 600 60 and
-// 39).
+// 39).  fp32 [200, 8,000] is on the wrong side of that: 28 and 31.
 template <typename Tin>
 static bool short_rows(const RowArgs& a, int64_t T) {
   if (a.V > RowShape<256>::kMaxWords) return false;
