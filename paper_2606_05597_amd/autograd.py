@@ -141,8 +141,9 @@ class SampledLogp(torch.autograd.Function):
     own: logits [T, V] (bf16 or fp32, on the GPU), ``opts`` a dict of the keyword options of ``grpo_sampled_logp``
     (temperature, top_k, top_p, min_p, V, error_flags, workspace, stream).  backward reads the logits again and writes
     their gradient (``grpo_sampled_logp_bwd``; zero in columns past V) on the stream that was current in forward, which
-    waits for a ``stream`` of the caller's before it takes the log-probs; the kept set is a constant.  An action that is
-    not kept has log-prob -inf and no gradient.
+    has to wait for a ``stream`` of the caller's before it takes the log-probs; the kept set is a constant.  An action that
+    is not kept has log-prob -inf and no gradient.  Forward and backward can be captured into a graph together, while no
+    eager autograd graph of the same leaves is alive.
     """
 
     @staticmethod
