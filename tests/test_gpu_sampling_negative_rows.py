@@ -17,7 +17,7 @@ def tau_of(octaves, top=1.0):
     return float(np.float32((top + 2.0**-15) * np.log2(np.e) / octaves))
 
 
-@pytest.mark.parametrize("octaves", [100.0, 1023.0, 1024.0, 1024.4, 1025.0, 2048.0, 3072.2, 1e5])
+@pytest.mark.parametrize("octaves", [100.0, 1023.0, 1024.0, 1024.4, 1025.0, 2048.0, 5120.2, 1e5])
 @pytest.mark.parametrize("T,V", [(2, 9001), (260, 20000)])
 def test_all_negative(T, V, octaves):
     rng = np.random.default_rng(int(octaves))
