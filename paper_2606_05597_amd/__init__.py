@@ -17,7 +17,7 @@ from . import _lib
 from ._lib import (GRPO_ADV_GROUP_NORM, GRPO_ADV_SUCCESS_FILTER, GRPO_BF16, GRPO_F32,  # noqa: F401
                    GRPO_FLAG_ACTION, GRPO_FLAG_NONFINITE, GRPO_FLAG_OFFSETS, GRPO_FLAG_SETTING, GRPO_GRAD_PARTIALS,
                    GRPO_NOALLOC_SCRATCH_BYTES,
-                   GRPO_NORM_CONST_K, GRPO_NORM_TRAJ_STEPS, GRPO_SAMPLING_MAX_V, GrpoError)
+                   GRPO_NORM_CONST_K, GRPO_NORM_TRAJ_STEPS, GRPO_SAMPLING_MAX_V, GRPO_TOP_MAX, GrpoError)
 
 __all__ = ["grpo_advantages", "grpo_advantages_ex", "grpo_loss_workspace_bytes", "grpo_loss_fwd_bwd",
            "grpo_loss_fwd_bwd_noalloc", "fused_lmhead_workspace_bytes",
@@ -25,6 +25,7 @@ __all__ = ["grpo_advantages", "grpo_advantages_ex", "grpo_loss_workspace_bytes",
            "vocab_stats_fields", "fused_lmhead_vocab_shard_stats", "fused_lmhead_grpo_vocab_shard",
            "vocab_shard_logits_buffer", "GrpoLoss", "FusedLmHeadGrpoLoss", "loss",
            "fused_lmhead_token_logp", "grpo_sample", "grpo_sampled_logp", "grpo_sampled_logp_bwd", "SampledLogp",
+           "grpo_token_logp_top", "grpo_token_logp_top_bwd", "TokenLogpTop",
            "GradList", "grpo_grad_sumsq", "grpo_grad_clip", "grpo_clip_grad_norm_",
            "grpo_status_str", "LossAux", "GrpoError"]
 
@@ -636,5 +637,6 @@ def fused_lmhead_grpo_vocab_shard(hidden: torch.Tensor, w_shard: torch.Tensor, s
 
 
 from .sampling import grpo_sample, grpo_sampled_logp, grpo_sampled_logp_bwd  # noqa: E402  (need the helpers above)
+from .top import grpo_token_logp_top, grpo_token_logp_top_bwd  # noqa: E402
 from .clip import GradList, grpo_clip_grad_norm_, grpo_grad_clip, grpo_grad_sumsq  # noqa: E402
-from .autograd import FusedLmHeadGrpoLoss, GrpoLoss, SampledLogp  # noqa: E402
+from .autograd import FusedLmHeadGrpoLoss, GrpoLoss, SampledLogp, TokenLogpTop  # noqa: E402

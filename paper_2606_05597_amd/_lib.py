@@ -1,4 +1,4 @@
-"""ctypes view of libgrpo's C ABI (include/grpo.h, grpo_sampling.h, grpo_clip.h).  Marshalling only."""
+"""ctypes view of libgrpo's C ABI (include/grpo*.h).  Marshalling only."""
 from __future__ import annotations
 
 import ctypes
@@ -31,6 +31,7 @@ GRPO_FLAG_SETTING = 8
 
 GRPO_SAMPLING_MAX_V = 4194304
 GRPO_GRAD_PARTIALS = 2048
+GRPO_TOP_MAX = 64
 
 P = ctypes.c_void_p
 
@@ -134,6 +135,12 @@ def load() -> ctypes.CDLL:
         lib.grpo_sampled_logp.restype = ctypes.c_int
         lib.grpo_sampled_logp_bwd.argtypes = [P, I32, I64, I64, I64, P, P, P, P, P]
         lib.grpo_sampled_logp_bwd.restype = ctypes.c_int
+        lib.grpo_token_logp_top_workspace_bytes.argtypes = [I64, I64, I32]
+        lib.grpo_token_logp_top_workspace_bytes.restype = SZ
+        lib.grpo_token_logp_top.argtypes = [P, I32, I64, I64, I64, P, ctypes.c_float, P, I32, P, P, P, P, P, P, P, SZ, P]
+        lib.grpo_token_logp_top.restype = ctypes.c_int
+        lib.grpo_token_logp_top_bwd.argtypes = [P, I32, I64, I64, I64, P, I32, P, P, P, P, P, P, P]
+        lib.grpo_token_logp_top_bwd.restype = ctypes.c_int
         lib.grpo_grad_table_bytes.argtypes = [I32]
         lib.grpo_grad_table_bytes.restype = SZ
         lib.grpo_grad_table.argtypes = [ctypes.POINTER(Grad), I32, P, SZ, ctypes.POINTER(GradLayout)]

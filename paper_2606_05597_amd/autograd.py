@@ -20,6 +20,7 @@ from torch.autograd.function import once_differentiable
 
 from . import _check, _lib, _ptr, _stream, fused_lmhead_grpo, fused_lmhead_grpo_blocked, grpo_loss_fwd_bwd
 from .sampling import grpo_sampled_logp, grpo_sampled_logp_bwd
+from .top import grpo_token_logp_top, grpo_token_logp_top_bwd
 
 _UPSTREAM = ("scale", "unit")
 
@@ -134,6 +135,13 @@ class FusedLmHeadGrpoLoss(torch.autograd.Function):
         return dh, dW, None, None, None, None, None, None, None
 
 
+def _dlogits_like(logits, V):
+    """What a call takes as ``dlogits`` to return the gradient of ``logits``: zeros in columns past V, which it leaves."""
+    if V is None or V >= logits.shape[1]:
+        return True
+    return torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=logits.device).zero_()
+
+
 class SampledLogp(torch.autograd.Function):
     """``logp = SampledLogp.apply(logits, actions, opts)``
 
@@ -159,10 +167,45 @@ class SampledLogp(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, grad_output):
         logits, actions, rows = ctx.saved_tensors
-        padded = ctx.V is not None and ctx.V < logits.shape[1]
-        dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype,
-                                      device=logits.device).zero_() if padded else True
         if not ctx.own_stream:  # their memory belongs to the forward's stream and may go before this one has read them
             rows.record_stream(torch.cuda.current_stream(logits.device))
-        d = grpo_sampled_logp_bwd(logits, actions, rows, grad_output.contiguous(), V=ctx.V, dlogits=dlogits)
+        d = grpo_sampled_logp_bwd(logits, actions, rows, grad_output.contiguous(), V=ctx.V,
+                                  dlogits=_dlogits_like(logits, ctx.V))
         return d, None, None
+
+
+class TokenLogpTop(torch.autograd.Function):
+    """``logp, entropy, ids, top_logp = TokenLogpTop.apply(logits, actions, n, opts)``
+
+    ``grpo_token_logp_top`` for objectives of the caller's own: the log-probs of given actions (fp32 [T]), the entropies
+    (fp32 [T]) and the n likeliest words (int32 [T, n]) with their log-probs (fp32 [T, n]), all three differentiable.
+    logits [T, V] (bf16 or fp32, on the GPU), ``opts`` a dict of the keyword options of ``grpo_token_logp_top``
+    (temperature, V, error_flags, workspace, stream).  backward reads the logits again and writes their gradient
+    (``grpo_token_logp_top_bwd``; zero in columns past V) on the stream that was current in forward, which has to wait for
+    a ``stream`` of the caller's before it takes the results.  Which words are the alternatives is a constant.  Forward
+    and backward can be captured into a graph together, while no eager autograd graph of the same leaves is alive.
+    """
+
+    @staticmethod
+    def forward(ctx, logits, actions, n, opts=None):
+        opts = dict(opts or {})
+        ctx.V = opts.get("V")
+        ctx.own_stream = opts.get("stream") is None
+        logp, entropy, ids, top_logp, rows = grpo_token_logp_top(logits.detach(), actions, n, **opts)
+        ctx.save_for_backward(logits, actions, ids, rows)
+        ctx.mark_non_differentiable(ids)
+        ctx.set_materialize_grads(False)
+        return logp, entropy, ids, top_logp
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp, dentropy, _, dtop):
+        if dlogp is None and dentropy is None and dtop is None:
+            return None, None, None, None
+        logits, actions, ids, rows = ctx.saved_tensors
+        if not ctx.own_stream:  # their memory belongs to the forward's stream and may go before this one has read them
+            for t in (ids, rows):
+                t.record_stream(torch.cuda.current_stream(logits.device))
+        up = (None if t is None else t.contiguous() for t in (dlogp, dentropy, dtop))
+        d = grpo_token_logp_top_bwd(logits, actions, ids, rows, *up, V=ctx.V, dlogits=_dlogits_like(logits, ctx.V))
+        return d, None, None, None

@@ -74,6 +74,16 @@ inline RowForm row_form(const void* in, const void* out, int64_t V, int64_t ld, 
   return (!out || ((uintptr_t)in - (uintptr_t)out) % 16 == 0) ? RowForm::kRagged : RowForm::kElements;
 }
 
+// Whether T rows of V elements, ld apart, at two places share memory without being the same rows.
+inline bool rows_overlap(const void* a, const void* b, int64_t T, int64_t V, int64_t ld, size_t esz) {
+  const bool before = (uintptr_t)a < (uintptr_t)b;
+  const uintptr_t x = (uintptr_t)(before ? a : b), y = (uintptr_t)(before ? b : a);
+  const uintptr_t bytes = (uintptr_t)V * esz, step = (uintptr_t)ld * esz;
+  if (x == y || y - x >= (uintptr_t)(T - 1) * step + bytes) return false;
+  const uintptr_t r = (y - x) % step;  // a row of the second begins r bytes into one of the first
+  return r < bytes || (step - r < bytes && (y - x) / step + 1 < (uintptr_t)T);
+}
+
 // Compute units of the device the stream belongs to (which need not be the current device), or 0 if the
 // runtime cannot say.
 inline int stream_cu_count(hipStream_t s) {

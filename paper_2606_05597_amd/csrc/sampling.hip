@@ -2149,15 +2149,6 @@ static bool bad_shape(int64_t T, int64_t V, int64_t ld) {
   return T < 0 || T >= ((int64_t)1 << 31) || V < 1 || V > GRPO_SAMPLING_MAX_V || ld < V;
 }
 
-// Whether T rows of V elements, ld apart, at two places share memory without being the same rows.
-static bool rows_overlap(const void* a, const void* b, int64_t T, int64_t V, int64_t ld, size_t esz) {
-  const uintptr_t x = std::min((uintptr_t)a, (uintptr_t)b), y = std::max((uintptr_t)a, (uintptr_t)b);
-  const uintptr_t bytes = (uintptr_t)V * esz, step = (uintptr_t)ld * esz;
-  if (x == y || y - x >= (uintptr_t)(T - 1) * step + bytes) return false;
-  const uintptr_t r = (y - x) % step;  // a row of the second begins r bytes into one of the first
-  return r < bytes || (step - r < bytes && (y - x) / step + 1 < (uintptr_t)T);
-}
-
 constexpr int64_t kRowsPerLaunch = 1 << 20;  // a launch's threads stay below 2^32
 
 template <typename Tin, bool FUSED, bool DRAW, int NT>

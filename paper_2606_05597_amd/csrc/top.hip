@@ -1,0 +1,753 @@
+// What a row of logits says about a token (grpo_top.h): the given token's log-prob, the entropy and the n likeliest
+// alternatives, in one pass over the row, and the gradient of all three, in another.
+//
+// Forward.  Each thread walks its vectors and keeps, relative to its running maximum m and in units of log 2,
+//   s = sum 2^w, t = sum 2^w w, w = (z - m) log2(e) / tau,
+// over the words (z > -1e8).  m is the sum's shift and, for the alternatives, the maximum of a part of the row: the n-th
+// largest of 256 such maxima (each over the words of NT / 256 neighbouring lanes) is a lower bound L of the n-th largest
+// word, and no word >= L lies outside the parts whose maximum is >= L.  Those parts, n of them unless maxima repeat, are
+// read a second time, their words >= L (n and a few) go to a list in LDS, and a word's place is the number of list words
+// in front of it.  Where maxima repeat so often that the list or the number of parts is too small, the n-th largest word is
+// found by bisection with counts over the row.
+// Where rows are few and long, a row is cut into parts of their own workgroups, and a second launch joins them.
+//
+// Backward.  A streaming pass: dlogits_v = p_v (A log2 p_v + B) with A, B of the row; the words with a coefficient of their
+// own (the action, the alternatives) are formed apart in fp64 and stored over it by the thread that stored their vector.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "device.h"
+#include "grpo_top.h"
+#include "host.h"
+
+namespace grpo {
+
+constexpr int kGroups = 256;      // maxima that bound the n-th largest word
+constexpr int kMostGroups = 128;  // parts that are read again
+constexpr int kTopCap = 1024;     // words the list holds
+constexpr uint32_t kNothing = 0;  // the key of no word (a word's is larger)
+
+// A row's part of a workgroup: its sums relative to max, in units of log 2.
+struct TopPart {
+  double s, t;
+  float max;
+  float pad;
+};
+
+struct TopArgs {
+  const void* logits;
+  int64_t ld;
+  int V, n;
+  const float* tau_rows;
+  float tau_all;
+  const int32_t* actions;
+  float* logp;
+  float* entropy;
+  int32_t* ids;
+  float* top_logp;
+  grpo_top_row* rows;
+  int32_t* flags;
+  int parts, part_cols;  // workgroups to a row and their columns
+  TopPart* part;         // ws [T][parts]
+  uint64_t* part_keys;   // ws [T][parts][n]
+};
+
+// Order of words: fp32 values as whole numbers (-0 as 0), the larger the greater; below them the index, the lower the
+// greater.  bf16 words' lower 16 bits say nothing, and the first 16 are an order by themselves.
+__device__ __forceinline__ uint32_t order_of(float z) {
+  const uint32_t b = __float_as_uint(z + 0.f);
+  return (b >> 31) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+  return __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
+}
+__device__ __forceinline__ uint64_t key_of(float z, int idx) {
+  return ((uint64_t)order_of(z) << 32) | (0xffffffffu - (uint32_t)idx);
+}
+__device__ __forceinline__ bool is_word(float z) { return z > kShiftMin; }
+
+// One word folded into (s, t) at the shift m.  The difference comes first, so that w's error is relative to w whatever m
+// and tau are.  A masked word adds 2^-200 = 0; a NaN is not masked and makes s NaN.
+__device__ __forceinline__ void fold_word(float z, float m, float sc, float& s, float& t) {
+  const float w = z <= kShiftMin ? -200.f : (z - m) * sc;
+  const float e = __builtin_amdgcn_exp2f(w);
+  s += e;
+  t = fmaf(e, w, t);
+}
+
+__device__ __forceinline__ void raise_shift(float& m, float mn, float sc, float& s, float& t) {
+  if (mn > m) {
+    const float dl = (mn - m) * sc, f = __builtin_amdgcn_exp2f(-dl);
+    t = f == 0.f ? 0.f : f * fmaf(-dl, s, t);
+    s *= f;
+    m = mn;
+  }
+}
+
+// log2(e) / tau, NaN for a temperature out of range (which then makes the row's sums NaN).
+__device__ __forceinline__ float scale_of(float tau) {
+  return tau >= 1e-6f && tau <= 1e6f ? kLog2e / tau : NAN;
+}
+
+template <int NT>
+struct TopSmem {
+  float m[NT / 64];
+  double s[NT / 64], t[NT / 64];
+  double log_sum;
+  uint32_t group[kGroups];  // upper 16 bits of the order of each group's maximum
+  uint32_t bound;           // and of L
+  int n_groups, count;
+  int wave_count[NT / 64];
+  uint16_t groups[kMostGroups];
+  uint64_t list[kTopCap];
+};
+
+// All threads' (m, s, t) joined in fp64, the result in every thread.
+template <int NT>
+__device__ __forceinline__ void join_threads(float m, float s, float t, float sc, TopSmem<NT>& sm, float& M, double& S,
+                                             double& T) {
+  constexpr int NW = NT / 64;
+  static_assert(NW <= 16, "one wave to a lane of 16");
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const float mw = wave_max_dpp(m);
+  const float dl = (m - mw) * sc, f = __builtin_amdgcn_exp2f(dl);
+  const double sw = wave_sum_dpp((double)f * (double)s);
+  const double tw = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * ((double)t + (double)dl * (double)s));
+  if (lane == 0) {
+    sm.m[wv] = mw;
+    sm.s[wv] = sw;
+    sm.t[wv] = tw;
+  }
+  __syncthreads();
+  const int q = lane & 15;
+  const bool in = q < NW;
+  const float mq = in ? sm.m[q] : -INFINITY;
+  M = row16_max(mq);
+  const float dq = (mq - M) * sc, g = in ? __builtin_amdgcn_exp2f(dq) : 0.f;
+  S = row16_sum(in ? (double)g * sm.s[q] : 0.0);
+  T = row16_sum(g == 0.f || !in ? 0.0 : (double)g * (sm.t[q] + (double)dq * sm.s[q]));
+}
+
+// What the row comes to, from the joined sums: one thread.
+__device__ inline grpo_top_row finish_row(const TopArgs& a, int t, float tau, float M, double S, double Tsum) {
+  grpo_top_row r;
+  const int act = a.actions[t];
+  const bool act_ok = act >= 0 && act < a.V;
+  const bool bad_tau = !(tau >= 1e-6f && tau <= 1e6f), bad = isnan(S) || isnan(M) || M == INFINITY || bad_tau;
+  r.temperature = tau;
+  int flags = act_ok ? 0 : GRPO_FLAG_ACTION;
+  if (bad) {
+    r.log_sum = NAN;
+    r.max = NAN;
+    r.entropy = NAN;
+    r.logp = act_ok ? NAN : 0.f;
+    flags |= bad_tau ? GRPO_FLAG_SETTING : GRPO_FLAG_NONFINITE;
+  } else if (S == 0.0) {
+    r.log_sum = -INFINITY;
+    r.max = -INFINITY;
+    r.entropy = 0.f;
+    r.logp = act_ok ? -INFINITY : 0.f;
+    flags |= GRPO_FLAG_NONFINITE;
+  } else {
+    r.log_sum = log(S);
+    r.max = M;
+    r.entropy = (float)(r.log_sum - Tsum / S * kLn2);  // both terms >= 0
+    r.logp = 0.f;
+  }
+  if (flags && a.flags) atomicOr(a.flags, flags);
+  return r;
+}
+
+template <typename Tin>
+__device__ __forceinline__ void store_row(const TopArgs& a, int t, grpo_top_row r) {
+  const int act = a.actions[t];
+  if (r.max > -INFINITY && act >= 0 && act < a.V) {
+    const float z = load_elem(static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld + act);
+    r.logp = is_word(z) ? (float)(((double)z - (double)r.max) / (double)r.temperature - r.log_sum) : -INFINITY;
+  }
+  if (a.logp) a.logp[t] = r.logp;
+  if (a.entropy) a.entropy[t] = r.entropy;
+  if (a.rows) a.rows[t] = r;
+}
+
+// Where a list word goes: a final row's outputs, or a part's keys.
+struct TopOut {
+  int32_t* ids;      // the row's, or NULL
+  float* logp;
+  uint64_t* keys;    // the part's, or NULL
+  double max, tau, log_sum;
+  int c0;
+  __device__ __forceinline__ void put(int j, uint64_t key) const {
+    const uint32_t idx = 0xffffffffu - (uint32_t)key;
+    if (keys) {
+      keys[j] = key;
+      return;
+    }
+    if (ids) ids[j] = (int)idx;
+    if (logp) logp[j] = (float)(((double)value_of((uint32_t)(key >> 32)) - max) / tau - log_sum);
+  }
+  __device__ __forceinline__ void none(int j, bool bad) const {
+    if (keys) keys[j] = kNothing;
+    if (ids) ids[j] = -1;
+    if (logp) logp[j] = bad ? NAN : -INFINITY;
+  }
+};
+
+// The list's first n words in order; the rest of the n places empty.  Every thread of the workgroup.
+template <int NT, class Smem>
+__device__ __forceinline__ void rank_list(const Smem& sm, int c, int n, const TopOut& out) {
+  const int tid = threadIdx.x;
+  for (int i = tid; i < c; i += NT) {
+    const uint64_t key = sm.list[i];
+    int rank = 0;
+    for (int j = 0; j < c; ++j) rank += sm.list[j] > key;
+    if (rank < n) out.put(rank, key);
+  }
+  for (int j = c + tid; j < n; j += NT) out.none(j, false);
+}
+
+// The n-th largest of `per * 64` 16-bit keys, those of lane l its `per` in k: one wave.
+template <int PER>
+__device__ __forceinline__ uint32_t nth_largest(const uint32_t (&k)[PER], int n) {
+  uint32_t p = 0;
+#pragma unroll 1
+  for (int b = 15; b >= 0; --b) {
+    const uint32_t c = p | (1u << b);
+    int cnt = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) cnt += __popcll(__ballot(k[i] >= c));
+    if (cnt >= n) p = c;
+  }
+  return p;
+}
+
+// The sum of v over the workgroup, in every thread.
+template <int NT, class Smem>
+__device__ __forceinline__ int block_sum(int v, Smem& sm) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  __syncthreads();  // the last use of wave_count is over
+  if ((threadIdx.x & 63) == 0) sm.wave_count[threadIdx.x >> 6] = v;
+  __syncthreads();
+  int sum = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) sum += sm.wave_count[w];
+  return sum;
+}
+
+// The n likeliest of a row (or part) with more than n words >= the bound, whatever repeats in it: the n-th largest value by
+// bisection between the bound and the maximum, each step a count over the row; then the words above it (fewer than n) and
+// the first of those that equal it.
+template <typename Tin, int NT>
+__device__ __noinline__ void top_by_counts(const Tin* row, int cols, int n, float M, TopSmem<NT>& sm, const TopOut& out) {
+  constexpr int EPV = 16 / (int)sizeof(Tin), SH = sizeof(Tin) == 2 ? 16 : 0;
+  typedef typename VecAt<Tin>::type u32x4_any;
+  const int tid = threadIdx.x, nvec = cols / EPV, tiles = (nvec + NT - 1) / NT, n_edge = cols - nvec * EPV;
+  const float ez = tid < n_edge ? load_elem(row + nvec * EPV + tid) : -INFINITY;
+  auto rank_of = [](float z) { return is_word(z) ? order_of(z) >> SH : 0u; };
+  uint32_t lo = (sm.bound << 16) >> SH, hi = (order_of(M) >> SH) + 1;  // count(>= lo) >= n > count(>= hi)
+  while (hi - lo > 1) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    int cnt = rank_of(ez) >= mid;
+#pragma unroll 4
+    for (int q = 0; q < tiles; ++q) {
+      const int vi = q * NT + tid;
+      if (vi >= nvec) break;
+      const u32x4 x = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi * EPV);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) cnt += rank_of(elem<Tin>(x, e)) >= mid;
+    }
+    if (block_sum<NT>(cnt, sm) >= n) lo = mid;
+    else hi = mid;
+  }
+  __syncthreads();
+  if (tid == 0) sm.count = 0;
+  __syncthreads();
+  uint64_t* equal = sm.list + GRPO_TOP_MAX;
+  int n_equal = 0;  // words that equal lo so far, in index order
+  auto take = [&](float z, int idx, int& at) {
+    const uint32_t r = rank_of(z);
+    if (r > lo) sm.list[atomicAdd(&sm.count, 1)] = key_of(z, out.c0 + idx);
+    else if (r == lo) {
+      if (at < n) equal[at] = key_of(z, out.c0 + idx);
+      ++at;
+    }
+  };
+#pragma unroll 1
+  for (int q = 0; q <= tiles; ++q) {  // the last tile: the row's last words
+    const int vi = q * NT + tid;
+    const bool vec = q < tiles && vi < nvec;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (vec) x = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi * EPV);
+    const bool edge = q == tiles && tid < n_edge;
+    int here = 0;
+    if (vec) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) here += rank_of(elem<Tin>(x, e)) == lo;
+    } else if (edge) {
+      here = rank_of(ez) == lo;
+    }
+    int before = here;  // inclusive prefix over the wave
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(before, o, 64);
+      if ((tid & 63) >= o) before += v;
+    }
+    __syncthreads();
+    if ((tid & 63) == 63) sm.wave_count[tid >> 6] = before;
+    __syncthreads();
+    int at = n_equal + before - here;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < (tid >> 6)) at += sm.wave_count[w];
+      n_equal += sm.wave_count[w];
+    }
+    if (vec) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) take(elem<Tin>(x, e), vi * EPV + e, at);
+    } else if (edge) {
+      take(ez, nvec * EPV + tid, at);
+    }
+  }
+  __syncthreads();
+  const int above = sm.count;  // < n
+  if (tid < above) {
+    const uint64_t key = sm.list[tid];
+    int rank = 0;
+    for (int j = 0; j < above; ++j) rank += sm.list[j] > key;
+    out.put(rank, key);
+  }
+  if (tid >= above && tid < n) out.put(tid, equal[tid - above]);
+}
+
+// One workgroup to a row, or (PART) to a part of it.
+template <typename Tin, int NT, int U, bool PART>
+__global__ __launch_bounds__(NT) void k_top(const TopArgs a, int row0) {
+  constexpr int EPV = 16 / (int)sizeof(Tin), G = NT / kGroups;
+  static_assert(G == 1 || G == 2 || G == 4, "lanes to a group");
+  typedef typename VecAt<Tin>::type u32x4_any;
+  __shared__ TopSmem<NT> sm;
+  const int tid = threadIdx.x;
+  const int t = row0 + (int)(PART ? blockIdx.x / (unsigned)a.parts : blockIdx.x);
+  const int part = PART ? (int)(blockIdx.x % (unsigned)a.parts) : 0;
+  const int c0 = PART ? part * a.part_cols : 0, cols = PART ? min(a.part_cols, a.V - c0) : a.V;
+  const Tin* row = static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld + c0;
+  const float tau = a.tau_rows ? a.tau_rows[t] : a.tau_all, sc = scale_of(tau);
+  const int nvec = cols / EPV, n_edge = cols - nvec * EPV;
+  if (tid == 0) sm.n_groups = sm.count = 0;
+  const float ez = tid < n_edge ? load_elem(row + nvec * EPV + tid) : -INFINITY;
+  float m = fmaxf(kShiftMin, ez), s = 0.f, tt = 0.f;
+  fold_word(ez, m, sc, s, tt);
+  for (int base = tid; base < nvec; base += NT * U) {
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int vi = base + u * NT;
+      if (vi < nvec) x[u] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi * EPV);
+    }
+    float cm = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (base + u * NT < nvec) cm = vec_max<Tin>(x[u], cm);
+    raise_shift(m, cm, sc, s, tt);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (base + u * NT < nvec) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) fold_word(elem<Tin>(x[u], e), m, sc, s, tt);
+      }
+    }
+  }
+  float gm = m;  // the maximum of the group's lanes
+  if (G >= 2) gm = fmaxf(gm, dpp_f32v<0xB1>(gm));
+  if (G >= 4) gm = fmaxf(gm, dpp_f32v<0x4E>(gm));
+  const uint32_t gkey = order_of(gm) >> 16;
+  if (tid % G == 0) sm.group[tid / G] = gkey;
+  float M;
+  double S, Tsum;
+  join_threads<NT>(m, s, tt, sc, sm, M, S, Tsum);
+  const bool bad = isnan(S) || isnan(M) || M == INFINITY || isnan(sc), some = !bad && S > 0.0;
+  if (PART) {
+    if (tid == 0) a.part[(int64_t)t * a.parts + part] = TopPart{bad ? (double)NAN : S, Tsum, some ? M : kShiftMin, 0.f};
+  } else if (tid == 0) {
+    const grpo_top_row r = finish_row(a, t, tau, M, S, Tsum);
+    sm.log_sum = r.log_sum;
+    store_row<Tin>(a, t, r);
+  }
+  const int n = a.n;
+  if (n == 0) return;
+  if (tid < 64 && some) {
+    uint32_t k[kGroups / 64];
+#pragma unroll
+    for (int i = 0; i < kGroups / 64; ++i) k[i] = sm.group[tid + 64 * i];
+    const uint32_t p = nth_largest(k, n);
+    if (tid == 0) sm.bound = p;
+  }
+  __syncthreads();
+  TopOut out;
+  const int64_t at = (int64_t)t * n;
+  out.ids = !PART && a.ids ? a.ids + at : nullptr;
+  out.logp = !PART && a.top_logp ? a.top_logp + at : nullptr;
+  out.keys = PART ? a.part_keys + ((int64_t)t * a.parts + part) * n : nullptr;
+  out.max = M;
+  out.tau = tau;
+  out.log_sum = PART ? 0.0 : sm.log_sum;
+  out.c0 = c0;
+  if (!some) {
+    if (tid < n) out.none(tid, bad);
+    return;
+  }
+  const uint32_t bound = sm.bound;
+  if (tid % G == 0 && gkey >= bound && is_word(gm)) {
+    const int g = atomicAdd(&sm.n_groups, 1);
+    if (g < kMostGroups) sm.groups[g] = (uint16_t)(tid / G);
+  }
+  __syncthreads();
+  const int ng = sm.n_groups;
+  bool fits = ng <= kMostGroups;
+  if (fits) {
+    const float least = value_of(bound << 16);
+    auto take = [&](float z, int idx) {
+      if (z >= least && is_word(z)) {
+        const int i = atomicAdd(&sm.count, 1);
+        if (i < kTopCap) sm.list[i] = key_of(z, c0 + idx);
+      }
+    };
+    if (tid < n_edge) take(ez, nvec * EPV + tid);
+    const int per = (nvec + NT - 1) / NT * G, items = ng * per;
+    constexpr int R = 2;  // loads in flight
+    for (int i0 = tid; i0 < items; i0 += R * NT) {
+      int vi[R];
+      u32x4 x[R];
+#pragma unroll
+      for (int u = 0; u < R; ++u) {
+        const int i = i0 + u * NT, gi = i / per, r = i - gi * per;
+        vi[u] = i < items ? r / G * NT + sm.groups[gi] * G + r % G : nvec;
+        if (vi[u] < nvec) x[u] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi[u] * EPV);
+      }
+#pragma unroll
+      for (int u = 0; u < R; ++u) {
+        if (vi[u] >= nvec || !(vec_max<Tin>(x[u], -INFINITY) >= least)) continue;
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) take(elem<Tin>(x[u], e), vi[u] * EPV + e);
+      }
+    }
+    __syncthreads();
+    fits = sm.count <= kTopCap;
+  }
+  if (fits) rank_list<NT>(sm, sm.count, n, out);
+  else top_by_counts<Tin, NT>(row, cols, n, M, sm, out);
+}
+
+// A row's parts joined: one workgroup to a row.
+constexpr int kJoinNT = 256;
+struct JoinSmem {
+  uint64_t list[kTopCap];
+  uint64_t all[kTopCap];
+  double log_sum;
+  uint32_t bound;
+  int count;
+};
+template <typename Tin>
+__global__ __launch_bounds__(kJoinNT) void k_top_join(const TopArgs a) {
+  __shared__ JoinSmem sm;
+  const int t = blockIdx.x, tid = threadIdx.x, n = a.n, c = a.parts * n;
+  const float tau = a.tau_rows ? a.tau_rows[t] : a.tau_all, sc = scale_of(tau);
+  const uint64_t* keys = a.part_keys + (int64_t)t * c;
+  for (int i = tid; i < c; i += kJoinNT) sm.all[i] = keys[i];
+  if (tid == 0) sm.count = 0;
+  const TopPart* part = a.part + (int64_t)t * a.parts;
+  float M = kShiftMin;
+  for (int p = 0; p < a.parts; ++p) M = fmaxf(M, part[p].max);
+  double S = 0.0, Tsum = 0.0;
+  for (int p = 0; p < a.parts; ++p) {
+    const TopPart r = part[p];
+    const float d = (r.max - M) * sc, f = __builtin_amdgcn_exp2f(d);
+    S += (double)f * r.s;
+    if (f != 0.f) Tsum += (double)f * (r.t + (double)d * r.s);
+  }
+  const bool bad = isnan(S) || isnan(sc), some = !bad && S > 0.0;
+  if (tid == 0) {
+    const grpo_top_row r = finish_row(a, t, tau, M, S, Tsum);
+    sm.log_sum = r.log_sum;
+    store_row<Tin>(a, t, r);
+  }
+  if (n == 0) return;
+  __syncthreads();
+  TopOut out;
+  const int64_t at = (int64_t)t * n;
+  out.ids = a.ids ? a.ids + at : nullptr;
+  out.logp = a.top_logp ? a.top_logp + at : nullptr;
+  out.keys = nullptr;
+  out.max = M;
+  out.tau = tau;
+  out.log_sum = sm.log_sum;
+  out.c0 = 0;
+  if (!some) {
+    if (tid < n) out.none(tid, bad);
+    return;
+  }
+  if (tid < 64) {
+    uint32_t k[kTopCap / 64];
+#pragma unroll
+    for (int i = 0; i < kTopCap / 64; ++i) k[i] = tid + 64 * i < c ? (uint32_t)(sm.all[tid + 64 * i] >> 48) : 0u;
+    const uint32_t p = nth_largest(k, n);
+    if (tid == 0) sm.bound = p;
+  }
+  __syncthreads();
+  const uint32_t bound = sm.bound;
+  for (int i = tid; i < c; i += kJoinNT) {
+    const uint64_t key = sm.all[i];
+    if (key != kNothing && (uint32_t)(key >> 48) >= bound) sm.list[atomicAdd(&sm.count, 1)] = key;
+  }
+  __syncthreads();
+  rank_list<kJoinNT>(sm, sm.count, n, out);
+}
+
+// ---- the gradient ---------------------------------------------------------------
+struct TopBwdArgs {
+  const void* logits;
+  void* dlogits;
+  int64_t ld;
+  int V, blocks;  // blocks of columns to a row
+  int n;
+  const int32_t* actions;
+  const int32_t* ids;
+  const grpo_top_row* rows;
+  const float* dlogp;
+  const float* dent;
+  const float* dtop;
+};
+
+constexpr int kTopBwdNT = 256, kTopBwdCols = 8192;
+
+// One workgroup to kTopBwdCols columns of a row.  A word's log2 p is formed from z - max, which keeps the exponent's
+// rounding small whatever max and tau are.
+template <typename Tin>
+__global__ __launch_bounds__(kTopBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_top_bwd(const TopBwdArgs a,
+                                                                                                int row0) {
+  constexpr int NT = kTopBwdNT, EPV = 16 / (int)sizeof(Tin), U = kTopBwdCols / NT / EPV;
+  typedef typename VecAt<Tin>::type u32x4_any;
+  __shared__ int sh_id[GRPO_TOP_MAX];
+  __shared__ float sh_c[GRPO_TOP_MAX];
+  __shared__ double sh_sum;
+  __shared__ int sh_col[GRPO_TOP_MAX + 1];  // this workgroup's words with a coefficient, and their gradients
+  __shared__ float sh_d[GRPO_TOP_MAX + 1];
+  __shared__ int sh_count;
+  const int t = row0 + (int)(blockIdx.x / (unsigned)a.blocks), b = (int)(blockIdx.x % (unsigned)a.blocks);
+  const int tid = threadIdx.x, n = a.n;
+  const Tin* row = static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld;
+  Tin* drow = static_cast<Tin*>(a.dlogits) + (int64_t)t * a.ld;
+  const int c0 = b * kTopBwdCols, edge = a.V / EPV * EPV;
+  const int n_edge = b == a.blocks - 1 ? a.V - edge : 0;
+  u32x4 x[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int col = c0 + (i * NT + tid) * EPV;
+    if (col + EPV <= a.V) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + col));
+  }
+  const float ez = tid < n_edge ? load_elem(row + edge + tid) : 0.f;
+  const grpo_top_row r = a.rows[t];
+  const int act = a.actions[t];
+  const bool nan = isnan(r.log_sum), none = r.max == -INFINITY;
+  const bool act_on = a.dlogp && act >= 0 && act < a.V && r.logp > -INFINITY;
+  const float d_act = act_on ? a.dlogp[t] : 0.f;
+  if (tid < 64) {
+    int id = -1;
+    float c = 0.f;
+    if (tid < n) {
+      id = a.ids[(int64_t)t * n + tid];
+      if (id >= 0 && id < a.V) c = a.dtop ? a.dtop[(int64_t)t * n + tid] : 0.f;
+      else id = -1;
+    }
+    sh_id[tid] = id;
+    sh_c[tid] = c;
+    const double sum = wave_sum_dpp((double)c);
+    if (tid == 0) {
+      sh_sum = sum + (double)d_act;
+      sh_count = 0;
+    }
+  }
+  __syncthreads();
+  const double C = sh_sum, g = a.dent ? (double)a.dent[t] : 0.0, inv = 1.0 / (double)r.temperature;
+  // the words with a coefficient of their own in these columns, each once, in fp64
+  if (tid <= n && !nan && !none) {
+    int id = -1;
+    double c = 0.0;
+    if (tid < n) {
+      id = sh_id[tid];
+      for (int j = 0; j < n; ++j) {
+        if (sh_id[j] != id) continue;
+        if (j < tid) id = -2;  // an earlier one of the same word does it
+        c += (double)sh_c[j];
+      }
+      if (act_on && id == act) c += (double)d_act;
+    } else if (act_on) {
+      id = act;
+      c = (double)d_act;
+      for (int j = 0; j < n; ++j)
+        if (sh_id[j] == act) id = -1;
+    }
+    if (id >= c0 && id < min(c0 + kTopBwdCols, a.V)) {
+      const float z = load_elem(row + id);
+      double d = 0.0;
+      if (is_word(z)) {
+        const double lp = ((double)z - (double)r.max) * inv - r.log_sum;
+        d = (c - exp(lp) * (C + g * (lp + (double)r.entropy))) * inv;
+      }
+      const int i = atomicAdd(&sh_count, 1);
+      sh_col[i] = id;
+      sh_d[i] = (float)d;
+    }
+  }
+  __syncthreads();
+  auto store = [&](auto value) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int col = c0 + (i * NT + tid) * EPV;
+      if (col + EPV <= a.V) {
+        u32x4 o;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if constexpr (sizeof(Tin) == 2) o[q] = pack_bf16(value(bf16_lo(x[i][q])), value(bf16_hi(x[i][q])));
+          else o[q] = __float_as_uint(value(__uint_as_float(x[i][q])));
+        }
+        __builtin_nontemporal_store(o, reinterpret_cast<u32x4_any*>(drow + col));
+        asm volatile("s_nop 1" ::: "memory");  // the store has read its data before its registers are reused
+      }
+    }
+    if (tid < n_edge) store_elem(drow + edge + tid, value(ez));
+  };
+  if (nan || none) {
+    const float v = nan ? NAN : 0.f;
+    store([&](float) { return v; });
+    return;
+  }
+  // p (A log2 p + B)
+  const float sc = kLog2e / r.temperature, l2 = (float)(r.log_sum / kLn2), top = r.max;
+  const float A = (float)(-g * kLn2 * inv), B = (float)(-(C + g * (double)r.entropy) * inv);
+  store([&](float z) {
+    const float w = z <= kShiftMin ? -200.f : fmaf(z - top, sc, -l2);
+    return __builtin_amdgcn_exp2f(w) * fmaf(w, A, B);
+  });
+  // by the thread that stored the word's place, after that store
+  const int count = sh_count;
+  for (int i = 0; i < count; ++i) {
+    const int col = sh_col[i];
+    if (tid == (col >= edge ? col - edge : (col - c0) / EPV % NT)) store_elem(drow + col, sh_d[i]);
+  }
+}
+
+__global__ void k_clear_top_flag(int32_t* f) { *f = 0; }
+
+// ---- host -----------------------------------------------------------------------
+
+static bool bad_top_shape(int64_t T, int64_t V, int64_t ld, int32_t n) {
+  return T < 0 || T >= ((int64_t)1 << 31) || V < 1 || V > GRPO_TOP_MAX_V || ld < V || n < 0 || n > GRPO_TOP_MAX;
+}
+
+// How many workgroups a row goes to.
+struct TopPlan {
+  int parts, cols;
+};
+static TopPlan top_plan(int64_t T, int64_t V, int32_t n) {
+  TopPlan p{1, (int)V};
+  if (T <= 0 || T >= 128 || V <= 16384) return p;
+  int64_t parts = std::min<int64_t>(V / 8192, 256 / T);
+  parts = std::min<int64_t>(parts, n ? kTopCap / n : kTopCap);
+  if (parts < 2) return p;
+  p.cols = (int)(((V + parts - 1) / parts + 7) / 8 * 8);
+  p.parts = (int)((V + p.cols - 1) / p.cols);
+  return p;
+}
+
+static size_t top_part_bytes(int64_t T, const TopPlan& p) { return align_up(sizeof(TopPart) * (size_t)T * p.parts); }
+
+constexpr int64_t kTopRowsPerLaunch = 1 << 20;  // a launch's threads stay below 2^32
+
+template <typename Tin, int NT, int U>
+static void launch_top_rows(const TopArgs& a, int64_t T, hipStream_t s) {
+  for (int64_t r = 0; r < T; r += kTopRowsPerLaunch)
+    hipLaunchKernelGGL((k_top<Tin, NT, U, false>), dim3((unsigned)std::min(kTopRowsPerLaunch, T - r)), dim3(NT), 0, s, a,
+                       (int)r);
+}
+
+template <typename Tin>
+static void launch_top(const TopArgs& a, int64_t T, hipStream_t s) {
+  if (a.parts > 1) {
+    hipLaunchKernelGGL((k_top<Tin, 256, 4, true>), dim3((unsigned)(T * a.parts)), dim3(256), 0, s, a, 0);
+    hipLaunchKernelGGL(k_top_join<Tin>, dim3((unsigned)T), dim3(kJoinNT), 0, s, a);
+    return;
+  }
+  const int64_t vecs = a.V / (16 / (int64_t)sizeof(Tin));
+  if (vecs <= 2048) launch_top_rows<Tin, 256, 4>(a, T, s);
+  else if (vecs <= 8192) launch_top_rows<Tin, 512, 4>(a, T, s);
+  else launch_top_rows<Tin, 1024, 4>(a, T, s);
+}
+
+}  // namespace grpo
+
+using namespace grpo;
+
+extern "C" size_t grpo_token_logp_top_workspace_bytes(int64_t T, int64_t V, int32_t n) {
+  if (bad_top_shape(T, V, V, n)) return 0;
+  const TopPlan p = top_plan(T, V, n);
+  return p.parts == 1 ? 0 : top_part_bytes(T, p) + align_up(sizeof(uint64_t) * (size_t)T * p.parts * n);
+}
+
+extern "C" int grpo_token_logp_top(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                                   const float* temperature, float temperature_all, const int32_t* actions, int32_t n,
+                                   float* logp, float* entropy, int32_t* top_ids, float* top_logp, grpo_top_row* rows,
+                                   int32_t* error_flags, void* ws, size_t ws_bytes, hipStream_t s) {
+  if (bad_top_shape(T, V, ld, n)) return GRPO_ERR_SHAPE;
+  if (T > 0 && (!logits || !actions)) return GRPO_ERR_ARG;
+  if (!temperature && !(temperature_all >= 1e-6f && temperature_all <= 1e6f)) return GRPO_ERR_ARG;
+  if (dtype != GRPO_F32 && dtype != GRPO_BF16) return GRPO_ERR_DTYPE;
+  if (!aligned(logits, dtype == GRPO_BF16 ? 2 : 4) || !aligned(temperature, 4) || !aligned(actions, 4) ||
+      !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(top_ids, 4) || !aligned(top_logp, 4) || !aligned(rows, 8) ||
+      !aligned(error_flags, 4))
+    return GRPO_ERR_ALIGN;
+  const TopPlan p = top_plan(T, V, n);
+  if (p.parts > 1) {
+    if (!ws || ws_bytes < grpo_token_logp_top_workspace_bytes(T, V, n)) return GRPO_ERR_WORKSPACE;
+    if (!aligned(ws, 16)) return GRPO_ERR_ALIGN;
+  }
+  if (error_flags) hipLaunchKernelGGL(k_clear_top_flag, dim3(1), dim3(1), 0, s, error_flags);
+  if (T > 0) {
+    TopArgs a{logits, ld, (int)V, n, temperature, temperature_all, actions, logp, entropy, top_ids, top_logp, rows,
+              error_flags, p.parts, p.cols, nullptr, nullptr};
+    if (!top_ids && !top_logp) a.n = 0;
+    if (p.parts > 1) {
+      a.part = static_cast<TopPart*>(ws);
+      a.part_keys = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + top_part_bytes(T, p));
+    }
+    if (dtype == GRPO_BF16) launch_top<uint16_t>(a, T, s);
+    else launch_top<float>(a, T, s);
+  }
+  return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+}
+
+extern "C" int grpo_token_logp_top_bwd(const void* logits, int32_t dtype, int64_t T, int64_t V, int64_t ld,
+                                       const int32_t* actions, int32_t n, const int32_t* top_ids,
+                                       const grpo_top_row* rows, const float* dlogp, const float* dentropy,
+                                       const float* dtop, void* dlogits, hipStream_t s) {
+  if (bad_top_shape(T, V, ld, n)) return GRPO_ERR_SHAPE;
+  if (T > 0 && (!logits || !actions || !rows || !dlogits || (dtop && n > 0 && !top_ids))) return GRPO_ERR_ARG;
+  if (dtype != GRPO_F32 && dtype != GRPO_BF16) return GRPO_ERR_DTYPE;
+  const size_t esz = dtype == GRPO_BF16 ? 2 : 4;
+  if (!aligned(logits, esz) || !aligned(dlogits, esz) || !aligned(actions, 4) || !aligned(top_ids, 4) ||
+      !aligned(rows, 8) || !aligned(dlogp, 4) || !aligned(dentropy, 4) || !aligned(dtop, 4))
+    return GRPO_ERR_ALIGN;
+  if (T > 0 && rows_overlap(logits, dlogits, T, V, ld, esz)) return GRPO_ERR_ARG;
+  const int blocks = (int)((V + kTopBwdCols - 1) / kTopBwdCols);
+  const int64_t per = std::max<int64_t>(1, ((int64_t)1 << 23) / blocks);  // a launch's threads stay below 2^32
+  for (int64_t r = 0; r < T; r += per) {
+    const TopBwdArgs a{logits, dlogits, ld, (int)V, blocks, dtop ? n : 0, actions, top_ids, rows, dlogp, dentropy, dtop};
+    const unsigned grid = (unsigned)(std::min(per, T - r) * blocks);
+    if (dtype == GRPO_BF16) hipLaunchKernelGGL(k_top_bwd<uint16_t>, dim3(grid), dim3(kTopBwdNT), 0, s, a, (int)r);
+    else hipLaunchKernelGGL(k_top_bwd<float>, dim3(grid), dim3(kTopBwdNT), 0, s, a, (int)r);
+  }
+  return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+}
