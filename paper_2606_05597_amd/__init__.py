@@ -26,6 +26,7 @@ __all__ = ["grpo_advantages", "grpo_advantages_ex", "grpo_loss_workspace_bytes",
            "vocab_shard_logits_buffer", "GrpoLoss", "FusedLmHeadGrpoLoss", "loss",
            "fused_lmhead_token_logp", "grpo_sample", "grpo_sampled_logp", "grpo_sampled_logp_bwd", "SampledLogp",
            "grpo_token_logp_top", "grpo_token_logp_top_bwd", "TokenLogpTop",
+           "grpo_linear", "grpo_linear_bwd", "Linear",
            "GradList", "grpo_grad_sumsq", "grpo_grad_clip", "grpo_clip_grad_norm_",
            "grpo_status_str", "LossAux", "GrpoError"]
 
@@ -638,5 +639,6 @@ def fused_lmhead_grpo_vocab_shard(hidden: torch.Tensor, w_shard: torch.Tensor, s
 
 from .sampling import grpo_sample, grpo_sampled_logp, grpo_sampled_logp_bwd  # noqa: E402  (need the helpers above)
 from .top import grpo_token_logp_top, grpo_token_logp_top_bwd  # noqa: E402
+from .linear import grpo_linear, grpo_linear_bwd  # noqa: E402
 from .clip import GradList, grpo_clip_grad_norm_, grpo_grad_clip, grpo_grad_sumsq  # noqa: E402
-from .autograd import FusedLmHeadGrpoLoss, GrpoLoss, SampledLogp, TokenLogpTop  # noqa: E402
+from .autograd import FusedLmHeadGrpoLoss, GrpoLoss, Linear, SampledLogp, TokenLogpTop  # noqa: E402

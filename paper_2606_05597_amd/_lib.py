@@ -33,6 +33,12 @@ GRPO_SAMPLING_MAX_V = 4194304
 GRPO_GRAD_PARTIALS = 2048
 GRPO_TOP_MAX = 64
 
+GRPO_ACT_NONE = 0
+GRPO_ACT_RELU = 1
+GRPO_ACT_GELU = 2
+GRPO_ACT_GELU_TANH = 3
+GRPO_ACT_SILU = 4
+
 P = ctypes.c_void_p
 
 
@@ -65,6 +71,16 @@ class Grad(ctypes.Structure):
 class GradLayout(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("in_place", ctypes.c_int32), ("units", ctypes.c_int64),
                 ("bytes", ctypes.c_int64)]
+
+
+class LinearOp(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("K", ctypes.c_int64), ("N", ctypes.c_int64), ("x", P), ("ldx", ctypes.c_int64),
+                ("w", P), ("ldw", ctypes.c_int64), ("w_out_in", ctypes.c_int32), ("act", ctypes.c_int32), ("bias", P),
+                ("bias_dtype", ctypes.c_int32)]
+
+
+class LinearGrads(ctypes.Structure):
+    _fields_ = [("dx", P), ("dw", P), ("dbias", P), ("dw_dtype", ctypes.c_int32), ("accumulate_dw", ctypes.c_int32)]
 
 
 class GrpoError(RuntimeError):
@@ -141,6 +157,15 @@ def load() -> ctypes.CDLL:
         lib.grpo_token_logp_top.restype = ctypes.c_int
         lib.grpo_token_logp_top_bwd.argtypes = [P, I32, I64, I64, I64, P, I32, P, P, P, P, P, P, P]
         lib.grpo_token_logp_top_bwd.restype = ctypes.c_int
+        op, grads = ctypes.POINTER(LinearOp), ctypes.POINTER(LinearGrads)
+        lib.grpo_linear_workspace_bytes.argtypes = [op]
+        lib.grpo_linear_workspace_bytes.restype = SZ
+        lib.grpo_linear.argtypes = [op, P, I64, P, I64, I32, P, P, SZ, P]
+        lib.grpo_linear.restype = ctypes.c_int
+        lib.grpo_linear_bwd_workspace_bytes.argtypes = [op, P, I64, I32, grads]
+        lib.grpo_linear_bwd_workspace_bytes.restype = SZ
+        lib.grpo_linear_bwd.argtypes = [op, P, I64, I32, P, grads, P, SZ, P]
+        lib.grpo_linear_bwd.restype = ctypes.c_int
         lib.grpo_grad_table_bytes.argtypes = [I32]
         lib.grpo_grad_table_bytes.restype = SZ
         lib.grpo_grad_table.argtypes = [ctypes.POINTER(Grad), I32, P, SZ, ctypes.POINTER(GradLayout)]

@@ -19,6 +19,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import _check, _lib, _ptr, _stream, fused_lmhead_grpo, fused_lmhead_grpo_blocked, grpo_loss_fwd_bwd
+from .linear import grpo_linear, grpo_linear_bwd
 from .sampling import grpo_sampled_logp, grpo_sampled_logp_bwd
 from .top import grpo_token_logp_top, grpo_token_logp_top_bwd
 
@@ -209,3 +210,41 @@ class TokenLogpTop(torch.autograd.Function):
         up = (None if t is None else t.contiguous() for t in (dlogp, dentropy, dtop))
         d = grpo_token_logp_top_bwd(logits, actions, ids, rows, *up, V=ctx.V, dlogits=_dlogits_like(logits, ctx.V))
         return d, None, None, None
+
+
+class Linear(torch.autograd.Function):
+    """``y = Linear.apply(x, w, bias, residual, opts)``
+
+    ``grpo_linear`` in a model: x bf16 [M, K], w bf16 [K, N] or the transpose of an [N, K] weight, bias [N] (bf16 or fp32)
+    or None, residual [M, N] of y's type or None; ``opts`` a dict of ``act`` and ``out_dtype``.  With an activation z is
+    kept in fp32 for backward, which runs on the stream that was current in forward.  The residual's gradient is the
+    incoming one.  Forward and backward can be captured into a graph together, while no eager autograd graph of the same
+    leaves is alive.
+    """
+
+    @staticmethod
+    def forward(ctx, x, w, bias=None, residual=None, opts=None):
+        opts = dict(opts or {})
+        ctx.act = opts.get("act", "none")
+        ctx.bias_dtype = None if bias is None else bias.dtype
+        unknown = set(opts) - {"act", "out_dtype"}
+        if unknown:
+            raise ValueError(f"unknown options: {sorted(unknown)}")
+        keep = ctx.act != "none" and any(ctx.needs_input_grad[:3])
+        y, z = grpo_linear(x.detach(), w.detach(), None if bias is None else bias.detach(),
+                           None if residual is None else residual.detach(), keep_z=keep, **opts)
+        ctx.save_for_backward(x, w, z)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, w, z = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(need[:3]):
+            if dy.dim() == 2 and dy.stride(1) != 1:
+                dy = dy.contiguous()
+            db = torch.empty(w.shape[1], dtype=ctx.bias_dtype, device=w.device) if need[2] else None
+            dx, dw, db = grpo_linear_bwd(dy, x, w, z, act=ctx.act, dx=bool(need[0]), dw=bool(need[1]), dbias=db)
+        return dx, dw, db, dy if need[3] else None, None

@@ -1,0 +1,508 @@
+// A product with bias, activation and residual in its epilogue, and its gradient (grpo_linear.h).
+//
+// Every product is the GEMM core of gemm.h, both operands with the summed dimension contiguous:
+//   y  [M, N] = x [M, K] . W as [N, K]        dx [M, K] = dz [M, N] . W as [K, N]
+//   dW [K, N] = x^T [K, M] . dz^T [N, M], or [N, K] with the two exchanged.
+// An operand that lies the other way, or whose rows are not whole aligned vectors of 16 bytes, is copied first.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "device.h"
+#include "gemm.h"
+#include "grpo_linear.h"
+#include "host.h"
+
+namespace grpo {
+
+// ---- activations ----------------------------------------------------------------
+__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+  if constexpr (ACT == GRPO_ACT_RELU) return z > 0.f || isnan(z) ? z : 0.f;
+  if constexpr (ACT == GRPO_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+  if constexpr (ACT == GRPO_ACT_GELU_TANH)
+    return 0.5f * z * (1.f + tanhf(0.79788456f * fmaf(0.044715f * z * z, z, z)));
+  if constexpr (ACT == GRPO_ACT_SILU) return z * sigmoid(z);
+  return z;
+}
+
+template <int ACT>
+__device__ __forceinline__ float slope_of(float z) {
+  if constexpr (ACT == GRPO_ACT_RELU) return z > 0.f ? 1.f : isnan(z) ? z : 0.f;
+  if constexpr (ACT == GRPO_ACT_GELU)
+    return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+  if constexpr (ACT == GRPO_ACT_GELU_TANH) {
+    const float t = tanhf(0.79788456f * fmaf(0.044715f * z * z, z, z));
+    return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.79788456f * fmaf(3.f * 0.044715f * z, z, 1.f);
+  }
+  if constexpr (ACT == GRPO_ACT_SILU) {
+    const float g = sigmoid(z);
+    return g * fmaf(z, 1.f - g, 1.f);
+  }
+  return 1.f;
+}
+
+__device__ __forceinline__ float load_any(const void* p, int64_t i, bool bf16) {
+  return bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store_any(void* p, int64_t i, float v, bool bf16) {
+  if (bf16) store_elem(static_cast<uint16_t*>(p) + i, v);
+  else static_cast<float*>(p)[i] = v;
+}
+
+// ---- the products ---------------------------------------------------------------
+struct Epilogue {
+  void* out;  // [M, N], rows ldo apart
+  int64_t ldo;
+  const void* bias;      // [N] or NULL
+  const void* residual;  // [M, N] of out's type, rows ldr apart, or NULL
+  int64_t ldr;
+  float* z;  // [M, N] or NULL
+  int act;
+  bool out_bf16, bias_bf16, accumulate;
+};
+
+struct ProductArgs {
+  GemmArgs g;
+  Epilogue e;
+};
+
+typedef GemmCfg<256, 256, 2, 4> LinCfg;
+
+// 8 columns of a row, at any alignment of their elements.
+__device__ __forceinline__ void load8(const void* p, int64_t i, bool bf16, float (&v)[8]) {
+  if (bf16) {
+    const u32x4 x = *reinterpret_cast<const u32x4_a2*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = elem<uint16_t>(x, q);
+  } else {
+    const u32x4_a4* x = reinterpret_cast<const u32x4_a4*>(static_cast<const float*>(p) + i);
+    const u32x4 a = x[0], b = x[1];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[q] = __uint_as_float(a[q]);
+      v[q + 4] = __uint_as_float(b[q]);
+    }
+  }
+}
+__device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const float (&v)[8]) {
+  if (bf16) {
+    u32x4 x;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = pack_bf16(v[2 * q], v[2 * q + 1]);
+    *reinterpret_cast<u32x4_a2*>(static_cast<uint16_t*>(p) + i) = x;
+  } else {
+    u32x4 a, b;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      a[q] = __float_as_uint(v[q]);
+      b[q] = __float_as_uint(v[q + 4]);
+    }
+    u32x4_a4* x = reinterpret_cast<u32x4_a4*>(static_cast<float*>(p) + i);
+    x[0] = a;
+    x[1] = b;
+  }
+  asm volatile("s_nop 1" ::: "memory");  // the stores have read their data before their registers are reused
+}
+
+// The epilogue of 8 sums v of row m, columns n .. n + 7 (those below N).
+template <int ACT>
+__device__ __forceinline__ void finish8(const Epilogue& e, int m, int n, int N, const float (&bias)[8], float (&v)[8]) {
+  const bool all = n + 8 <= N;
+  const int k = all ? 8 : N - n;
+  const int64_t o = (int64_t)m * e.ldo + n;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] += bias[q];
+  if (e.z) {
+    const int64_t oz = (int64_t)m * N + n;
+    if (all) store8(e.z, oz, false, v);
+    else
+      for (int q = 0; q < 8; ++q)
+        if (q < k) e.z[oz + q] = v[q];
+  }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = act_of<ACT>(v[q]);
+  const void* more = e.residual ? e.residual : e.accumulate ? e.out : nullptr;
+  if (more) {
+    const int64_t om = e.residual ? (int64_t)m * e.ldr + n : o;
+    float r[8];
+    if (all) load8(more, om, e.out_bf16, r);
+    else
+#pragma unroll
+      for (int q = 0; q < 8; ++q) r[q] = q < k ? load_any(more, om + q, e.out_bf16) : 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] += r[q];
+  }
+  if (all) store8(e.out, o, e.out_bf16, v);
+  else
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q < k) store_any(e.out, o + q, v[q], e.out_bf16);
+}
+
+typedef float lin_f32x4 __attribute__((ext_vector_type(4)));
+
+// What lanes of a wave stored to LDS before is what others of it read after.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A wave's sums, 32 rows at a time, through its own part of the LDS into rows of 16-byte vectors: out of the registers
+// they would be stored 64 bytes to a row.
+template <class C, int ACT>
+__device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, int M, int N,
+                                            const g_f32x16 (&acc)[C::IB][C::JB], float* lds) {
+  constexpr int LD = C::WTN + 4, LPR = C::WTN / 8, RPS = 64 / LPR;  // lanes to a row, rows to a step
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WGN, wn = wave % C::WGN;
+  float* mine = lds + wave * 32 * LD;
+  const int cl = lane % LPR * 8, n = n0 + wn * C::WTN + cl;
+  float bias[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) bias[q] = e.bias && n + q < N ? load_any(e.bias, n + q, e.bias_bf16) : 0.f;
+#pragma unroll
+  for (int i = 0; i < C::IB; ++i) {
+#pragma unroll
+    for (int j = 0; j < C::JB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mine[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * LD + j * 32 + (lane & 31)] = acc[i][j][r];
+    wave_order();
+#pragma unroll 1
+    for (int q = 0; q < 32; q += RPS) {
+      const int rl = q + lane / LPR, m = m0 + wm * C::WTM + i * 32 + rl;
+      if (m >= M || n >= N) continue;
+      float v[8];
+      const lin_f32x4* src = reinterpret_cast<const lin_f32x4*>(mine + rl * LD + cl);
+      const lin_f32x4 a = src[0], b = src[1];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = a[k];
+        v[k + 4] = b[k];
+      }
+      finish8<ACT>(e, m, n, N, bias, v);
+    }
+    wave_order();
+  }
+}
+
+template <int ACT>
+__global__ __launch_bounds__(LinCfg::NT) void k_linear(const ProductArgs p) {
+  typedef LinCfg C;
+  __shared__ __attribute__((aligned(16))) uint16_t lds[2 * C::STAGE];
+  static_assert(sizeof(float) * C::NW * 32 * (C::WTN + 4) <= sizeof(lds), "the epilogue's rows");
+  int tm, tn;
+  const int tiles_m = (p.g.M + C::BM - 1) / C::BM, tiles_n = (p.g.N + C::BN - 1) / C::BN;
+  if (!gemm_tile_of(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn)) return;
+  const int m0 = tm * C::BM, n0 = tn * C::BN;
+  g_f32x16 acc[C::IB][C::JB];
+  gemm_mainloop<C>(p.g, m0, n0, acc, lds);
+  __syncthreads();  // every wave's last reads are done
+  finish_tile<C, ACT>(p.e, m0, n0, p.g.M, p.g.N, acc, reinterpret_cast<float*>(lds));
+}
+
+typedef void (*ProductKernel)(const ProductArgs);
+static ProductKernel product_kernel(int act) {
+  switch (act) {
+    case GRPO_ACT_RELU: return k_linear<GRPO_ACT_RELU>;
+    case GRPO_ACT_GELU: return k_linear<GRPO_ACT_GELU>;
+    case GRPO_ACT_GELU_TANH: return k_linear<GRPO_ACT_GELU_TANH>;
+    case GRPO_ACT_SILU: return k_linear<GRPO_ACT_SILU>;
+    default: return k_linear<GRPO_ACT_NONE>;
+  }
+}
+
+// ---- operands laid out anew -----------------------------------------------------
+// dst [R, ldd] = src [R, C] (rows lds_ apart), zeros in columns C .. ldd - 1.
+__global__ __launch_bounds__(256) void k_lin_copy(const uint16_t* __restrict__ src, int64_t lds_, int R, int C,
+                                                  uint16_t* __restrict__ dst, int64_t ldd) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= ldd) return;
+  for (int r = blockIdx.y; r < R; r += gridDim.y) dst[r * ldd + c] = c < C ? src[r * lds_ + c] : (uint16_t)0;
+}
+
+// dst [C, ldd] = the transpose of src [R, C] (rows lds_ apart), zeros in columns R .. ldd - 1.
+__global__ __launch_bounds__(256) void k_lin_transpose(const uint16_t* __restrict__ src, int64_t lds_, int R, int C,
+                                                       uint16_t* __restrict__ dst, int64_t ldd) {
+  __shared__ uint16_t tile[64][66];
+  const int c0 = blockIdx.x * 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+  for (int r0 = blockIdx.y * 64; r0 < ldd; r0 += gridDim.y * 64) {
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const int r = r0 + ty + 4 * q, c = c0 + tx;
+      tile[ty + 4 * q][tx] = r < R && c < C ? src[r * lds_ + c] : (uint16_t)0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const int c = c0 + ty + 4 * q, r = r0 + tx;
+      if (c < C && r < ldd) dst[c * ldd + r] = tile[tx][ty + 4 * q];
+    }
+  }
+}
+
+// ---- dz -------------------------------------------------------------------------
+struct DzArgs {
+  const void* dy;  // [M, N], rows lddy apart
+  int64_t lddy;
+  const float* z;  // [M, N] or NULL (no activation)
+  uint16_t* dz;    // [M, lddz] or NULL, zeros past column N
+  int64_t lddz;
+  float* part;     // [blocks of rows][N] column sums, or NULL
+  int M, N;
+  bool dy_bf16;
+};
+constexpr int kDzRows = 128;  // rows whose column sums are one fp32 partial
+
+template <int ACT>
+__global__ __launch_bounds__(256) void k_lin_dz(const DzArgs a) {
+  const int n = blockIdx.x * 256 + threadIdx.x, blocks = (a.M + kDzRows - 1) / kDzRows;
+  for (int b = blockIdx.y; b < blocks; b += gridDim.y) {
+    const int end = min(a.M, (b + 1) * kDzRows);
+    float sum = 0.f;
+    for (int m = b * kDzRows; m < end; ++m) {
+      float v = 0.f;
+      if (n < a.N) {
+        v = load_any(a.dy, m * a.lddy + n, a.dy_bf16);
+        if (ACT != GRPO_ACT_NONE) v *= slope_of<ACT>(a.z[(int64_t)m * a.N + n]);
+      }
+      if (a.dz && n < a.lddz) store_elem(a.dz + m * a.lddz + n, v);
+      sum += v;
+    }
+    if (a.part && n < a.N) a.part[(int64_t)b * a.N + n] = sum;
+  }
+}
+
+typedef void (*DzKernel)(const DzArgs);
+static DzKernel dz_kernel(int act) {
+  switch (act) {
+    case GRPO_ACT_RELU: return k_lin_dz<GRPO_ACT_RELU>;
+    case GRPO_ACT_GELU: return k_lin_dz<GRPO_ACT_GELU>;
+    case GRPO_ACT_GELU_TANH: return k_lin_dz<GRPO_ACT_GELU_TANH>;
+    case GRPO_ACT_SILU: return k_lin_dz<GRPO_ACT_SILU>;
+    default: return k_lin_dz<GRPO_ACT_NONE>;
+  }
+}
+
+// dbias from the partial sums, added in fp64 in the order of the rows.
+__global__ __launch_bounds__(256) void k_lin_dbias(const float* __restrict__ part, int blocks, int N, void* dbias,
+                                                   bool bf16) {
+  const int n = blockIdx.x * 256 + threadIdx.x;
+  if (n >= N) return;
+  double sum = 0.0;
+  for (int b = 0; b < blocks; ++b) sum += (double)part[(int64_t)b * N + n];
+  store_any(dbias, n, (float)sum, bf16);
+}
+
+// ---- host -----------------------------------------------------------------------
+constexpr int64_t kMostLin = 8388352;  // 2^23 - 256: 256 rows of an operand stay below 4 GB
+
+static int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
+
+// Whether rows of C elements, ld apart, can be loaded as whole aligned vectors.
+static bool whole(const void* p, int64_t C, int64_t ld) {
+  return C % 8 == 0 && ld % 8 == 0 && ld <= kMostLin && aligned(p, 16);
+}
+
+// An operand of a product as it will be read: [rows, cols], cols summed over.
+struct Operand {
+  const uint16_t* src;
+  int64_t ld, rows, cols;
+  bool turned;  // src is [cols, rows]
+  bool copied() const { return turned || !whole(src, cols, ld); }
+  size_t bytes() const { return copied() ? align_up(2 * (size_t)rows * (size_t)up8(cols)) : 0; }
+};
+
+static const uint16_t* lay_out(const Operand& o, char*& ws, int64_t& ld, hipStream_t s) {
+  if (!o.copied()) {
+    ld = o.ld;
+    return o.src;
+  }
+  uint16_t* dst = reinterpret_cast<uint16_t*>(ws);
+  ws += o.bytes();
+  ld = up8(o.cols);
+  const unsigned most = 16384;
+  if (o.turned)
+    hipLaunchKernelGGL(k_lin_transpose, dim3((unsigned)((o.rows + 63) / 64), std::min(most, (unsigned)((ld + 63) / 64))),
+                       dim3(256), 0, s, o.src, o.ld, (int)o.cols, (int)o.rows, dst, ld);
+  else
+    hipLaunchKernelGGL(k_lin_copy, dim3((unsigned)((ld + 255) / 256), std::min(most, (unsigned)o.rows)), dim3(256), 0, s,
+                       o.src, o.ld, (int)o.rows, (int)o.cols, dst, ld);
+  return dst;
+}
+
+// C [a.rows, b.rows] = A B^T with the epilogue e.
+static void launch_product(const Operand& a, const Operand& b, const Epilogue& e, char*& ws, hipStream_t s) {
+  ProductArgs p;
+  p.g.A = lay_out(a, ws, p.g.lda, s);
+  p.g.B = lay_out(b, ws, p.g.ldb, s);
+  p.g.M = (int)a.rows;
+  p.g.N = (int)b.rows;
+  p.g.K = (int)up8(a.cols);
+  p.e = e;
+  const int64_t tiles = ((a.rows + LinCfg::BM - 1) / LinCfg::BM) * ((b.rows + LinCfg::BN - 1) / LinCfg::BN);
+  hipLaunchKernelGGL(product_kernel(e.act), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(LinCfg::NT), 0, s, p);
+}
+
+static bool is_dtype(int32_t d) { return d == GRPO_F32 || d == GRPO_BF16; }
+static size_t size_of(int32_t d) { return d == GRPO_BF16 ? 2 : 4; }
+
+static int check_op(const grpo_linear_op* op) {
+  if (!op || op->act < GRPO_ACT_NONE || op->act > GRPO_ACT_SILU || (op->w_out_in != 0 && op->w_out_in != 1))
+    return GRPO_ERR_ARG;
+  if (op->M < 0 || op->M > kMostLin || op->K < 1 || op->K > kMostLin || op->N < 1 || op->N > kMostLin ||
+      op->ldx < op->K || op->ldw < (op->w_out_in ? op->K : op->N))
+    return GRPO_ERR_SHAPE;
+  return GRPO_OK;
+}
+
+static Operand x_rows(const grpo_linear_op& op) {
+  return Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.M, op.K, false};
+}
+static Operand w_as_nk(const grpo_linear_op& op) {
+  return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.N, op.K, op.w_out_in == 0};
+}
+static Operand w_as_kn(const grpo_linear_op& op) {
+  return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.K, op.N, op.w_out_in == 1};
+}
+
+// What the backward call does and keeps.
+struct BwdPlan {
+  bool make_dz;  // dz is not dy as it lies
+  size_t dz, part;
+  Operand dz_rows, dz_cols, x_cols, w;
+  size_t total;
+};
+static BwdPlan bwd_plan(const grpo_linear_op& op, const void* dy, int64_t lddy, int32_t dy_dtype,
+                        const grpo_linear_grads& g) {
+  BwdPlan p{};
+  const bool products = g.dx || g.dw;
+  p.make_dz = products && (op.act != GRPO_ACT_NONE || dy_dtype != GRPO_BF16 || !whole(dy, op.N, lddy));
+  p.dz = p.make_dz ? align_up(2 * (size_t)op.M * (size_t)up8(op.N)) : 0;
+  p.part = g.dbias ? align_up(4 * (size_t)((op.M + kDzRows - 1) / kDzRows) * (size_t)op.N) : 0;
+  const uint16_t* dz = static_cast<const uint16_t*>(dy);
+  const int64_t ld = p.make_dz ? up8(op.N) : lddy;
+  p.dz_rows = Operand{dz, ld, op.M, op.N, false};
+  p.dz_cols = Operand{dz, ld, op.N, op.M, true};
+  p.x_cols = Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.K, op.M, true};
+  p.w = w_as_kn(op);
+  p.total = p.dz + p.part;
+  if (g.dx) p.total += p.w.bytes();
+  if (g.dw) p.total += p.dz_cols.bytes() + p.x_cols.bytes();
+  return p;
+}
+
+static int check_bwd(const grpo_linear_op* op, int64_t lddy, int32_t dy_dtype, const grpo_linear_grads* g) {
+  const int st = check_op(op);
+  if (st != GRPO_OK) return st;
+  if (!g || (g->accumulate_dw != 0 && g->accumulate_dw != 1)) return GRPO_ERR_ARG;
+  if (lddy < op->N) return GRPO_ERR_SHAPE;
+  if (!is_dtype(dy_dtype) || (g->dw && !is_dtype(g->dw_dtype)) || (g->dbias && !is_dtype(op->bias_dtype)))
+    return GRPO_ERR_DTYPE;
+  if (g->dw && g->accumulate_dw && g->dw_dtype != GRPO_F32) return GRPO_ERR_ARG;
+  return GRPO_OK;
+}
+
+// n elements of 2 bytes.
+__global__ __launch_bounds__(256) void k_lin_zero(uint16_t* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+static void zero_fill(void* p, int64_t n, size_t esz, hipStream_t s) {
+  n *= (int64_t)(esz / 2);
+  hipLaunchKernelGGL(k_lin_zero, dim3((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), dim3(256), 0, s,
+                     static_cast<uint16_t*>(p), n);
+}
+
+}  // namespace grpo
+
+using namespace grpo;
+
+extern "C" size_t grpo_linear_workspace_bytes(const grpo_linear_op* op) {
+  if (check_op(op) != GRPO_OK || op->M == 0) return 0;
+  return x_rows(*op).bytes() + w_as_nk(*op).bytes();
+}
+
+extern "C" int grpo_linear(const grpo_linear_op* op, const void* residual, int64_t ldr, void* y, int64_t ldy,
+                           int32_t y_dtype, float* z, void* ws, size_t ws_bytes, hipStream_t s) {
+  const int st = check_op(op);
+  if (st != GRPO_OK) return st;
+  if (op->M > 0 && (!op->x || !op->w || !y)) return GRPO_ERR_ARG;
+  if (ldy < op->N || (residual && ldr < op->N)) return GRPO_ERR_SHAPE;
+  if (!is_dtype(y_dtype) || (op->bias && !is_dtype(op->bias_dtype))) return GRPO_ERR_DTYPE;
+  if (!aligned(op->x, 2) || !aligned(op->w, 2) || !aligned(y, size_of(y_dtype)) || !aligned(z, 4) ||
+      !aligned(residual, size_of(y_dtype)) || (op->bias && !aligned(op->bias, size_of(op->bias_dtype))))
+    return GRPO_ERR_ALIGN;
+  if (residual == y && residual && ldr != ldy) return GRPO_ERR_ARG;
+  const size_t need = grpo_linear_workspace_bytes(op);
+  if (need > 0) {
+    if (!ws || ws_bytes < need) return GRPO_ERR_WORKSPACE;
+    if (!aligned(ws, 16)) return GRPO_ERR_ALIGN;
+  }
+  if (op->M > 0) {
+    char* at = static_cast<char*>(ws);
+    const Epilogue e{y, ldy, op->bias, residual, ldr, z, op->act, y_dtype == GRPO_BF16, op->bias_dtype == GRPO_BF16, false};
+    launch_product(x_rows(*op), w_as_nk(*op), e, at, s);
+  }
+  return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+}
+
+extern "C" size_t grpo_linear_bwd_workspace_bytes(const grpo_linear_op* op, const void* dy, int64_t lddy,
+                                                  int32_t dy_dtype, const grpo_linear_grads* grads) {
+  if (check_bwd(op, lddy, dy_dtype, grads) != GRPO_OK || op->M == 0) return 0;
+  return bwd_plan(*op, dy, lddy, dy_dtype, *grads).total;
+}
+
+extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t lddy, int32_t dy_dtype, const float* z,
+                               const grpo_linear_grads* grads, void* ws, size_t ws_bytes, hipStream_t s) {
+  const int st = check_bwd(op, lddy, dy_dtype, grads);
+  if (st != GRPO_OK) return st;
+  const grpo_linear_grads& g = *grads;
+  const bool act = op->act != GRPO_ACT_NONE, work = g.dx || g.dw || g.dbias;
+  if (op->M > 0 && work && (!dy || (act && !z))) return GRPO_ERR_ARG;
+  if (op->M > 0 && ((g.dx && !op->w) || (g.dw && !op->x))) return GRPO_ERR_ARG;
+  if (!aligned(op->x, 2) || !aligned(op->w, 2) || !aligned(dy, size_of(dy_dtype)) || !aligned(z, 4) || !aligned(g.dx, 2) ||
+      (g.dw && !aligned(g.dw, size_of(g.dw_dtype))) || (g.dbias && !aligned(g.dbias, size_of(op->bias_dtype))))
+    return GRPO_ERR_ALIGN;
+  const size_t need = grpo_linear_bwd_workspace_bytes(op, dy, lddy, dy_dtype, grads);
+  if (need > 0) {
+    if (!ws || ws_bytes < need) return GRPO_ERR_WORKSPACE;
+    if (!aligned(ws, 16)) return GRPO_ERR_ALIGN;
+  }
+  if (op->M == 0) {
+    if (g.dw && !g.accumulate_dw) zero_fill(g.dw, op->K * op->N, size_of(g.dw_dtype), s);
+    if (g.dbias) zero_fill(g.dbias, op->N, size_of(op->bias_dtype), s);
+    return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+  }
+  BwdPlan p = bwd_plan(*op, dy, lddy, dy_dtype, g);
+  char* at = static_cast<char*>(ws);
+  uint16_t* dz = p.make_dz ? reinterpret_cast<uint16_t*>(at) : nullptr;
+  at += p.dz;
+  float* part = g.dbias ? reinterpret_cast<float*>(at) : nullptr;
+  at += p.part;
+  if (dz || part) {
+    const int blocks = (int)((op->M + kDzRows - 1) / kDzRows);
+    const DzArgs a{dy, lddy, act ? z : nullptr, dz, up8(op->N), part, (int)op->M, (int)op->N, dy_dtype == GRPO_BF16};
+    hipLaunchKernelGGL(dz_kernel(op->act), dim3((unsigned)((up8(op->N) + 255) / 256), (unsigned)std::min(blocks, 16384)), dim3(256), 0,
+                       s, a);
+    if (part)
+      hipLaunchKernelGGL(k_lin_dbias, dim3((unsigned)((op->N + 255) / 256)), dim3(256), 0, s, part, blocks, (int)op->N,
+                         g.dbias, op->bias_dtype == GRPO_BF16);
+  }
+  if (dz) p.dz_rows.src = p.dz_cols.src = dz;
+  // dz's padding columns are zeros, so that W's may be anything: both are summed over whole vectors
+  if (dz) p.dz_rows.cols = p.dz_rows.ld;
+  if (g.dx) {
+    const Epilogue e{g.dx, op->K, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE, true, false, false};
+    launch_product(p.dz_rows, p.w, e, at, s);
+  }
+  if (g.dw) {
+    const Epilogue e{g.dw, op->w_out_in ? op->K : op->N, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE,
+                     g.dw_dtype == GRPO_BF16, false, g.accumulate_dw == 1};
+    launch_product(op->w_out_in ? p.dz_cols : p.x_cols, op->w_out_in ? p.x_cols : p.dz_cols, e, at, s);
+  }
+  return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+}
