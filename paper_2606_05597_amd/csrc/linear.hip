@@ -8,6 +8,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "gemm.h"
@@ -215,6 +216,206 @@ static ProductKernel product_kernel(int act) {
   }
 }
 
+// ---- few rows ---------------------------------------------------------------------
+// Up to 32 rows: a product is then as long as reading W once takes.  A wave goes down its part of the summed dimension, 32
+// at a time, over 128 outputs, W's vectors from memory straight into the operands of v_mfma_f32_16x16x32_bf16 (a lane: 8
+// consecutive k of one column):
+//   rows of W along the outputs (KN): a lane reads 8 columns of 8 rows and turns them in its registers (v_perm), so that
+//     fragment c holds its column c;
+//   rows along the summed dimension: a lane reads 8 k of a row, fragment c of row 8 (lane % 16) + c.
+// Either way a lane ends with 8 consecutive outputs.  The waves of a workgroup, each with its part of the sum, are added
+// through the LDS in their order.  W's rows may start at any element.
+typedef float lin_acc4 __attribute__((ext_vector_type(4)));
+
+struct FewArgs {
+  const uint16_t* x;  // [M, K]
+  const uint16_t* w;
+  int64_t ldx, ldw;
+  int M, K, N;
+  int strips;     // of 128 outputs
+  int splits;     // workgroups that share a strip's sum; > 1: their sums go to part [splits][M][N]
+  int wave_k;     // summed over by a wave, a multiple of 32
+  float* part;
+  Epilogue e;
+};
+
+constexpr int kFewWaves = 8, kFewCols = 128, kFewRows = 32;
+
+template <int ACT, bool PART>
+__device__ __forceinline__ void few_out(const FewArgs& a, int split, int m, int n, float (&v)[8]) {
+  if constexpr (PART) {
+    float* o = a.part + ((int64_t)split * a.M + m) * a.N + n;
+    if (n + 8 <= a.N) store8(o, 0, false, v);
+    else
+      for (int q = 0; q < 8; ++q)
+        if (n + q < a.N) o[q] = v[q];
+  } else {
+    float bias[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) bias[q] = a.e.bias && n + q < a.N ? load_any(a.e.bias, n + q, a.e.bias_bf16) : 0.f;
+    finish8<ACT>(a.e, m, n, a.N, bias, v);
+  }
+}
+
+// 8 elements p[0 .. 7], those from `left` on zeros and unread: the last 8 before p + left (which have to be there) moved down.
+__device__ __forceinline__ u32x4 load_vec(const uint16_t* p, int left) {
+  const int past = 8 - min(left, 8);
+  if (past >= 8) return u32x4{0u, 0u, 0u, 0u};
+  const u32x4 v = *reinterpret_cast<const u32x4_a2*>(p - past);
+  return __builtin_bit_cast(u32x4, __builtin_bit_cast(unsigned __int128, v) >> (16 * past));
+}
+
+template <int MB, bool KN, int ACT, bool PART>
+__global__ __launch_bounds__(64 * kFewWaves) void k_lin_few(const FewArgs a) {
+  __shared__ float red[kFewWaves][32][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int strip = blockIdx.x % a.strips, split = blockIdx.x / a.strips;
+  const int n = strip * kFewCols + 8 * (lane & 15);  // the lane's 8 outputs
+  const int kl = 8 * (lane >> 4);                    // and its place in a step
+  const int k0 = (split * kFewWaves + wave) * a.wave_k, k1 = min(k0 + a.wave_k, a.K);
+  lin_acc4 acc[MB][8];
+#pragma unroll
+  for (int b = 0; b < MB; ++b)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[b][c] = lin_acc4{0.f, 0.f, 0.f, 0.f};
+  // byte offsets from the strip's and step's start, which are the wave's alone
+  uint32_t xo[MB], wo[KN ? 1 : 8];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) xo[b] = 2u * ((uint32_t)min(16 * b + (lane & 15), a.M - 1) * (uint32_t)a.ldx + (uint32_t)kl);
+  // the lane's columns (KN: of N >= 8, the last 8 where fewer are left, computed twice) or rows of W
+  const uint16_t* wb = KN ? a.w : a.w + (int64_t)strip * kFewCols * a.ldw;
+  if constexpr (KN) {
+    wo[0] = 2u * ((uint32_t)kl * (uint32_t)a.ldw + (uint32_t)min(n, a.N - 8));
+  } else {
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      wo[c] = 2u * ((uint32_t)(min(n + c, a.N - 1) - strip * kFewCols) * (uint32_t)a.ldw + (uint32_t)kl);
+  }
+  auto w_at = [&](int c, int k) {
+    const uint16_t* base = KN ? wb + (int64_t)(k + c) * a.ldw : wb + k;
+    return reinterpret_cast<const uint16_t*>(reinterpret_cast<const char*>(base) + wo[KN ? 0 : c]);
+  };
+  auto x_at = [&](int b, int k) {
+    return reinterpret_cast<const uint16_t*>(reinterpret_cast<const char*>(a.x + k) + xo[b]);
+  };
+  auto multiply = [&](const u32x4 (&wv)[8], const u32x4 (&xv)[MB]) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      u32x4 f;
+      if constexpr (KN) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          f[j] = __builtin_amdgcn_perm(wv[2 * j + 1][c >> 1], wv[2 * j][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+      } else {
+        f = wv[c];
+      }
+#pragma unroll
+      for (int b = 0; b < MB; ++b)
+        acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(g_bf16x8, xv[b]),
+                                                            __builtin_bit_cast(g_bf16x8, f), acc[b][c], 0, 0, 0);
+    }
+  };
+  u32x4 w0[8], w1[8], x0[MB], x1[MB];
+  auto load = [&](u32x4 (&wv)[8], u32x4 (&xv)[MB], int k) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) wv[c] = *reinterpret_cast<const u32x4_a2*>(w_at(c, k));
+#pragma unroll
+    for (int b = 0; b < MB; ++b) xv[b] = *reinterpret_cast<const u32x4_a2*>(x_at(b, k));
+  };
+  const int steps = max(0, k1 - k0) / 32;
+  int k = k0, left = steps;
+  if (left > 0) load(w0, x0, k);
+  while (left >= 2) {
+    load(w1, x1, k + 32);
+    multiply(w0, x0);
+    if (left > 2) load(w0, x0, k + 64);
+    multiply(w1, x1);
+    k += 64;
+    left -= 2;
+  }
+  if (left) {
+    multiply(w0, x0);
+    k += 32;
+  }
+  if (k < k1) {  // the last, shorter step
+    const int rest = k1 - k - kl;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      if constexpr (KN) w0[c] = c < rest ? *reinterpret_cast<const u32x4_a2*>(w_at(c, k)) : u32x4{0u, 0u, 0u, 0u};
+      else w0[c] = load_vec(w_at(c, k), rest);
+    }
+#pragma unroll
+    for (int b = 0; b < MB; ++b) x0[b] = load_vec(x_at(b, k), rest);
+    multiply(w0, x0);
+  }
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    if (b) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) red[wave][r * 8 + c][lane] = acc[b][c][r];
+    __syncthreads();
+    // row 4 (l / 16) + r of the block, outputs of lane l
+    if (tid < 256) {
+      const int l = tid & 63, r = tid >> 6, m = 16 * b + 4 * (l >> 4) + r;
+      const int no = strip * kFewCols + 8 * (l & 15);
+      if (m < a.M && no < a.N) {
+        float v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          float sum = red[0][r * 8 + c][l];
+#pragma unroll
+          for (int q = 1; q < kFewWaves; ++q) sum += red[q][r * 8 + c][l];
+          v[c] = sum;
+        }
+        // columns computed from N - 8 on: the ones from `no` on
+        if (KN && no + 8 > a.N) {
+          float u[8];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            u[c] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+              if (d == c + no + 8 - a.N) u[c] = v[d];
+          }
+#pragma unroll
+          for (int c = 0; c < 8; ++c) v[c] = u[c];
+        }
+        few_out<ACT, PART>(a, split, m, no, v);
+      }
+    }
+  }
+}
+
+// The sums of the splits joined in their order, then the epilogue: a thread to 8 columns of a row.
+template <int ACT>
+__global__ __launch_bounds__(256) void k_lin_join(const float* __restrict__ part, int splits, int M, int N,
+                                                  const Epilogue e) {
+  const int per = (N + 7) / 8;
+  const int64_t total = (int64_t)M * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int m = (int)(i / per), n = (int)(i % per) * 8;
+    float v[8], bias[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      v[q] = 0.f;
+      bias[q] = e.bias && n + q < N ? load_any(e.bias, n + q, e.bias_bf16) : 0.f;
+    }
+    for (int s = 0; s < splits; ++s) {
+      const float* p = part + ((int64_t)s * M + m) * N + n;
+      float u[8];
+      if (n + 8 <= N) load8(p, 0, false, u);
+      else
+#pragma unroll
+        for (int q = 0; q < 8; ++q) u[q] = n + q < N ? p[q] : 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += u[q];
+    }
+    finish8<ACT>(e, m, n, N, bias, v);
+  }
+}
+
 // ---- operands laid out anew -----------------------------------------------------
 // dst [R, ldd] = src [R, C] (rows lds_ apart), zeros in columns C .. ldd - 1.
 __global__ __launch_bounds__(256) void k_lin_copy(const uint16_t* __restrict__ src, int64_t lds_, int R, int C,
@@ -313,7 +514,8 @@ struct Operand {
   const uint16_t* src;
   int64_t ld, rows, cols;
   bool turned;  // src is [cols, rows]
-  bool copied() const { return turned || !whole(src, cols, ld); }
+  bool padded;  // zeros from cols to a multiple of 8
+  bool copied() const { return turned || !whole(src, padded ? up8(cols) : cols, ld); }
   size_t bytes() const { return copied() ? align_up(2 * (size_t)rows * (size_t)up8(cols)) : 0; }
 };
 
@@ -335,8 +537,69 @@ static const uint16_t* lay_out(const Operand& o, char*& ws, int64_t& ld, hipStre
   return dst;
 }
 
+// How a product is done: by the kernel for few rows, in `splits` parts of the summed dimension, or by tiles.
+struct ProductPlan {
+  bool few;
+  int splits, wave_k;
+  size_t part;  // bytes of the splits' sums
+};
+static ProductPlan product_plan(const Operand& a, const Operand& b) {
+  ProductPlan p{};
+  p.splits = 1;
+  p.few = a.rows <= kFewRows && !a.turned && a.cols >= 8 && (!b.turned || b.rows >= 8);
+  if (!p.few) return p;
+  const int64_t K = a.cols, strips = (b.rows + kFewCols - 1) / kFewCols, steps = (K + 31) / 32;
+  // workgroups for the whole chip, of waves that have at least 4 steps each
+  const int64_t most = std::max<int64_t>(1, steps / (4 * kFewWaves));
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, 256 / strips, 16}));
+  const int64_t waves = (int64_t)p.splits * kFewWaves;
+  p.wave_k = (int)((steps + waves - 1) / waves * 32);
+  if (p.splits > 1) p.part = align_up(4 * (size_t)p.splits * (size_t)a.rows * (size_t)b.rows);
+  return p;
+}
+
+static size_t product_bytes(const Operand& a, const Operand& b) {
+  const ProductPlan p = product_plan(a, b);
+  return p.few ? p.part : a.bytes() + b.bytes();
+}
+
+template <int ACT>
+static void launch_few(const FewArgs& f, bool kn, hipStream_t s) {
+  const dim3 grid((unsigned)(f.strips * f.splits)), block(64 * kFewWaves);
+  auto go = [&](auto mb, auto is_kn) {
+    constexpr int MB = decltype(mb)::value;
+    constexpr bool KN = decltype(is_kn)::value;
+    if (f.splits > 1) hipLaunchKernelGGL((k_lin_few<MB, KN, GRPO_ACT_NONE, true>), grid, block, 0, s, f);
+    else hipLaunchKernelGGL((k_lin_few<MB, KN, ACT, false>), grid, block, 0, s, f);
+  };
+  auto rows = [&](auto mb) {
+    if (kn) go(mb, std::true_type());
+    else go(mb, std::false_type());
+  };
+  if (f.M <= 16) rows(std::integral_constant<int, 1>());
+  else rows(std::integral_constant<int, 2>());
+  if (f.splits > 1) {
+    const int64_t n = (int64_t)f.M * ((f.N + 7) / 8);
+    hipLaunchKernelGGL(k_lin_join<ACT>, dim3((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), dim3(256), 0, s, f.part,
+                       f.splits, f.M, f.N, f.e);
+  }
+}
+
 // C [a.rows, b.rows] = A B^T with the epilogue e.
 static void launch_product(const Operand& a, const Operand& b, const Epilogue& e, char*& ws, hipStream_t s) {
+  const ProductPlan plan = product_plan(a, b);
+  if (plan.few) {
+    const FewArgs f{a.src, b.src, a.ld, b.ld, (int)a.rows, (int)a.cols, (int)b.rows,
+                    (int)((b.rows + kFewCols - 1) / kFewCols), plan.splits, plan.wave_k, reinterpret_cast<float*>(ws), e};
+    ws += plan.part;
+    switch (e.act) {
+      case GRPO_ACT_RELU: return launch_few<GRPO_ACT_RELU>(f, b.turned, s);
+      case GRPO_ACT_GELU: return launch_few<GRPO_ACT_GELU>(f, b.turned, s);
+      case GRPO_ACT_GELU_TANH: return launch_few<GRPO_ACT_GELU_TANH>(f, b.turned, s);
+      case GRPO_ACT_SILU: return launch_few<GRPO_ACT_SILU>(f, b.turned, s);
+      default: return launch_few<GRPO_ACT_NONE>(f, b.turned, s);
+    }
+  }
   ProductArgs p;
   p.g.A = lay_out(a, ws, p.g.lda, s);
   p.g.B = lay_out(b, ws, p.g.ldb, s);
@@ -361,13 +624,13 @@ static int check_op(const grpo_linear_op* op) {
 }
 
 static Operand x_rows(const grpo_linear_op& op) {
-  return Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.M, op.K, false};
+  return Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.M, op.K, false, false};
 }
 static Operand w_as_nk(const grpo_linear_op& op) {
-  return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.N, op.K, op.w_out_in == 0};
+  return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.N, op.K, op.w_out_in == 0, false};
 }
 static Operand w_as_kn(const grpo_linear_op& op) {
-  return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.K, op.N, op.w_out_in == 1};
+  return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.K, op.N, op.w_out_in == 1, false};
 }
 
 // What the backward call does and keeps.
@@ -386,13 +649,13 @@ static BwdPlan bwd_plan(const grpo_linear_op& op, const void* dy, int64_t lddy, 
   p.part = g.dbias ? align_up(4 * (size_t)((op.M + kDzRows - 1) / kDzRows) * (size_t)op.N) : 0;
   const uint16_t* dz = static_cast<const uint16_t*>(dy);
   const int64_t ld = p.make_dz ? up8(op.N) : lddy;
-  p.dz_rows = Operand{dz, ld, op.M, op.N, false};
-  p.dz_cols = Operand{dz, ld, op.N, op.M, true};
-  p.x_cols = Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.K, op.M, true};
+  p.dz_rows = Operand{dz, ld, op.M, op.N, false, p.make_dz};
+  p.dz_cols = Operand{dz, ld, op.N, op.M, true, false};
+  p.x_cols = Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.K, op.M, true, false};
   p.w = w_as_kn(op);
   p.total = p.dz + p.part;
-  if (g.dx) p.total += p.w.bytes();
-  if (g.dw) p.total += p.dz_cols.bytes() + p.x_cols.bytes();
+  if (g.dx) p.total += product_bytes(p.dz_rows, p.w);
+  if (g.dw) p.total += product_bytes(op.w_out_in ? p.dz_cols : p.x_cols, op.w_out_in ? p.x_cols : p.dz_cols);
   return p;
 }
 
@@ -423,7 +686,7 @@ using namespace grpo;
 
 extern "C" size_t grpo_linear_workspace_bytes(const grpo_linear_op* op) {
   if (check_op(op) != GRPO_OK || op->M == 0) return 0;
-  return x_rows(*op).bytes() + w_as_nk(*op).bytes();
+  return product_bytes(x_rows(*op), w_as_nk(*op));
 }
 
 extern "C" int grpo_linear(const grpo_linear_op* op, const void* residual, int64_t ldr, void* y, int64_t ldy,
@@ -493,8 +756,6 @@ extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t
                          g.dbias, op->bias_dtype == GRPO_BF16);
   }
   if (dz) p.dz_rows.src = p.dz_cols.src = dz;
-  // dz's padding columns are zeros, so that W's may be anything: both are summed over whole vectors
-  if (dz) p.dz_rows.cols = p.dz_rows.ld;
   if (g.dx) {
     const Epilogue e{g.dx, op->K, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE, true, false, false};
     launch_product(p.dz_rows, p.w, e, at, s);
