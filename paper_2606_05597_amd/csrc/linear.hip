@@ -1,220 +1,21 @@
 // A product with bias, activation and residual in its epilogue, and its gradient (grpo_linear.h).
 //
-// Every product is the GEMM core of gemm.h, both operands with the summed dimension contiguous:
-//   y  [M, N] = x [M, K] . W as [N, K]        dx [M, K] = dz [M, N] . W as [K, N]
-//   dW [K, N] = x^T [K, M] . dz^T [N, M], or [N, K] with the two exchanged.
-// An operand that lies the other way, or whose rows are not whole aligned vectors of 16 bytes, is copied first.
+//   y  [M, N] = x W           dx [M, K] = dz W^T          dW [K, N] = x^T dz, or [N, K] = dz^T x
+// Few rows go to the kernel below, which is as fast as W can be read; everything else to tiles (linear_tiles.hip), which take
+// operands whichever way they lie.  Only where rows are not whole aligned vectors of 16 bytes is an operand copied for the
+// tiles.  A product with too few tiles for the chip is split along its sum, the splits' sums are joined by a launch of their
+// own.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
 #include <algorithm>
 #include <type_traits>
 
-#include "device.h"
 #include "gemm.h"
-#include "grpo_linear.h"
 #include "host.h"
+#include "linear.h"
 
 namespace grpo {
-
-// ---- activations ----------------------------------------------------------------
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
-
-template <int ACT>
-__device__ __forceinline__ float act_of(float z) {
-  if constexpr (ACT == GRPO_ACT_RELU) return z > 0.f || isnan(z) ? z : 0.f;
-  if constexpr (ACT == GRPO_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
-  if constexpr (ACT == GRPO_ACT_GELU_TANH)
-    return 0.5f * z * (1.f + tanhf(0.79788456f * fmaf(0.044715f * z * z, z, z)));
-  if constexpr (ACT == GRPO_ACT_SILU) return z * sigmoid(z);
-  return z;
-}
-
-template <int ACT>
-__device__ __forceinline__ float slope_of(float z) {
-  if constexpr (ACT == GRPO_ACT_RELU) return z > 0.f ? 1.f : isnan(z) ? z : 0.f;
-  if constexpr (ACT == GRPO_ACT_GELU)
-    return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
-  if constexpr (ACT == GRPO_ACT_GELU_TANH) {
-    const float t = tanhf(0.79788456f * fmaf(0.044715f * z * z, z, z));
-    return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.79788456f * fmaf(3.f * 0.044715f * z, z, 1.f);
-  }
-  if constexpr (ACT == GRPO_ACT_SILU) {
-    const float g = sigmoid(z);
-    return g * fmaf(z, 1.f - g, 1.f);
-  }
-  return 1.f;
-}
-
-__device__ __forceinline__ float load_any(const void* p, int64_t i, bool bf16) {
-  return bf16 ? bf16_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
-}
-__device__ __forceinline__ void store_any(void* p, int64_t i, float v, bool bf16) {
-  if (bf16) store_elem(static_cast<uint16_t*>(p) + i, v);
-  else static_cast<float*>(p)[i] = v;
-}
-
-// ---- the products ---------------------------------------------------------------
-struct Epilogue {
-  void* out;  // [M, N], rows ldo apart
-  int64_t ldo;
-  const void* bias;      // [N] or NULL
-  const void* residual;  // [M, N] of out's type, rows ldr apart, or NULL
-  int64_t ldr;
-  float* z;  // [M, N] or NULL
-  int act;
-  bool out_bf16, bias_bf16, accumulate;
-};
-
-struct ProductArgs {
-  GemmArgs g;
-  Epilogue e;
-};
-
-typedef GemmCfg<256, 256, 2, 4> LinCfg;
-
-// 8 columns of a row, at any alignment of their elements.
-__device__ __forceinline__ void load8(const void* p, int64_t i, bool bf16, float (&v)[8]) {
-  if (bf16) {
-    const u32x4 x = *reinterpret_cast<const u32x4_a2*>(static_cast<const uint16_t*>(p) + i);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = elem<uint16_t>(x, q);
-  } else {
-    const u32x4_a4* x = reinterpret_cast<const u32x4_a4*>(static_cast<const float*>(p) + i);
-    const u32x4 a = x[0], b = x[1];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      v[q] = __uint_as_float(a[q]);
-      v[q + 4] = __uint_as_float(b[q]);
-    }
-  }
-}
-__device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const float (&v)[8]) {
-  if (bf16) {
-    u32x4 x;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = pack_bf16(v[2 * q], v[2 * q + 1]);
-    *reinterpret_cast<u32x4_a2*>(static_cast<uint16_t*>(p) + i) = x;
-  } else {
-    u32x4 a, b;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      a[q] = __float_as_uint(v[q]);
-      b[q] = __float_as_uint(v[q + 4]);
-    }
-    u32x4_a4* x = reinterpret_cast<u32x4_a4*>(static_cast<float*>(p) + i);
-    x[0] = a;
-    x[1] = b;
-  }
-  asm volatile("s_nop 1" ::: "memory");  // the stores have read their data before their registers are reused
-}
-
-// The epilogue of 8 sums v of row m, columns n .. n + 7 (those below N).
-template <int ACT>
-__device__ __forceinline__ void finish8(const Epilogue& e, int m, int n, int N, const float (&bias)[8], float (&v)[8]) {
-  const bool all = n + 8 <= N;
-  const int k = all ? 8 : N - n;
-  const int64_t o = (int64_t)m * e.ldo + n;
-#pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] += bias[q];
-  if (e.z) {
-    const int64_t oz = (int64_t)m * N + n;
-    if (all) store8(e.z, oz, false, v);
-    else
-      for (int q = 0; q < 8; ++q)
-        if (q < k) e.z[oz + q] = v[q];
-  }
-#pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] = act_of<ACT>(v[q]);
-  const void* more = e.residual ? e.residual : e.accumulate ? e.out : nullptr;
-  if (more) {
-    const int64_t om = e.residual ? (int64_t)m * e.ldr + n : o;
-    float r[8];
-    if (all) load8(more, om, e.out_bf16, r);
-    else
-#pragma unroll
-      for (int q = 0; q < 8; ++q) r[q] = q < k ? load_any(more, om + q, e.out_bf16) : 0.f;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] += r[q];
-  }
-  if (all) store8(e.out, o, e.out_bf16, v);
-  else
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      if (q < k) store_any(e.out, o + q, v[q], e.out_bf16);
-}
-
-typedef float lin_f32x4 __attribute__((ext_vector_type(4)));
-
-// What lanes of a wave stored to LDS before is what others of it read after.
-__device__ __forceinline__ void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
-// A wave's sums, 32 rows at a time, through its own part of the LDS into rows of 16-byte vectors: out of the registers
-// they would be stored 64 bytes to a row.
-template <class C, int ACT>
-__device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, int M, int N,
-                                            const g_f32x16 (&acc)[C::IB][C::JB], float* lds) {
-  constexpr int LD = C::WTN + 4, LPR = C::WTN / 8, RPS = 64 / LPR;  // lanes to a row, rows to a step
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WGN, wn = wave % C::WGN;
-  float* mine = lds + wave * 32 * LD;
-  const int cl = lane % LPR * 8, n = n0 + wn * C::WTN + cl;
-  float bias[8];
-#pragma unroll
-  for (int q = 0; q < 8; ++q) bias[q] = e.bias && n + q < N ? load_any(e.bias, n + q, e.bias_bf16) : 0.f;
-#pragma unroll
-  for (int i = 0; i < C::IB; ++i) {
-#pragma unroll
-    for (int j = 0; j < C::JB; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mine[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * LD + j * 32 + (lane & 31)] = acc[i][j][r];
-    wave_order();
-#pragma unroll 1
-    for (int q = 0; q < 32; q += RPS) {
-      const int rl = q + lane / LPR, m = m0 + wm * C::WTM + i * 32 + rl;
-      if (m >= M || n >= N) continue;
-      float v[8];
-      const lin_f32x4* src = reinterpret_cast<const lin_f32x4*>(mine + rl * LD + cl);
-      const lin_f32x4 a = src[0], b = src[1];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k] = a[k];
-        v[k + 4] = b[k];
-      }
-      finish8<ACT>(e, m, n, N, bias, v);
-    }
-    wave_order();
-  }
-}
-
-template <int ACT>
-__global__ __launch_bounds__(LinCfg::NT) void k_linear(const ProductArgs p) {
-  typedef LinCfg C;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2 * C::STAGE];
-  static_assert(sizeof(float) * C::NW * 32 * (C::WTN + 4) <= sizeof(lds), "the epilogue's rows");
-  int tm, tn;
-  const int tiles_m = (p.g.M + C::BM - 1) / C::BM, tiles_n = (p.g.N + C::BN - 1) / C::BN;
-  if (!gemm_tile_of(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn)) return;
-  const int m0 = tm * C::BM, n0 = tn * C::BN;
-  g_f32x16 acc[C::IB][C::JB];
-  gemm_mainloop<C>(p.g, m0, n0, acc, lds);
-  __syncthreads();  // every wave's last reads are done
-  finish_tile<C, ACT>(p.e, m0, n0, p.g.M, p.g.N, acc, reinterpret_cast<float*>(lds));
-}
-
-typedef void (*ProductKernel)(const ProductArgs);
-static ProductKernel product_kernel(int act) {
-  switch (act) {
-    case GRPO_ACT_RELU: return k_linear<GRPO_ACT_RELU>;
-    case GRPO_ACT_GELU: return k_linear<GRPO_ACT_GELU>;
-    case GRPO_ACT_GELU_TANH: return k_linear<GRPO_ACT_GELU_TANH>;
-    case GRPO_ACT_SILU: return k_linear<GRPO_ACT_SILU>;
-    default: return k_linear<GRPO_ACT_NONE>;
-  }
-}
 
 // ---- few rows ---------------------------------------------------------------------
 // Up to 32 rows: a product is then as long as reading W once takes.  A wave goes down its part of the summed dimension, 32
@@ -425,27 +226,6 @@ __global__ __launch_bounds__(256) void k_lin_copy(const uint16_t* __restrict__ s
   for (int r = blockIdx.y; r < R; r += gridDim.y) dst[r * ldd + c] = c < C ? src[r * lds_ + c] : (uint16_t)0;
 }
 
-// dst [C, ldd] = the transpose of src [R, C] (rows lds_ apart), zeros in columns R .. ldd - 1.
-__global__ __launch_bounds__(256) void k_lin_transpose(const uint16_t* __restrict__ src, int64_t lds_, int R, int C,
-                                                       uint16_t* __restrict__ dst, int64_t ldd) {
-  __shared__ uint16_t tile[64][66];
-  const int c0 = blockIdx.x * 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  for (int r0 = blockIdx.y * 64; r0 < ldd; r0 += gridDim.y * 64) {
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      const int r = r0 + ty + 4 * q, c = c0 + tx;
-      tile[ty + 4 * q][tx] = r < R && c < C ? src[r * lds_ + c] : (uint16_t)0;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      const int c = c0 + ty + 4 * q, r = r0 + tx;
-      if (c < C && r < ldd) dst[c * ldd + r] = tile[tx][ty + 4 * q];
-    }
-  }
-}
-
 // ---- dz -------------------------------------------------------------------------
 struct DzArgs {
   const void* dy;  // [M, N], rows lddy apart
@@ -478,17 +258,6 @@ __global__ __launch_bounds__(256) void k_lin_dz(const DzArgs a) {
   }
 }
 
-typedef void (*DzKernel)(const DzArgs);
-static DzKernel dz_kernel(int act) {
-  switch (act) {
-    case GRPO_ACT_RELU: return k_lin_dz<GRPO_ACT_RELU>;
-    case GRPO_ACT_GELU: return k_lin_dz<GRPO_ACT_GELU>;
-    case GRPO_ACT_GELU_TANH: return k_lin_dz<GRPO_ACT_GELU_TANH>;
-    case GRPO_ACT_SILU: return k_lin_dz<GRPO_ACT_SILU>;
-    default: return k_lin_dz<GRPO_ACT_NONE>;
-  }
-}
-
 // dbias from the partial sums, added in fp64 in the order of the rows.
 __global__ __launch_bounds__(256) void k_lin_dbias(const float* __restrict__ part, int blocks, int N, void* dbias,
                                                    bool bf16) {
@@ -500,6 +269,7 @@ __global__ __launch_bounds__(256) void k_lin_dbias(const float* __restrict__ par
 }
 
 // ---- host -----------------------------------------------------------------------
+constexpr int64_t kCus = 256;
 constexpr int64_t kMostLin = 8388352;  // 2^23 - 256: 256 rows of an operand stay below 4 GB
 
 static int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -509,58 +279,74 @@ static bool whole(const void* p, int64_t C, int64_t ld) {
   return C % 8 == 0 && ld % 8 == 0 && ld <= kMostLin && aligned(p, 16);
 }
 
-// An operand of a product as it will be read: [rows, cols], cols summed over.
+// An operand of a product: `rows` rows whose `cols` elements are summed over, as it lies (TileOperand).
 struct Operand {
   const uint16_t* src;
   int64_t ld, rows, cols;
   bool turned;  // src is [cols, rows]
-  bool padded;  // zeros from cols to a multiple of 8
-  bool copied() const { return turned || !whole(src, padded ? up8(cols) : cols, ld); }
-  size_t bytes() const { return copied() ? align_up(2 * (size_t)rows * (size_t)up8(cols)) : 0; }
+  bool padded;  // its lines end in zeros up to a multiple of 8
+  int64_t lines() const { return turned ? cols : rows; }
+  int64_t length() const { return padded ? up8(turned ? rows : cols) : turned ? rows : cols; }
+  bool copied() const { return !whole(src, length(), ld); }  // where tiles read it
+  size_t bytes() const { return copied() ? align_up(2 * (size_t)lines() * (size_t)up8(length())) : 0; }
 };
 
-static const uint16_t* lay_out(const Operand& o, char*& ws, int64_t& ld, hipStream_t s) {
-  if (!o.copied()) {
-    ld = o.ld;
-    return o.src;
-  }
+static TileOperand lay_out(const Operand& o, char*& ws, hipStream_t s) {
+  if (!o.copied()) return TileOperand{o.src, o.ld, o.turned};
   uint16_t* dst = reinterpret_cast<uint16_t*>(ws);
   ws += o.bytes();
-  ld = up8(o.cols);
-  const unsigned most = 16384;
-  if (o.turned)
-    hipLaunchKernelGGL(k_lin_transpose, dim3((unsigned)((o.rows + 63) / 64), std::min(most, (unsigned)((ld + 63) / 64))),
-                       dim3(256), 0, s, o.src, o.ld, (int)o.cols, (int)o.rows, dst, ld);
-  else
-    hipLaunchKernelGGL(k_lin_copy, dim3((unsigned)((ld + 255) / 256), std::min(most, (unsigned)o.rows)), dim3(256), 0, s,
-                       o.src, o.ld, (int)o.rows, (int)o.cols, dst, ld);
-  return dst;
+  const int64_t ld = up8(o.length());
+  hipLaunchKernelGGL(k_lin_copy, dim3((unsigned)((ld + 255) / 256), (unsigned)std::min<int64_t>(16384, o.lines())), dim3(256),
+                     0, s, o.src, o.ld, (int)o.lines(), (int)o.length(), dst, ld);
+  return TileOperand{dst, ld, o.turned};
 }
 
 // How a product is done: by the kernel for few rows, in `splits` parts of the summed dimension, or by tiles.
 struct ProductPlan {
   bool few;
-  int splits, wave_k;
+  int shape, splits;
+  int range;    // few: the part of the sum of a wave; tiles: of a split
   size_t part;  // bytes of the splits' sums
 };
 static ProductPlan product_plan(const Operand& a, const Operand& b) {
   ProductPlan p{};
   p.splits = 1;
-  p.few = a.rows <= kFewRows && !a.turned && a.cols >= 8 && (!b.turned || b.rows >= 8);
-  if (!p.few) return p;
-  const int64_t K = a.cols, strips = (b.rows + kFewCols - 1) / kFewCols, steps = (K + 31) / 32;
-  // workgroups for the whole chip, of waves that have at least 4 steps each
-  const int64_t most = std::max<int64_t>(1, steps / (4 * kFewWaves));
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, 256 / strips, 16}));
-  const int64_t waves = (int64_t)p.splits * kFewWaves;
-  p.wave_k = (int)((steps + waves - 1) / waves * 32);
+  const int64_t K = a.cols;
+  p.few = a.rows <= kFewRows && !a.turned && K >= 8 && (!b.turned || b.rows >= 8) && a.ld <= kMostLin && b.ld <= kMostLin;
+  if (p.few) {
+    const int64_t strips = (b.rows + kFewCols - 1) / kFewCols, steps = (K + 31) / 32;
+    // workgroups for the whole chip, of waves that have at least 4 steps each
+    const int64_t most = std::max<int64_t>(1, steps / (4 * kFewWaves));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, kCus / strips, 16}));
+    const int64_t waves = (int64_t)p.splits * kFewWaves;
+    p.range = (int)((steps + waves - 1) / waves * 32);
+  } else {
+    p.shape = a.rows <= 64 ? 2 : a.rows <= 128 || a.rows * b.rows < (int64_t)128 * 256 * 256 ? 1 : 0;
+    const TileShape& t = kTileShapes[p.shape];
+    const int64_t tiles = ((a.rows + t.m - 1) / t.m) * ((b.rows + t.n - 1) / t.n), slabs = (K + 63) / 64;
+    int64_t splits = std::max<int64_t>(1, std::min<int64_t>({slabs / 8, kCus / tiles, 16}));
+    p.range = (int)((slabs + splits - 1) / splits * 64);
+    p.splits = (int)((K + p.range - 1) / p.range);
+  }
   if (p.splits > 1) p.part = align_up(4 * (size_t)p.splits * (size_t)a.rows * (size_t)b.rows);
   return p;
 }
 
+// go(the activation as a constant).
+template <class F>
+static void with_act(int act, F&& go) {
+  switch (act) {
+    case GRPO_ACT_RELU: return go(std::integral_constant<int, GRPO_ACT_RELU>());
+    case GRPO_ACT_GELU: return go(std::integral_constant<int, GRPO_ACT_GELU>());
+    case GRPO_ACT_GELU_TANH: return go(std::integral_constant<int, GRPO_ACT_GELU_TANH>());
+    case GRPO_ACT_SILU: return go(std::integral_constant<int, GRPO_ACT_SILU>());
+    default: return go(std::integral_constant<int, GRPO_ACT_NONE>());
+  }
+}
+
 static size_t product_bytes(const Operand& a, const Operand& b) {
   const ProductPlan p = product_plan(a, b);
-  return p.few ? p.part : a.bytes() + b.bytes();
+  return p.part + (p.few ? 0 : a.bytes() + b.bytes());
 }
 
 template <int ACT>
@@ -578,37 +364,38 @@ static void launch_few(const FewArgs& f, bool kn, hipStream_t s) {
   };
   if (f.M <= 16) rows(std::integral_constant<int, 1>());
   else rows(std::integral_constant<int, 2>());
-  if (f.splits > 1) {
-    const int64_t n = (int64_t)f.M * ((f.N + 7) / 8);
-    hipLaunchKernelGGL(k_lin_join<ACT>, dim3((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), dim3(256), 0, s, f.part,
-                       f.splits, f.M, f.N, f.e);
-  }
+}
+
+static void join_splits(const float* part, int splits, int M, int N, const Epilogue& e, hipStream_t s) {
+  const int64_t n = (int64_t)M * ((N + 7) / 8);
+  const dim3 grid((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), block(256);
+  auto go = [&](auto act) { hipLaunchKernelGGL(k_lin_join<decltype(act)::value>, grid, block, 0, s, part, splits, M, N, e); };
+  with_act(e.act, go);
 }
 
 // C [a.rows, b.rows] = A B^T with the epilogue e.
 static void launch_product(const Operand& a, const Operand& b, const Epilogue& e, char*& ws, hipStream_t s) {
-  const ProductPlan plan = product_plan(a, b);
-  if (plan.few) {
-    const FewArgs f{a.src, b.src, a.ld, b.ld, (int)a.rows, (int)a.cols, (int)b.rows,
-                    (int)((b.rows + kFewCols - 1) / kFewCols), plan.splits, plan.wave_k, reinterpret_cast<float*>(ws), e};
-    ws += plan.part;
-    switch (e.act) {
-      case GRPO_ACT_RELU: return launch_few<GRPO_ACT_RELU>(f, b.turned, s);
-      case GRPO_ACT_GELU: return launch_few<GRPO_ACT_GELU>(f, b.turned, s);
-      case GRPO_ACT_GELU_TANH: return launch_few<GRPO_ACT_GELU_TANH>(f, b.turned, s);
-      case GRPO_ACT_SILU: return launch_few<GRPO_ACT_SILU>(f, b.turned, s);
-      default: return launch_few<GRPO_ACT_NONE>(f, b.turned, s);
-    }
+  const ProductPlan p = product_plan(a, b);
+  const int M = (int)a.rows, N = (int)b.rows, K = (int)a.cols;
+  float* part = reinterpret_cast<float*>(ws);
+  ws += p.part;
+  if (p.few) {
+    const FewArgs f{a.src, b.src, a.ld, b.ld, M, K, N, (N + kFewCols - 1) / kFewCols, p.splits, p.range, part, e};
+    with_act(e.act, [&](auto act) { launch_few<decltype(act)::value>(f, b.turned, s); });
+  } else {
+    TileArgs t;
+    t.a = lay_out(a, ws, s);
+    t.b = lay_out(b, ws, s);
+    t.M = M;
+    t.N = N;
+    t.K = K;
+    t.splits = p.splits;
+    t.split_k = p.range;
+    t.part = part;
+    t.e = e;
+    launch_tiles(t, p.shape, s);
   }
-  ProductArgs p;
-  p.g.A = lay_out(a, ws, p.g.lda, s);
-  p.g.B = lay_out(b, ws, p.g.ldb, s);
-  p.g.M = (int)a.rows;
-  p.g.N = (int)b.rows;
-  p.g.K = (int)up8(a.cols);
-  p.e = e;
-  const int64_t tiles = ((a.rows + LinCfg::BM - 1) / LinCfg::BM) * ((b.rows + LinCfg::BN - 1) / LinCfg::BN);
-  hipLaunchKernelGGL(product_kernel(e.act), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(LinCfg::NT), 0, s, p);
+  if (p.splits > 1) join_splits(part, p.splits, M, N, e, s);
 }
 
 static bool is_dtype(int32_t d) { return d == GRPO_F32 || d == GRPO_BF16; }
@@ -650,7 +437,7 @@ static BwdPlan bwd_plan(const grpo_linear_op& op, const void* dy, int64_t lddy, 
   const uint16_t* dz = static_cast<const uint16_t*>(dy);
   const int64_t ld = p.make_dz ? up8(op.N) : lddy;
   p.dz_rows = Operand{dz, ld, op.M, op.N, false, p.make_dz};
-  p.dz_cols = Operand{dz, ld, op.N, op.M, true, false};
+  p.dz_cols = Operand{dz, ld, op.N, op.M, true, p.make_dz};
   p.x_cols = Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.K, op.M, true, false};
   p.w = w_as_kn(op);
   p.total = p.dz + p.part;
@@ -749,8 +536,8 @@ extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t
   if (dz || part) {
     const int blocks = (int)((op->M + kDzRows - 1) / kDzRows);
     const DzArgs a{dy, lddy, act ? z : nullptr, dz, up8(op->N), part, (int)op->M, (int)op->N, dy_dtype == GRPO_BF16};
-    hipLaunchKernelGGL(dz_kernel(op->act), dim3((unsigned)((up8(op->N) + 255) / 256), (unsigned)std::min(blocks, 16384)), dim3(256), 0,
-                       s, a);
+    const dim3 grid((unsigned)((up8(op->N) + 255) / 256), (unsigned)std::min(blocks, 16384));
+    with_act(op->act, [&](auto kind) { hipLaunchKernelGGL(k_lin_dz<decltype(kind)::value>, grid, dim3(256), 0, s, a); });
     if (part)
       hipLaunchKernelGGL(k_lin_dbias, dim3((unsigned)((op->N + 255) / 256)), dim3(256), 0, s, part, blocks, (int)op->N,
                          g.dbias, op->bias_dtype == GRPO_BF16);

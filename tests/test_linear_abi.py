@@ -109,8 +109,8 @@ def test_refused_backward_arguments(lib, kw, gkw, status):
 def test_workspace(lib):
     f = lambda **kw: lib.grpo_linear_workspace_bytes(ctypes.byref(an_op(**kw)))  # noqa: E731
     assert lib.grpo_linear_workspace_bytes(None) == 0 and f(M=0) == 0 and f(K=0) == 0
-    odd = f(K=63, ldx=63)
-    assert odd >= 2 * 8 * 64 and odd % 256 == 0
+    odd = f(M=100, K=63, ldx=63)  # x is laid out anew for the tiles
+    assert odd >= 2 * 100 * 64 and odd % 256 == 0
     op, g = an_op(act=2), grads()
     b = lambda op=op, g=g, lddy=128: lib.grpo_linear_bwd_workspace_bytes(ctypes.byref(op), Y, lddy, 1, ctypes.byref(g))  # noqa: E731
     assert b() >= 2 * 8 * 128 and b() % 256 == 0 and b(lddy=12) == 0
