@@ -1,14 +1,14 @@
 // What a row of logits says about a token (grpo_top.h): the given token's log-prob, the entropy and the n likeliest
 // alternatives, in one pass over the row, and the gradient of all three, in another.
 //
-// Forward.  Each thread walks its vectors and keeps, relative to its running maximum m and in units of log 2,
+// Forward.  Each thread walks its vectors, U of them (a chunk) at a time, and keeps, relative to its running maximum m and in
+// units of log 2,
 //   s = sum 2^w, t = sum 2^w w, w = (z - m) log2(e) / tau,
-// over the words (z > -1e8).  m is the sum's shift and, for the alternatives, the maximum of a part of the row: the n-th
-// largest of 256 such maxima (each over the words of NT / 256 neighbouring lanes) is a lower bound L of the n-th largest
-// word, and no word >= L lies outside the parts whose maximum is >= L.  Those parts, n of them unless maxima repeat, are
-// read a second time, their words >= L (n and a few) go to a list in LDS, and a word's place is the number of list words
-// in front of it.  Where maxima repeat so often that the list or the number of parts is too small, the n-th largest word is
-// found by bisection with counts over the row.
+// over the words (z > -1e8).  m also bounds the alternatives: the n-th largest of the threads' maxima is a lower bound L of
+// the n-th largest word.  The maximum of each chunk of four neighbouring lanes is kept in LDS, and only the chunks whose
+// maximum is >= L, n of them unless words repeat, are read a second time; their words >= L (n and a few) go to a list in
+// LDS, and a word's place is the number of list words in front of it.  Where words repeat so often that the list or the
+// number of chunks is too small, the n-th largest word is found by bisection with counts over the row.
 // Where rows are few and long, a row is cut into parts of their own workgroups, and a second launch joins them.
 //
 // Backward.  A streaming pass: dlogits_v = p_v (A log2 p_v + B) with A, B of the row; the words with a coefficient of their
@@ -24,8 +24,7 @@
 
 namespace grpo {
 
-constexpr int kGroups = 256;      // maxima that bound the n-th largest word
-constexpr int kMostGroups = 128;  // parts that are read again
+constexpr int kMostGroups = 256;  // chunks of four lanes that are read again
 constexpr int kTopCap = 1024;     // words the list holds
 constexpr uint32_t kNothing = 0;  // the key of no word (a word's is larger)
 
@@ -68,21 +67,54 @@ __device__ __forceinline__ uint64_t key_of(float z, int idx) {
 }
 __device__ __forceinline__ bool is_word(float z) { return z > kShiftMin; }
 
-// One word folded into (s, t) at the shift m.  The difference comes first, so that w's error is relative to w whatever m
-// and tau are.  A masked word adds 2^-200 = 0; a NaN is not masked and makes s NaN.
-__device__ __forceinline__ void fold_word(float z, float m, float sc, float& s, float& t) {
-  const float w = z <= kShiftMin ? -200.f : (z - m) * sc;
-  const float e = __builtin_amdgcn_exp2f(w);
-  s += e;
-  t = fmaf(e, w, t);
-}
+// A thread's sums relative to the shift m sc - rest: w = z sc - m sc + rest.  Near: m sc is small enough that c = -m sc,
+// rounded, is a shift to half a unit, rest its rounding, and w one fma, whose error is relative to w; otherwise the
+// difference z - m comes first and rest is 0.
+struct Sums {
+  float m = kShiftMin, s = 0.f, t = 0.f, c = 0.f, rest = 0.f;
+  bool near = false;
 
-__device__ __forceinline__ void raise_shift(float& m, float mn, float sc, float& s, float& t) {
-  if (mn > m) {
-    const float dl = (mn - m) * sc, f = __builtin_amdgcn_exp2f(-dl);
-    t = f == 0.f ? 0.f : f * fmaf(-dl, s, t);
-    s *= f;
-    m = mn;
+  __device__ __forceinline__ void raise(float mn, float sc) {
+    if (mn > m) {
+      c = -(mn * sc);
+      near = fabsf(c) < 4194304.f;
+      const float r = near ? fmaf(mn, sc, c) : 0.f;
+      const float dl = fmaf(m - mn, sc, r - rest), f = __builtin_amdgcn_exp2f(dl);
+      t = f == 0.f ? 0.f : f * fmaf(dl, s, t);
+      s *= f;
+      m = mn;
+      rest = r;
+    }
+  }
+  // A word at the shift, near and above -1e8; a NaN makes s NaN.
+  __device__ __forceinline__ void fold_near(float z, float sc) {
+    const float w = fmaf(z, sc, c), e = __builtin_amdgcn_exp2f(w);
+    s += e;
+    t = fmaf(e, w, t);
+  }
+  // Any element: a masked word adds 2^-200 = 0, a NaN is not masked.
+  __device__ __forceinline__ void fold(float z, float sc) {
+    const float w = z <= kShiftMin ? -200.f : fmaf(z - m, sc, rest);
+    const float e = __builtin_amdgcn_exp2f(w);
+    s += e;
+    t = fmaf(e, w, t);
+  }
+};
+
+__device__ __forceinline__ float min3f(float a, float b, float c) {  // as max3f (device.h)
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+template <typename Tin>
+__device__ __forceinline__ float vec_min(const u32x4& x, float m) {
+  if constexpr (sizeof(Tin) == 2) {
+    const float a = min3f(bf16_lo(x[0]), bf16_hi(x[0]), bf16_lo(x[1]));
+    const float b = min3f(bf16_hi(x[1]), bf16_lo(x[2]), bf16_hi(x[2]));
+    const float c = min3f(bf16_lo(x[3]), bf16_hi(x[3]), m);
+    return min3f(a, b, c);
+  } else {
+    return min3f(min3f(m, __uint_as_float(x[0]), __uint_as_float(x[1])), __uint_as_float(x[2]), __uint_as_float(x[3]));
   }
 }
 
@@ -91,30 +123,32 @@ __device__ __forceinline__ float scale_of(float tau) {
   return tau >= 1e-6f && tau <= 1e6f ? kLog2e / tau : NAN;
 }
 
+constexpr int kSlices = 32;  // chunks, or runs of chunks, of a lane that have a maximum of their own
+
 template <int NT>
 struct TopSmem {
   float m[NT / 64];
   double s[NT / 64], t[NT / 64];
   double log_sum;
-  uint32_t group[kGroups];  // upper 16 bits of the order of each group's maximum
-  uint32_t bound;           // and of L
+  uint16_t top[NT];                   // upper 16 bits of the order of each thread's maximum
+  uint16_t group[kSlices * NT / 4];   // and of four lanes' chunk
+  uint32_t bound;                     // and of L
   int n_groups, count;
   int wave_count[NT / 64];
   uint16_t groups[kMostGroups];
   uint64_t list[kTopCap];
 };
 
-// All threads' (m, s, t) joined in fp64, the result in every thread.
+// All threads' sums joined in fp64 at the shift of the row's maximum M, in every thread.
 template <int NT>
-__device__ __forceinline__ void join_threads(float m, float s, float t, float sc, TopSmem<NT>& sm, float& M, double& S,
-                                             double& T) {
+__device__ __forceinline__ void join_threads(const Sums& a, float sc, TopSmem<NT>& sm, float& M, double& S, double& T) {
   constexpr int NW = NT / 64;
   static_assert(NW <= 16, "one wave to a lane of 16");
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const float mw = wave_max_dpp(m);
-  const float dl = (m - mw) * sc, f = __builtin_amdgcn_exp2f(dl);
-  const double sw = wave_sum_dpp((double)f * (double)s);
-  const double tw = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * ((double)t + (double)dl * (double)s));
+  const float mw = wave_max_dpp(a.m);
+  const float dl = fmaf(a.m - mw, sc, -a.rest), f = __builtin_amdgcn_exp2f(dl);
+  const double sw = wave_sum_dpp((double)f * (double)a.s);
+  const double tw = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * ((double)a.t + (double)dl * (double)a.s));
   if (lane == 0) {
     sm.m[wv] = mw;
     sm.s[wv] = sw;
@@ -130,10 +164,10 @@ __device__ __forceinline__ void join_threads(float m, float s, float t, float sc
   T = row16_sum(g == 0.f || !in ? 0.0 : (double)g * (sm.t[q] + (double)dq * sm.s[q]));
 }
 
-// What the row comes to, from the joined sums: one thread.
-__device__ inline grpo_top_row finish_row(const TopArgs& a, int t, float tau, float M, double S, double Tsum) {
+// What the row comes to, from the joined sums, and its outputs: one thread.  za: the logit of the action act.
+__device__ inline grpo_top_row finish_row(const TopArgs& a, int t, int act, float za, float tau, float M, double S,
+                                          double Tsum) {
   grpo_top_row r;
-  const int act = a.actions[t];
   const bool act_ok = act >= 0 && act < a.V;
   const bool bad_tau = !(tau >= 1e-6f && tau <= 1e6f), bad = isnan(S) || isnan(M) || M == INFINITY || bad_tau;
   r.temperature = tau;
@@ -154,22 +188,13 @@ __device__ inline grpo_top_row finish_row(const TopArgs& a, int t, float tau, fl
     r.log_sum = log(S);
     r.max = M;
     r.entropy = (float)(r.log_sum - Tsum / S * kLn2);  // both terms >= 0
-    r.logp = 0.f;
+    r.logp = !act_ok ? 0.f : is_word(za) ? (float)(((double)za - (double)M) / (double)tau - r.log_sum) : -INFINITY;
   }
   if (flags && a.flags) atomicOr(a.flags, flags);
-  return r;
-}
-
-template <typename Tin>
-__device__ __forceinline__ void store_row(const TopArgs& a, int t, grpo_top_row r) {
-  const int act = a.actions[t];
-  if (r.max > -INFINITY && act >= 0 && act < a.V) {
-    const float z = load_elem(static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld + act);
-    r.logp = is_word(z) ? (float)(((double)z - (double)r.max) / (double)r.temperature - r.log_sum) : -INFINITY;
-  }
   if (a.logp) a.logp[t] = r.logp;
   if (a.entropy) a.entropy[t] = r.entropy;
   if (a.rows) a.rows[t] = r;
+  return r;
 }
 
 // Where a list word goes: a final row's outputs, or a part's keys.
@@ -241,7 +266,7 @@ __device__ __forceinline__ int block_sum(int v, Smem& sm) {
 // bisection between the bound and the maximum, each step a count over the row; then the words above it (fewer than n) and
 // the first of those that equal it.
 template <typename Tin, int NT>
-__device__ __noinline__ void top_by_counts(const Tin* row, int cols, int n, float M, TopSmem<NT>& sm, const TopOut& out) {
+__device__ __forceinline__ void top_by_counts(const Tin* row, int cols, int n, float M, TopSmem<NT>& sm, const TopOut& out) {
   constexpr int EPV = 16 / (int)sizeof(Tin), SH = sizeof(Tin) == 2 ? 16 : 0;
   typedef typename VecAt<Tin>::type u32x4_any;
   const int tid = threadIdx.x, nvec = cols / EPV, tiles = (nvec + NT - 1) / NT, n_edge = cols - nvec * EPV;
@@ -251,7 +276,7 @@ __device__ __noinline__ void top_by_counts(const Tin* row, int cols, int n, floa
   while (hi - lo > 1) {
     const uint32_t mid = lo + (hi - lo) / 2;
     int cnt = rank_of(ez) >= mid;
-#pragma unroll 4
+#pragma unroll 1
     for (int q = 0; q < tiles; ++q) {
       const int vi = q * NT + tid;
       if (vi >= nvec) break;
@@ -323,10 +348,10 @@ __device__ __noinline__ void top_by_counts(const Tin* row, int cols, int n, floa
 }
 
 // One workgroup to a row, or (PART) to a part of it.
-template <typename Tin, int NT, int U, bool PART>
-__global__ __launch_bounds__(NT) void k_top(const TopArgs a, int row0) {
-  constexpr int EPV = 16 / (int)sizeof(Tin), G = NT / kGroups;
-  static_assert(G == 1 || G == 2 || G == 4, "lanes to a group");
+template <typename Tin, int NT, bool PART>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ? 8 : 4))) void k_top(const TopArgs a,
+                                                                                                  int row0) {
+  constexpr int EPV = 16 / (int)sizeof(Tin), U = 4, QUADS = NT / 4;
   typedef typename VecAt<Tin>::type u32x4_any;
   __shared__ TopSmem<NT> sm;
   const int tid = threadIdx.x;
@@ -335,53 +360,88 @@ __global__ __launch_bounds__(NT) void k_top(const TopArgs a, int row0) {
   const int c0 = PART ? part * a.part_cols : 0, cols = PART ? min(a.part_cols, a.V - c0) : a.V;
   const Tin* row = static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld + c0;
   const float tau = a.tau_rows ? a.tau_rows[t] : a.tau_all, sc = scale_of(tau);
-  const int nvec = cols / EPV, n_edge = cols - nvec * EPV;
+  const int n = a.n, nvec = cols / EPV, n_edge = cols - nvec * EPV;
+  const int chunks = (nvec + NT * U - 1) / (NT * U), run = (chunks + kSlices - 1) / kSlices;  // chunks to a slice
   if (tid == 0) sm.n_groups = sm.count = 0;
   const float ez = tid < n_edge ? load_elem(row + nvec * EPV + tid) : -INFINITY;
-  float m = fmaxf(kShiftMin, ez), s = 0.f, tt = 0.f;
-  fold_word(ez, m, sc, s, tt);
-  for (int base = tid; base < nvec; base += NT * U) {
-    u32x4 x[U];
+  int act = -1;
+  float za = -INFINITY;  // the action's logit, for the thread that finishes the row
+  if (!PART && tid == 64) {
+    act = a.actions[t];
+    if (act >= 0 && act < a.V) za = load_elem(row + act);
+  }
+  Sums sum;
+  sum.raise(ez, sc);
+  sum.fold(ez, sc);
+  float gm = -INFINITY;
+  for (int q = 0; q < chunks; ++q) {
+    const int base = q * NT * U + tid;
+    float cm = -INFINITY, cn = INFINITY;
+    auto words = [&](const u32x4& x) {
+      if (sum.near && cn > kShiftMin) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int vi = base + u * NT;
-      if (vi < nvec) x[u] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi * EPV);
+        for (int e = 0; e < EPV; ++e) sum.fold_near(elem<Tin>(x, e), sc);
+      } else {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) sum.fold(elem<Tin>(x, e), sc);
+      }
+    };
+    if ((q + 1) * NT * U <= nvec) {
+      u32x4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(base + u * NT) * EPV);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        cm = vec_max<Tin>(x[u], cm);
+        cn = vec_min<Tin>(x[u], cn);
+      }
+      sum.raise(cm, sc);
+      if (sum.near && cn > kShiftMin) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) sum.fold_near(elem<Tin>(x[u], e), sc);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) sum.fold(elem<Tin>(x[u], e), sc);
+      }
+    } else {
+#pragma unroll 1
+      for (int vi = base; vi < nvec; vi += NT) {
+        const u32x4 x = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi * EPV);
+        cm = vec_max<Tin>(x, cm);
+        cn = vec_min<Tin>(x, cn);
+        sum.raise(cm, sc);
+        words(x);
+      }
     }
-    float cm = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (base + u * NT < nvec) cm = vec_max<Tin>(x[u], cm);
-    raise_shift(m, cm, sc, s, tt);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (base + u * NT < nvec) {
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) fold_word(elem<Tin>(x[u], e), m, sc, s, tt);
+    if (n > 0) {
+      cm = fmaxf(cm, dpp_f32v<0xB1>(cm));
+      gm = fmaxf(gm, fmaxf(cm, dpp_f32v<0x4E>(cm)));  // of the four lanes
+      if ((q + 1) % run == 0 || q + 1 == chunks) {
+        if ((tid & 3) == 0) sm.group[q / run * QUADS + (tid >> 2)] = is_word(gm) ? (uint16_t)(order_of(gm) >> 16) : 0;
+        gm = -INFINITY;
       }
     }
   }
-  float gm = m;  // the maximum of the group's lanes
-  if (G >= 2) gm = fmaxf(gm, dpp_f32v<0xB1>(gm));
-  if (G >= 4) gm = fmaxf(gm, dpp_f32v<0x4E>(gm));
-  const uint32_t gkey = order_of(gm) >> 16;
-  if (tid % G == 0) sm.group[tid / G] = gkey;
+  sm.top[tid] = (uint16_t)(order_of(sum.m) >> 16);
   float M;
   double S, Tsum;
-  join_threads<NT>(m, s, tt, sc, sm, M, S, Tsum);
+  join_threads<NT>(sum, sc, sm, M, S, Tsum);
   const bool bad = isnan(S) || isnan(M) || M == INFINITY || isnan(sc), some = !bad && S > 0.0;
   if (PART) {
-    if (tid == 0) a.part[(int64_t)t * a.parts + part] = TopPart{bad ? (double)NAN : S, Tsum, some ? M : kShiftMin, 0.f};
-  } else if (tid == 0) {
-    const grpo_top_row r = finish_row(a, t, tau, M, S, Tsum);
+    if (tid == 64) a.part[(int64_t)t * a.parts + part] = TopPart{bad ? (double)NAN : S, Tsum, some ? M : kShiftMin, 0.f};
+  } else if (tid == 64) {
+    const grpo_top_row r = finish_row(a, t, act, za, tau, M, S, Tsum);
     sm.log_sum = r.log_sum;
-    store_row<Tin>(a, t, r);
   }
-  const int n = a.n;
   if (n == 0) return;
   if (tid < 64 && some) {
-    uint32_t k[kGroups / 64];
+    uint32_t k[NT / 64];
 #pragma unroll
-    for (int i = 0; i < kGroups / 64; ++i) k[i] = sm.group[tid + 64 * i];
+    for (int i = 0; i < NT / 64; ++i) k[i] = sm.top[tid + 64 * i];
     const uint32_t p = nth_largest(k, n);
     if (tid == 0) sm.bound = p;
   }
@@ -400,39 +460,33 @@ __global__ __launch_bounds__(NT) void k_top(const TopArgs a, int row0) {
     return;
   }
   const uint32_t bound = sm.bound;
-  if (tid % G == 0 && gkey >= bound && is_word(gm)) {
-    const int g = atomicAdd(&sm.n_groups, 1);
-    if (g < kMostGroups) sm.groups[g] = (uint16_t)(tid / G);
-  }
+  const float least = value_of(bound << 16);
+  auto take = [&](float z, int idx) {
+    if (z >= least && is_word(z)) {
+      const int i = atomicAdd(&sm.count, 1);
+      if (i < kTopCap) sm.list[i] = key_of(z, c0 + idx);
+    }
+  };
+  if (tid < n_edge) take(ez, nvec * EPV + tid);
+  const int slices = (chunks + run - 1) / run;
+  for (int i = tid; i < slices * QUADS; i += NT)
+    if (sm.group[i] >= bound) {
+      const int g = atomicAdd(&sm.n_groups, 1);
+      if (g < kMostGroups) sm.groups[g] = (uint16_t)i;
+    }
   __syncthreads();
   const int ng = sm.n_groups;
   bool fits = ng <= kMostGroups;
   if (fits) {
-    const float least = value_of(bound << 16);
-    auto take = [&](float z, int idx) {
-      if (z >= least && is_word(z)) {
-        const int i = atomicAdd(&sm.count, 1);
-        if (i < kTopCap) sm.list[i] = key_of(z, c0 + idx);
-      }
-    };
-    if (tid < n_edge) take(ez, nvec * EPV + tid);
-    const int per = (nvec + NT - 1) / NT * G, items = ng * per;
-    constexpr int R = 2;  // loads in flight
-    for (int i0 = tid; i0 < items; i0 += R * NT) {
-      int vi[R];
-      u32x4 x[R];
+    const int per = run * U * 4, items = ng * per;
+    for (int i = tid; i < items; i += NT) {
+      const int gi = i / per, r = i - gi * per, g = sm.groups[gi];
+      const int vi = (g / QUADS * run * U + r / 4) * NT + g % QUADS * 4 + r % 4;
+      if (vi >= nvec) continue;
+      const u32x4 x = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi * EPV);
+      if (!(vec_max<Tin>(x, -INFINITY) >= least)) continue;
 #pragma unroll
-      for (int u = 0; u < R; ++u) {
-        const int i = i0 + u * NT, gi = i / per, r = i - gi * per;
-        vi[u] = i < items ? r / G * NT + sm.groups[gi] * G + r % G : nvec;
-        if (vi[u] < nvec) x[u] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)vi[u] * EPV);
-      }
-#pragma unroll
-      for (int u = 0; u < R; ++u) {
-        if (vi[u] >= nvec || !(vec_max<Tin>(x[u], -INFINITY) >= least)) continue;
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) take(elem<Tin>(x[u], e), vi[u] * EPV + e);
-      }
+      for (int e = 0; e < EPV; ++e) take(elem<Tin>(x, e), vi * EPV + e);
     }
     __syncthreads();
     fits = sm.count <= kTopCap;
@@ -442,39 +496,51 @@ __global__ __launch_bounds__(NT) void k_top(const TopArgs a, int row0) {
 }
 
 // A row's parts joined: one workgroup to a row.
-constexpr int kJoinNT = 256;
+constexpr int kJoinNT = 256, kMostParts = 64;
 struct JoinSmem {
   uint64_t list[kTopCap];
-  uint64_t all[kTopCap];
   double log_sum;
   uint32_t bound;
   int count;
 };
 template <typename Tin>
 __global__ __launch_bounds__(kJoinNT) void k_top_join(const TopArgs a) {
+  constexpr int PER = kTopCap / kJoinNT;
   __shared__ JoinSmem sm;
-  const int t = blockIdx.x, tid = threadIdx.x, n = a.n, c = a.parts * n;
+  __shared__ uint16_t sh_top[kTopCap];
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, n = a.n, c = a.parts * n;
   const float tau = a.tau_rows ? a.tau_rows[t] : a.tau_all, sc = scale_of(tau);
   const uint64_t* keys = a.part_keys + (int64_t)t * c;
-  for (int i = tid; i < c; i += kJoinNT) sm.all[i] = keys[i];
+  uint64_t mine[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine[i] = tid + kJoinNT * i < c ? keys[tid + kJoinNT * i] : kNothing;
+  TopPart p{0.0, 0.0, kShiftMin, 0.f};
+  if (lane < a.parts) p = a.part[(int64_t)t * a.parts + lane];
+  int act = -1;
+  float za = -INFINITY;
+  if (tid == 64) {
+    act = a.actions[t];
+    if (act >= 0 && act < a.V) za = load_elem(static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld + act);
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sh_top[tid + kJoinNT * i] = (uint16_t)(mine[i] >> 48);
   if (tid == 0) sm.count = 0;
-  const TopPart* part = a.part + (int64_t)t * a.parts;
-  float M = kShiftMin;
-  for (int p = 0; p < a.parts; ++p) M = fmaxf(M, part[p].max);
-  double S = 0.0, Tsum = 0.0;
-  for (int p = 0; p < a.parts; ++p) {
-    const TopPart r = part[p];
-    const float d = (r.max - M) * sc, f = __builtin_amdgcn_exp2f(d);
-    S += (double)f * r.s;
-    if (f != 0.f) Tsum += (double)f * (r.t + (double)d * r.s);
-  }
+  // every wave for itself
+  const float M = wave_max_dpp(p.max);
+  const float d = (p.max - M) * sc, f = __builtin_amdgcn_exp2f(d);
+  const double S = wave_sum_dpp((double)f * p.s);
+  const double Tsum = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * (p.t + (double)d * p.s));
   const bool bad = isnan(S) || isnan(sc), some = !bad && S > 0.0;
-  if (tid == 0) {
-    const grpo_top_row r = finish_row(a, t, tau, M, S, Tsum);
-    sm.log_sum = r.log_sum;
-    store_row<Tin>(a, t, r);
-  }
+  if (tid == 64) sm.log_sum = finish_row(a, t, act, za, tau, M, S, Tsum).log_sum;
   if (n == 0) return;
+  __syncthreads();
+  if (tid < 64 && some) {
+    uint32_t k[kTopCap / 64];
+#pragma unroll
+    for (int i = 0; i < kTopCap / 64; ++i) k[i] = sh_top[tid + 64 * i];
+    const uint32_t b = nth_largest(k, n);
+    if (tid == 0) sm.bound = b;
+  }
   __syncthreads();
   TopOut out;
   const int64_t at = (int64_t)t * n;
@@ -489,19 +555,10 @@ __global__ __launch_bounds__(kJoinNT) void k_top_join(const TopArgs a) {
     if (tid < n) out.none(tid, bad);
     return;
   }
-  if (tid < 64) {
-    uint32_t k[kTopCap / 64];
-#pragma unroll
-    for (int i = 0; i < kTopCap / 64; ++i) k[i] = tid + 64 * i < c ? (uint32_t)(sm.all[tid + 64 * i] >> 48) : 0u;
-    const uint32_t p = nth_largest(k, n);
-    if (tid == 0) sm.bound = p;
-  }
-  __syncthreads();
   const uint32_t bound = sm.bound;
-  for (int i = tid; i < c; i += kJoinNT) {
-    const uint64_t key = sm.all[i];
-    if (key != kNothing && (uint32_t)(key >> 48) >= bound) sm.list[atomicAdd(&sm.count, 1)] = key;
-  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (mine[i] != kNothing && (uint32_t)(mine[i] >> 48) >= bound) sm.list[atomicAdd(&sm.count, 1)] = mine[i];
   __syncthreads();
   rank_list<kJoinNT>(sm, sm.count, n, out);
 }
@@ -656,7 +713,7 @@ static TopPlan top_plan(int64_t T, int64_t V, int32_t n) {
   TopPlan p{1, (int)V};
   if (T <= 0 || T >= 128 || V <= 16384) return p;
   int64_t parts = std::min<int64_t>(V / 8192, 256 / T);
-  parts = std::min<int64_t>(parts, n ? kTopCap / n : kTopCap);
+  parts = std::min<int64_t>({parts, (int64_t)kMostParts, n ? (int64_t)(kTopCap / n) : (int64_t)kMostParts});
   if (parts < 2) return p;
   p.cols = (int)(((V + parts - 1) / parts + 7) / 8 * 8);
   p.parts = (int)((V + p.cols - 1) / p.cols);
@@ -667,24 +724,22 @@ static size_t top_part_bytes(int64_t T, const TopPlan& p) { return align_up(size
 
 constexpr int64_t kTopRowsPerLaunch = 1 << 20;  // a launch's threads stay below 2^32
 
-template <typename Tin, int NT, int U>
+template <typename Tin, int NT>
 static void launch_top_rows(const TopArgs& a, int64_t T, hipStream_t s) {
   for (int64_t r = 0; r < T; r += kTopRowsPerLaunch)
-    hipLaunchKernelGGL((k_top<Tin, NT, U, false>), dim3((unsigned)std::min(kTopRowsPerLaunch, T - r)), dim3(NT), 0, s, a,
+    hipLaunchKernelGGL((k_top<Tin, NT, false>), dim3((unsigned)std::min(kTopRowsPerLaunch, T - r)), dim3(NT), 0, s, a,
                        (int)r);
 }
 
 template <typename Tin>
 static void launch_top(const TopArgs& a, int64_t T, hipStream_t s) {
   if (a.parts > 1) {
-    hipLaunchKernelGGL((k_top<Tin, 256, 4, true>), dim3((unsigned)(T * a.parts)), dim3(256), 0, s, a, 0);
+    hipLaunchKernelGGL((k_top<Tin, 256, true>), dim3((unsigned)(T * a.parts)), dim3(256), 0, s, a, 0);
     hipLaunchKernelGGL(k_top_join<Tin>, dim3((unsigned)T), dim3(kJoinNT), 0, s, a);
     return;
   }
-  const int64_t vecs = a.V / (16 / (int64_t)sizeof(Tin));
-  if (vecs <= 2048) launch_top_rows<Tin, 256, 4>(a, T, s);
-  else if (vecs <= 8192) launch_top_rows<Tin, 512, 4>(a, T, s);
-  else launch_top_rows<Tin, 1024, 4>(a, T, s);
+  if (T >= 1024 || a.V <= 16384) launch_top_rows<Tin, 256>(a, T, s);
+  else launch_top_rows<Tin, 1024>(a, T, s);
 }
 
 }  // namespace grpo
