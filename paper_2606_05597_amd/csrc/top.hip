@@ -233,16 +233,17 @@ __device__ __forceinline__ void rank_list(const Smem& sm, int c, int n, const To
   for (int j = c + tid; j < n; j += NT) out.none(j, false);
 }
 
-// The n-th largest of `per * 64` 16-bit keys, those of lane l its `per` in k: one wave.
+// The n-th largest of 64 `per` 16-bit keys, those of a lane the first `per` in k: one wave.
 template <int PER>
-__device__ __forceinline__ uint32_t nth_largest(const uint32_t (&k)[PER], int n) {
+__device__ __forceinline__ uint32_t nth_largest(const uint32_t (&k)[PER], int per, int n) {
   uint32_t p = 0;
 #pragma unroll 1
   for (int b = 15; b >= 0; --b) {
     const uint32_t c = p | (1u << b);
     int cnt = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) cnt += __popcll(__ballot(k[i] >= c));
+    for (int i = 0; i < PER; ++i)
+      if (i < per) cnt += __popcll(__ballot(k[i] >= c));
     if (cnt >= n) p = c;
   }
   return p;
@@ -389,7 +390,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
     if ((q + 1) * NT * U <= nvec) {
       u32x4 x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const u32x4_any*>(row + (int64_t)(base + u * NT) * EPV);
+      for (int u = 0; u < U; ++u)  // non-temporal: 6.4 TB/s of long bf16 rows against 5.6
+        x[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + (int64_t)(base + u * NT) * EPV));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         cm = vec_max<Tin>(x[u], cm);
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
     uint32_t k[NT / 64];
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) k[i] = sm.top[tid + 64 * i];
-    const uint32_t p = nth_largest(k, n);
+    const uint32_t p = nth_largest(k, NT / 64, n);
     if (tid == 0) sm.bound = p;
   }
   __syncthreads();
@@ -496,7 +498,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
 }
 
 // A row's parts joined: one workgroup to a row.
-constexpr int kJoinNT = 256, kMostParts = 64;
+constexpr int kJoinNT = 256;
 struct JoinSmem {
   uint64_t list[kTopCap];
   double log_sum;
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(kJoinNT) void k_top_join(const TopArgs a) {
     uint32_t k[kTopCap / 64];
 #pragma unroll
     for (int i = 0; i < kTopCap / 64; ++i) k[i] = sh_top[tid + 64 * i];
-    const uint32_t b = nth_largest(k, n);
+    const uint32_t b = nth_largest(k, (c + 63) / 64, n);
     if (tid == 0) sm.bound = b;
   }
   __syncthreads();
@@ -705,15 +707,19 @@ static bool bad_top_shape(int64_t T, int64_t V, int64_t ld, int32_t n) {
   return T < 0 || T >= ((int64_t)1 << 31) || V < 1 || V > GRPO_TOP_MAX_V || ld < V || n < 0 || n > GRPO_TOP_MAX;
 }
 
-// How many workgroups a row goes to.
+// How many workgroups a row goes to.  Up to 48 rows of more than 16,384 words are cut, each into at most 16 parts; then a row
+// has 1,024 threads up to 400 rows (about as many as the chip takes at once), 256 beyond (us, the call with 8 alternatives
+// of 151,936 bf16 words, which the caches do not hold: T = 1 cut in 4, 8, 16, 32, 64: 22.0, 20.3, 18.2, 17.5, 16.0, whole with
+// 1,024 threads 21.7, with 256 31.7; T = 16: 22.3, 19.4, 17.6, 18.4, 18.7, 22.2, 32.2; T = 64: 23.8, 21.1, 21.2, 24.7, 29.5,
+// 22.8, 31.8; T = 256 whole 27.9 and 34.2, T = 512 48.3 and 39.3, T = 1,024 82.6 and 60.4).
+constexpr int64_t kFewTopRows = 48, kSomeTopRows = 400;
 struct TopPlan {
   int parts, cols;
 };
 static TopPlan top_plan(int64_t T, int64_t V, int32_t n) {
   TopPlan p{1, (int)V};
-  if (T <= 0 || T >= 128 || V <= 16384) return p;
-  int64_t parts = std::min<int64_t>(V / 8192, 256 / T);
-  parts = std::min<int64_t>({parts, (int64_t)kMostParts, n ? (int64_t)(kTopCap / n) : (int64_t)kMostParts});
+  if (T <= 0 || T > kFewTopRows || V <= 16384) return p;
+  const int64_t parts = std::min<int64_t>({V / 8192, (int64_t)16, n ? (int64_t)(kTopCap / n) : (int64_t)16});
   if (parts < 2) return p;
   p.cols = (int)(((V + parts - 1) / parts + 7) / 8 * 8);
   p.parts = (int)((V + p.cols - 1) / p.cols);
@@ -738,7 +744,7 @@ static void launch_top(const TopArgs& a, int64_t T, hipStream_t s) {
     hipLaunchKernelGGL(k_top_join<Tin>, dim3((unsigned)T), dim3(kJoinNT), 0, s, a);
     return;
   }
-  if (T >= 1024 || a.V <= 16384) launch_top_rows<Tin, 256>(a, T, s);
+  if (T > kSomeTopRows || a.V <= 16384) launch_top_rows<Tin, 256>(a, T, s);
   else launch_top_rows<Tin, 1024>(a, T, s);
 }
 
