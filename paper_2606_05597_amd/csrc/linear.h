@@ -10,14 +10,39 @@
 namespace grpo {
 
 // ---- activations ----------------------------------------------------------------
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+// On the hardware's exp2 and reciprocal (an ulp each): in a tile's epilogue nothing runs beside them, and the library's
+// erff, expf and division took 20 us of a 100 us tile.
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -kLog2e));
+}
+
+// tanh(u) = 1 - 2 / (1 + e^2u), off by 3e-7 at most.
+__device__ __forceinline__ float tanh_of(float u) {
+  return fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * (2.f * kLog2e))), 1.f);
+}
+
+// The normal distribution's function at z and e^(-z^2 / 2).  For x >= 0, erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 +
+// p x), off by 1.5e-7 at most (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26).
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float half = 0.5f * p * t * e;  // of the tail beyond |z|
+  return z >= 0.f ? 1.f - half : half;
+}
 
 template <int ACT>
 __device__ __forceinline__ float act_of(float z) {
   if constexpr (ACT == GRPO_ACT_RELU) return z > 0.f || isnan(z) ? z : 0.f;
-  if constexpr (ACT == GRPO_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678f));
+  if constexpr (ACT == GRPO_ACT_GELU) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   if constexpr (ACT == GRPO_ACT_GELU_TANH)
-    return 0.5f * z * (1.f + tanhf(0.79788456f * fmaf(0.044715f * z * z, z, z)));
+    return 0.5f * z * (1.f + tanh_of(0.79788456f * fmaf(0.044715f * z * z, z, z)));
   if constexpr (ACT == GRPO_ACT_SILU) return z * sigmoid(z);
   return z;
 }
@@ -25,10 +50,13 @@ __device__ __forceinline__ float act_of(float z) {
 template <int ACT>
 __device__ __forceinline__ float slope_of(float z) {
   if constexpr (ACT == GRPO_ACT_RELU) return z > 0.f ? 1.f : isnan(z) ? z : 0.f;
-  if constexpr (ACT == GRPO_ACT_GELU)
-    return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+  if constexpr (ACT == GRPO_ACT_GELU) {
+    float e;
+    const float c = normal_cdf(z, e);
+    return fmaf(0.39894228f * z, e, c);
+  }
   if constexpr (ACT == GRPO_ACT_GELU_TANH) {
-    const float t = tanhf(0.79788456f * fmaf(0.044715f * z * z, z, z));
+    const float t = tanh_of(0.79788456f * fmaf(0.044715f * z * z, z, z));
     return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.79788456f * fmaf(3.f * 0.044715f * z, z, 1.f);
   }
   if constexpr (ACT == GRPO_ACT_SILU) {
@@ -94,7 +122,45 @@ __device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const floa
   asm volatile("s_nop 1" ::: "memory");  // the stores have read their data before their registers are reused
 }
 
-// The epilogue of 8 sums v of row m, columns n .. n + 7 (those below N).
+// 8 columns as they lie in memory.
+struct Raw8 {
+  u32x4 a, b;  // bf16: a alone
+  __device__ __forceinline__ void load(const void* p, int64_t i, bool bf16) {
+    if (bf16) {
+      a = *reinterpret_cast<const u32x4_a2*>(static_cast<const uint16_t*>(p) + i);
+    } else {
+      const u32x4_a4* x = reinterpret_cast<const u32x4_a4*>(static_cast<const float*>(p) + i);
+      a = x[0];
+      b = x[1];
+    }
+  }
+  __device__ __forceinline__ float at(int q, bool bf16) const {
+    return bf16 ? elem<uint16_t>(a, q) : __uint_as_float(q < 4 ? a[q] : b[q - 4]);
+  }
+};
+
+// The epilogue of 8 sums v of row m, columns n .. n + 7, all of them below N; r: what is added last, or NULL.
+template <int ACT>
+__device__ __forceinline__ void finish_whole8(const Epilogue& e, int m, int n, int N, const float (&bias)[8], const Raw8* r,
+                                              float (&v)[8]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] += bias[q];
+  if (e.z) store8(e.z, (int64_t)m * N + n, false, v);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = act_of<ACT>(v[q]);
+  if (r) {
+    if (e.out_bf16) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += r->at(q, true);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] += r->at(q, false);
+    }
+  }
+  store8(e.out, (int64_t)m * e.ldo + n, e.out_bf16, v);
+}
+
+// The same of the columns below N.
 template <int ACT>
 __device__ __forceinline__ void finish8(const Epilogue& e, int m, int n, int N, const float (&bias)[8], float (&v)[8]) {
   const bool all = n + 8 <= N;

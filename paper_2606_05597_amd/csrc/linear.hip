@@ -237,35 +237,77 @@ struct DzArgs {
   int M, N;
   bool dy_bf16;
 };
-constexpr int kDzRows = 128;  // rows whose column sums are one fp32 partial
+// A workgroup to kDzRows rows of 256 columns, a thread to 8 columns of every eighth row, two rows' loads in flight: a
+// streaming pass.  The column sums of a thread's rows are joined through the LDS.
+constexpr int kDzRows = 64;
 
 template <int ACT>
 __global__ __launch_bounds__(256) void k_lin_dz(const DzArgs a) {
-  const int n = blockIdx.x * 256 + threadIdx.x, blocks = (a.M + kDzRows - 1) / kDzRows;
+  __shared__ float sh[8][256];
+  const int cl = threadIdx.x & 31, rl = threadIdx.x >> 5, n = blockIdx.x * 256 + 8 * cl;
+  const int blocks = (a.M + kDzRows - 1) / kDzRows, k = min(8, a.N - n);
   for (int b = blockIdx.y; b < blocks; b += gridDim.y) {
     const int end = min(a.M, (b + 1) * kDzRows);
-    float sum = 0.f;
-    for (int m = b * kDzRows; m < end; ++m) {
-      float v = 0.f;
-      if (n < a.N) {
-        v = load_any(a.dy, m * a.lddy + n, a.dy_bf16);
-        if (ACT != GRPO_ACT_NONE) v *= slope_of<ACT>(a.z[(int64_t)m * a.N + n]);
+    float sum[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sum[q] = 0.f;
+    auto row = [&](int m, float (&v)[8], float (&z)[8]) {
+      const int64_t od = m * a.lddy + n, oz = (int64_t)m * a.N + n;
+      if (k == 8) {
+        load8(a.dy, od, a.dy_bf16, v);
+        if (ACT != GRPO_ACT_NONE) load8(a.z, oz, false, z);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          v[q] = q < k ? load_any(a.dy, od + q, a.dy_bf16) : 0.f;
+          z[q] = ACT != GRPO_ACT_NONE && q < k ? a.z[oz + q] : 0.f;
+        }
       }
-      if (a.dz && n < a.lddz) store_elem(a.dz + m * a.lddz + n, v);
-      sum += v;
+    };
+    auto out = [&](int m, float (&v)[8], const float (&z)[8]) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (ACT != GRPO_ACT_NONE) v[q] *= slope_of<ACT>(z[q]);
+        sum[q] += v[q];
+      }
+      if (a.dz) store8(a.dz, m * a.lddz + n, true, v);
+    };
+    if (n < a.N) {
+      for (int m = b * kDzRows + rl; m < end; m += 16) {
+        float v0[8], z0[8], v1[8], z1[8];
+        row(m, v0, z0);
+        if (m + 8 < end) row(m + 8, v1, z1);
+        out(m, v0, z0);
+        if (m + 8 < end) out(m + 8, v1, z1);
+      }
     }
-    if (a.part && n < a.N) a.part[(int64_t)b * a.N + n] = sum;
+    if (a.part) {
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sh[rl][8 * cl + q] = sum[q];
+      __syncthreads();
+      const int c = threadIdx.x;
+      float s = sh[0][c];
+#pragma unroll
+      for (int q = 1; q < 8; ++q) s += sh[q][c];
+      if (blockIdx.x * 256 + c < a.N) a.part[(int64_t)b * a.N + blockIdx.x * 256 + c] = s;
+    }
   }
 }
 
-// dbias from the partial sums, added in fp64 in the order of the rows.
+// dbias from the partial sums, added in fp64, each quarter of them in the order of the rows.
 __global__ __launch_bounds__(256) void k_lin_dbias(const float* __restrict__ part, int blocks, int N, void* dbias,
                                                    bool bf16) {
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
+  __shared__ double sh[4][64];
+  const int c = threadIdx.x & 63, l = threadIdx.x >> 6, n = blockIdx.x * 64 + c;
   double sum = 0.0;
-  for (int b = 0; b < blocks; ++b) sum += (double)part[(int64_t)b * N + n];
-  store_any(dbias, n, (float)sum, bf16);
+  if (n < N) {
+#pragma unroll 8
+    for (int b = l; b < blocks; b += 4) sum += (double)part[(int64_t)b * N + n];
+  }
+  sh[l][c] = sum;
+  __syncthreads();
+  if (l == 0 && n < N) store_any(dbias, n, (float)((sh[0][c] + sh[1][c]) + (sh[2][c] + sh[3][c])), bf16);
 }
 
 // ---- host -----------------------------------------------------------------------
@@ -539,7 +581,7 @@ extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t
     const dim3 grid((unsigned)((up8(op->N) + 255) / 256), (unsigned)std::min(blocks, 16384));
     with_act(op->act, [&](auto kind) { hipLaunchKernelGGL(k_lin_dz<decltype(kind)::value>, grid, dim3(256), 0, s, a); });
     if (part)
-      hipLaunchKernelGGL(k_lin_dbias, dim3((unsigned)((op->N + 255) / 256)), dim3(256), 0, s, part, blocks, (int)op->N,
+      hipLaunchKernelGGL(k_lin_dbias, dim3((unsigned)((op->N + 63) / 64)), dim3(256), 0, s, part, blocks, (int)op->N,
                          g.dbias, op->bias_dtype == GRPO_BF16);
   }
   if (dz) p.dz_rows.src = p.dz_cols.src = dz;

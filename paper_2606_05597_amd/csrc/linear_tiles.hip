@@ -178,28 +178,39 @@ __device__ __forceinline__ void wave_order() {
 }
 
 // A wave's sums, 32 rows at a time, through its own part of the LDS into rows of 16-byte vectors: out of the registers
-// they would be stored 64 bytes to a row.
-template <class C, int ACT>
+// they would be stored 64 bytes to a row.  FULL: the tile lies inside C; what is added to the rows is then on its way
+// before the 32 rows before them are done (nothing else on the CU hides a load here: 8 rows at a time, each waiting for
+// its own, 8,192 x 3,584 x 3,584 with a residual took 235 us).
+template <class C, int ACT, bool FULL>
 __device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, int M, int N,
                                             const g_f32x16 (&acc)[C::IB][C::JB], float* lds) {
-  constexpr int LD = C::WTN + 4, LPR = C::WTN / 8, RPS = 64 / LPR;  // lanes to a row, rows to a step
+  constexpr int LD = C::WTN + 4, LPR = C::WTN / 8, RPS = 64 / LPR, STEPS = 32 / RPS;  // lanes to a row, rows to a step
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WGN, wn = wave % C::WGN;
   float* mine = lds + wave * 32 * LD;
   const int cl = lane % LPR * 8, n = n0 + wn * C::WTN + cl;
   float bias[8];
 #pragma unroll
   for (int q = 0; q < 8; ++q) bias[q] = e.bias && n + q < N ? load_any(e.bias, n + q, e.bias_bf16) : 0.f;
+  const void* more = e.residual ? e.residual : e.accumulate ? e.out : nullptr;
+  const int64_t ldm = e.residual ? e.ldr : e.ldo;
+  Raw8 r[2][STEPS];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q)
+      r[i & 1][q].load(more, (int64_t)(m0 + wm * C::WTM + i * 32 + q * RPS + lane / LPR) * ldm + n, e.out_bf16);
+  };
+  if (FULL && more) fetch(0);
 #pragma unroll
   for (int i = 0; i < C::IB; ++i) {
+    if (FULL && more && i + 1 < C::IB) fetch(i + 1);
 #pragma unroll
     for (int j = 0; j < C::JB; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mine[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * LD + j * 32 + (lane & 31)] = acc[i][j][r];
+      for (int k = 0; k < 16; ++k) mine[(8 * (k >> 2) + 4 * (lane >> 5) + (k & 3)) * LD + j * 32 + (lane & 31)] = acc[i][j][k];
     wave_order();
-#pragma unroll 1
-    for (int q = 0; q < 32; q += RPS) {
-      const int rl = q + lane / LPR, m = m0 + wm * C::WTM + i * 32 + rl;
-      if (m >= M || n >= N) continue;
+    auto step = [&](int q) {
+      const int rl = q * RPS + lane / LPR, m = m0 + wm * C::WTM + i * 32 + rl;
+      if (!FULL && (m >= M || n >= N)) return;
       float v[8];
       const lin_f32x4* src = reinterpret_cast<const lin_f32x4*>(mine + rl * LD + cl);
       const lin_f32x4 a = src[0], b = src[1];
@@ -208,10 +219,25 @@ __device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, i
         v[k] = a[k];
         v[k + 4] = b[k];
       }
-      finish8<ACT>(e, m, n, N, bias, v);
+      if constexpr (FULL) finish_whole8<ACT>(e, m, n, N, bias, more ? &r[i & 1][q] : nullptr, v);
+      else finish8<ACT>(e, m, n, N, bias, v);
+    };
+    if constexpr (FULL) {
+#pragma unroll
+      for (int q = 0; q < STEPS; ++q) step(q);
+    } else {
+#pragma unroll 1
+      for (int q = 0; q < STEPS; ++q) step(q);
     }
     wave_order();
   }
+}
+
+template <class C, int ACT>
+__device__ __forceinline__ void finish(const Epilogue& e, int m0, int n0, int M, int N, const g_f32x16 (&acc)[C::IB][C::JB],
+                                       float* lds) {
+  if (m0 + C::BM <= M && n0 + C::BN <= N) finish_tile<C, ACT, true>(e, m0, n0, M, N, acc, lds);
+  else finish_tile<C, ACT, false>(e, m0, n0, M, N, acc, lds);
 }
 
 template <class C, bool AT, bool BT, int ACT>
@@ -230,9 +256,9 @@ __global__ __launch_bounds__(C::NT) void k_lin_tiles(const TileArgs t) {
     Epilogue e{};
     e.out = t.part + (int64_t)split * t.M * t.N;
     e.ldo = t.N;
-    finish_tile<C, GRPO_ACT_NONE>(e, m0, n0, t.M, t.N, acc, reinterpret_cast<float*>(lds));
+    finish<C, GRPO_ACT_NONE>(e, m0, n0, t.M, t.N, acc, reinterpret_cast<float*>(lds));
   } else {
-    finish_tile<C, ACT>(t.e, m0, n0, t.M, t.N, acc, reinterpret_cast<float*>(lds));
+    finish<C, ACT>(t.e, m0, n0, t.M, t.N, acc, reinterpret_cast<float*>(lds));
   }
 }
 
