@@ -84,6 +84,8 @@ struct Epilogue {
   float* z;  // [M, N] or NULL
   int act;
   bool out_bf16, bias_bf16, accumulate;
+  // Results that the memory-side cache cannot hold pass the L2: 3,584 x 151,936 from 64 summed over, bf16, 253 us against 311.
+  bool past;
 };
 
 // 8 columns of a row, at any alignment of their elements.
@@ -102,12 +104,18 @@ __device__ __forceinline__ void load8(const void* p, int64_t i, bool bf16, float
     }
   }
 }
-__device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const float (&v)[8]) {
+__device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const float (&v)[8], bool past = false) {
   if (bf16) {
     u32x4 x;
 #pragma unroll
     for (int q = 0; q < 4; ++q) x[q] = pack_bf16(v[2 * q], v[2 * q + 1]);
-    *reinterpret_cast<u32x4_a2*>(static_cast<uint16_t*>(p) + i) = x;
+    u32x4_a2* o = reinterpret_cast<u32x4_a2*>(static_cast<uint16_t*>(p) + i);
+    if (past) {
+      __builtin_nontemporal_store(x, o);
+      asm volatile("; past the L2" ::: "memory");  // keeps the two stores from being taken for one
+    } else {
+      *o = x;
+    }
   } else {
     u32x4 a, b;
 #pragma unroll
@@ -116,8 +124,14 @@ __device__ __forceinline__ void store8(void* p, int64_t i, bool bf16, const floa
       b[q] = __float_as_uint(v[q + 4]);
     }
     u32x4_a4* x = reinterpret_cast<u32x4_a4*>(static_cast<float*>(p) + i);
-    x[0] = a;
-    x[1] = b;
+    if (past) {
+      __builtin_nontemporal_store(a, x);
+      __builtin_nontemporal_store(b, x + 1);
+      asm volatile("; past the L2" ::: "memory");
+    } else {
+      x[0] = a;
+      x[1] = b;
+    }
   }
   asm volatile("s_nop 1" ::: "memory");  // the stores have read their data before their registers are reused
 }
@@ -157,7 +171,7 @@ __device__ __forceinline__ void finish_whole8(const Epilogue& e, int m, int n, i
       for (int q = 0; q < 8; ++q) v[q] += r->at(q, false);
     }
   }
-  store8(e.out, (int64_t)m * e.ldo + n, e.out_bf16, v);
+  store8(e.out, (int64_t)m * e.ldo + n, e.out_bf16, v, e.past);
 }
 
 // The same of the columns below N.
@@ -188,7 +202,7 @@ __device__ __forceinline__ void finish8(const Epilogue& e, int m, int n, int N, 
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] += r[q];
   }
-  if (all) store8(e.out, o, e.out_bf16, v);
+  if (all) store8(e.out, o, e.out_bf16, v, e.past);
   else
 #pragma unroll
     for (int q = 0; q < 8; ++q)

@@ -312,6 +312,7 @@ __global__ __launch_bounds__(256) void k_lin_dbias(const float* __restrict__ par
 
 // ---- host -----------------------------------------------------------------------
 constexpr int64_t kCus = 256;
+constexpr int64_t kPastL2 = (int64_t)256 << 20;  // bytes of a result that passes the L2
 constexpr int64_t kMostLin = 8388352;  // 2^23 - 256: 256 rows of an operand stay below 4 GB
 
 static int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -343,6 +344,39 @@ static TileOperand lay_out(const Operand& o, char*& ws, hipStream_t s) {
   return TileOperand{dst, ld, o.turned};
 }
 
+// Tile shape and splits of the shortest launch, by what a CU was seen to take (us): for 64 summed over of a tile, with as
+// many tiles beside it as the CU holds (`full`, of `slots`) or alone; for a tile's first loads and its epilogue; for the
+// splits' sums, written, read and joined by a launch of their own.  Measured with bf16 operands of either layout (us, 256 x
+// 256, 128 x 128 and 64 x 128 tiles): 8,192 x 3,584 x 3,584 193, 233, 299; 304 x 32,000 x 3,584 95, 90, 103; 64 x 32,000 x
+// 3,584 83, 45, 44 and split in two 52, 39, 39; 512 x 2,048 x 2,048 47, 22, 24 and in four 22, 14, 16; 2,048 x 3,584 x
+// 151,936 in two 1,937, 2,409, 3,537, whole 3,480, 2,359, 4,233.
+static void plan_tiles(int64_t M, int64_t N, int64_t K, int& shape, int& splits, int& range) {
+  static const struct {
+    int slots;
+    double full, alone, ends;
+  } kCost[] = {{1, 1.70, 1.45, 9.0}, {2, 0.56, 0.78, 3.0}, {3, 0.36, 0.74, 2.0}};
+  const int64_t slabs = (K + 63) / 64;
+  double best = 0.0;
+  for (int s = 0; s < 3; ++s) {
+    const TileShape& t = kTileShapes[s];
+    const int64_t tiles = ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n);
+    for (int64_t k = 1; k <= 16 && (k == 1 || (k * 4 <= slabs && tiles * k <= 8 * kCus)); ++k) {
+      const int64_t per = (slabs + k - 1) / k;
+      if ((k - 1) * per >= slabs) continue;
+      const int64_t rounds = (tiles * k + kCus - 1) / kCus, turns = (rounds + kCost[s].slots - 1) / kCost[s].slots;
+      double us = std::max((double)rounds * (per * kCost[s].full + kCost[s].ends / 2),
+                           (double)turns * (per * kCost[s].alone + kCost[s].ends));
+      if (k > 1) us += 4.0 + (double)k * M * N * 8.0 / 5e6;
+      if (best == 0.0 || us < best) {
+        best = us;
+        shape = s;
+        splits = (int)k;
+        range = (int)per * 64;
+      }
+    }
+  }
+}
+
 // How a product is done: by the kernel for few rows, in `splits` parts of the summed dimension, or by tiles.
 struct ProductPlan {
   bool few;
@@ -363,12 +397,7 @@ static ProductPlan product_plan(const Operand& a, const Operand& b) {
     const int64_t waves = (int64_t)p.splits * kFewWaves;
     p.range = (int)((steps + waves - 1) / waves * 32);
   } else {
-    p.shape = a.rows <= 64 ? 2 : a.rows <= 128 || a.rows * b.rows < (int64_t)128 * 256 * 256 ? 1 : 0;
-    const TileShape& t = kTileShapes[p.shape];
-    const int64_t tiles = ((a.rows + t.m - 1) / t.m) * ((b.rows + t.n - 1) / t.n), slabs = (K + 63) / 64;
-    int64_t splits = std::max<int64_t>(1, std::min<int64_t>({slabs / 8, kCus / tiles, 16}));
-    p.range = (int)((slabs + splits - 1) / splits * 64);
-    p.splits = (int)((K + p.range - 1) / p.range);
+    plan_tiles(a.rows, b.rows, K, p.shape, p.splits, p.range);
   }
   if (p.splits > 1) p.part = align_up(4 * (size_t)p.splits * (size_t)a.rows * (size_t)b.rows);
   return p;
@@ -536,7 +565,8 @@ extern "C" int grpo_linear(const grpo_linear_op* op, const void* residual, int64
   }
   if (op->M > 0) {
     char* at = static_cast<char*>(ws);
-    const Epilogue e{y, ldy, op->bias, residual, ldr, z, op->act, y_dtype == GRPO_BF16, op->bias_dtype == GRPO_BF16, false};
+    const Epilogue e{y, ldy, op->bias, residual, ldr, z, op->act, y_dtype == GRPO_BF16, op->bias_dtype == GRPO_BF16, false,
+                     op->M * op->N * (int64_t)size_of(y_dtype) > kPastL2};
     launch_product(x_rows(*op), w_as_nk(*op), e, at, s);
   }
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
@@ -586,12 +616,13 @@ extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t
   }
   if (dz) p.dz_rows.src = p.dz_cols.src = dz;
   if (g.dx) {
-    const Epilogue e{g.dx, op->K, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE, true, false, false};
+    const Epilogue e{g.dx, op->K, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE, true, false, false,
+                     op->M * op->K * 2 > kPastL2};
     launch_product(p.dz_rows, p.w, e, at, s);
   }
   if (g.dw) {
     const Epilogue e{g.dw, op->w_out_in ? op->K : op->N, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE,
-                     g.dw_dtype == GRPO_BF16, false, g.accumulate_dw == 1};
+                     g.dw_dtype == GRPO_BF16, false, g.accumulate_dw == 1, op->K * op->N * (int64_t)size_of(g.dw_dtype) > kPastL2};
     launch_product(op->w_out_in ? p.dz_cols : p.x_cols, op->w_out_in ? p.x_cols : p.dz_cols, e, at, s);
   }
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
