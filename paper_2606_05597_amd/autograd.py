@@ -243,7 +243,7 @@ class Linear(torch.autograd.Function):
         need = ctx.needs_input_grad
         dx = dw = db = None
         if any(need[:3]):
-            if dy.dim() == 2 and dy.stride(1) != 1:
+            if dy.stride(1) != 1 or dy.stride(0) < dy.shape[1]:  # also rows that a sum's gradient repeats
                 dy = dy.contiguous()
             db = torch.empty(w.shape[1], dtype=ctx.bias_dtype, device=w.device) if need[2] else None
             dx, dw, db = grpo_linear_bwd(dy, x, w, z, act=ctx.act, dx=bool(need[0]), dw=bool(need[1]), dbias=db)

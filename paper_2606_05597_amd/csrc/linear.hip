@@ -189,20 +189,20 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_lin_few(const FewArgs a) {
   }
 }
 
-// The sums of the splits joined in their order, then the epilogue: a thread to 8 columns of a row.
+// The sums of the splits joined in their order, then the epilogue: a wave to 512 columns of a row.
 template <int ACT>
 __global__ __launch_bounds__(256) void k_lin_join(const float* __restrict__ part, int splits, int M, int N,
                                                   const Epilogue e) {
-  const int per = (N + 7) / 8;
-  const int64_t total = (int64_t)M * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int m = (int)(i / per), n = (int)(i % per) * 8;
-    float v[8], bias[8];
+  const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
+  if (n >= N) return;
+  float bias[8];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      v[q] = 0.f;
-      bias[q] = e.bias && n + q < N ? load_any(e.bias, n + q, e.bias_bf16) : 0.f;
-    }
+  for (int q = 0; q < 8; ++q) bias[q] = e.bias && n + q < N ? load_any(e.bias, n + q, e.bias_bf16) : 0.f;
+  for (int m = blockIdx.y * 4 + (threadIdx.x >> 6); m < M; m += gridDim.y * 4) {
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = 0.f;
+#pragma unroll 2
     for (int s = 0; s < splits; ++s) {
       const float* p = part + ((int64_t)s * M + m) * N + n;
       float u[8];
@@ -438,8 +438,7 @@ static void launch_few(const FewArgs& f, bool kn, hipStream_t s) {
 }
 
 static void join_splits(const float* part, int splits, int M, int N, const Epilogue& e, hipStream_t s) {
-  const int64_t n = (int64_t)M * ((N + 7) / 8);
-  const dim3 grid((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), block(256);
+  const dim3 grid((unsigned)((N + 511) / 512), (unsigned)std::min((M + 3) / 4, 16384)), block(256);
   auto go = [&](auto act) { hipLaunchKernelGGL(k_lin_join<decltype(act)::value>, grid, block, 0, s, part, splits, M, N, e); };
   with_act(e.act, go);
 }

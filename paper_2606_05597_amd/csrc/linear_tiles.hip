@@ -178,8 +178,8 @@ __device__ __forceinline__ void wave_order() {
 }
 
 // A wave's sums, 32 rows at a time, through its own part of the LDS into rows of 16-byte vectors: out of the registers
-// they would be stored 64 bytes to a row.  FULL: the tile lies inside C; what is added to the rows is then on its way
-// before the 32 rows before them are done (nothing else on the CU hides a load here: 8 rows at a time, each waiting for
+// they would be stored 64 bytes to a row.  FULL: the tile's columns lie inside C; what is added to the rows is then on its
+// way before the 32 rows before them are done (nothing else on the CU hides a load here: 8 rows at a time, each waiting for
 // its own, 8,192 x 3,584 x 3,584 with a residual took 235 us).
 template <class C, int ACT, bool FULL>
 __device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, int M, int N,
@@ -187,7 +187,7 @@ __device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, i
   constexpr int LD = C::WTN + 4, LPR = C::WTN / 8, RPS = 64 / LPR, STEPS = 32 / RPS;  // lanes to a row, rows to a step
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / C::WGN, wn = wave % C::WGN;
   float* mine = lds + wave * 32 * LD;
-  const int cl = lane % LPR * 8, n = n0 + wn * C::WTN + cl;
+  const int cl = lane % LPR * 8, n = n0 + wn * C::WTN + cl, mw = m0 + wm * C::WTM + lane / LPR;
   float bias[8];
 #pragma unroll
   for (int q = 0; q < 8; ++q) bias[q] = e.bias && n + q < N ? load_any(e.bias, n + q, e.bias_bf16) : 0.f;
@@ -196,8 +196,7 @@ __device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, i
   Raw8 r[2][STEPS];
   auto fetch = [&](int i) {
 #pragma unroll
-    for (int q = 0; q < STEPS; ++q)
-      r[i & 1][q].load(more, (int64_t)(m0 + wm * C::WTM + i * 32 + q * RPS + lane / LPR) * ldm + n, e.out_bf16);
+    for (int q = 0; q < STEPS; ++q) r[i & 1][q].load(more, min(mw + i * 32 + q * RPS, M - 1) * ldm + n, e.out_bf16);
   };
   if (FULL && more) fetch(0);
 #pragma unroll
@@ -209,10 +208,10 @@ __device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, i
       for (int k = 0; k < 16; ++k) mine[(8 * (k >> 2) + 4 * (lane >> 5) + (k & 3)) * LD + j * 32 + (lane & 31)] = acc[i][j][k];
     wave_order();
     auto step = [&](int q) {
-      const int rl = q * RPS + lane / LPR, m = m0 + wm * C::WTM + i * 32 + rl;
-      if (!FULL && (m >= M || n >= N)) return;
+      const int m = mw + i * 32 + q * RPS;
+      if (m >= M || (!FULL && n >= N)) return;
       float v[8];
-      const lin_f32x4* src = reinterpret_cast<const lin_f32x4*>(mine + rl * LD + cl);
+      const lin_f32x4* src = reinterpret_cast<const lin_f32x4*>(mine + (q * RPS + lane / LPR) * LD + cl);
       const lin_f32x4 a = src[0], b = src[1];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -236,7 +235,7 @@ __device__ __forceinline__ void finish_tile(const Epilogue& e, int m0, int n0, i
 template <class C, int ACT>
 __device__ __forceinline__ void finish(const Epilogue& e, int m0, int n0, int M, int N, const g_f32x16 (&acc)[C::IB][C::JB],
                                        float* lds) {
-  if (m0 + C::BM <= M && n0 + C::BN <= N) finish_tile<C, ACT, true>(e, m0, n0, M, N, acc, lds);
+  if (n0 + C::BN <= N) finish_tile<C, ACT, true>(e, m0, n0, M, N, acc, lds);
   else finish_tile<C, ACT, false>(e, m0, n0, M, N, acc, lds);
 }
 
