@@ -230,7 +230,7 @@ struct TileArgs {
 struct TileShape {
   int m, n;
 };
-constexpr TileShape kTileShapes[] = {{256, 256}, {128, 128}, {64, 128}};
+constexpr TileShape kTileShapes[] = {{256, 256}, {128, 128}, {64, 128}, {192, 256}};
 
 // C [M, N] = A B^T, with the epilogue where it is not split.
 void launch_tiles(const TileArgs& t, int shape, hipStream_t s);

@@ -347,17 +347,17 @@ static TileOperand lay_out(const Operand& o, char*& ws, hipStream_t s) {
 // Tile shape and splits of the shortest launch, by what a CU was seen to take (us): for 64 summed over of a tile, with as
 // many tiles beside it as the CU holds (`full`, of `slots`) or alone; for a tile's first loads and its epilogue; for the
 // splits' sums, written, read and joined by a launch of their own.  Measured with bf16 operands of either layout (us, 256 x
-// 256, 128 x 128 and 64 x 128 tiles): 8,192 x 3,584 x 3,584 193, 233, 299; 304 x 32,000 x 3,584 95, 90, 103; 64 x 32,000 x
-// 3,584 83, 45, 44 and split in two 52, 39, 39; 512 x 2,048 x 2,048 47, 22, 24 and in four 22, 14, 16; 2,048 x 3,584 x
-// 151,936 in two 1,937, 2,409, 3,537, whole 3,480, 2,359, 4,233.
+// 256, 128 x 128, 64 x 128 and 192 x 256 tiles): 8,192 x 3,584 x 3,584 182, 200, 253, 216; 300 x 32,000 x 3,584 100, 115, 134,
+// 82; 128 x 32,000 x 3,584 81, 50, 49, 66 and split in two 53, 42, 58, 48; 512 x 2,048 x 2,048 48, 22, 24, 40 and in two 29,
+// 15, 16, 25; 2,048 x 3,584 x 151,936 whole 3,480, 2,359, 4,233, in two (256 x 256) 1,937.
 static void plan_tiles(int64_t M, int64_t N, int64_t K, int& shape, int& splits, int& range) {
   static const struct {
     int slots;
     double full, alone, ends;
-  } kCost[] = {{1, 1.70, 1.45, 9.0}, {2, 0.56, 0.78, 3.0}, {3, 0.36, 0.74, 2.0}};
+  } kCost[] = {{1, 1.70, 1.45, 9.0}, {2, 0.56, 0.78, 3.0}, {3, 0.36, 0.74, 2.0}, {1, 1.30, 1.12, 8.0}};
   const int64_t slabs = (K + 63) / 64;
   double best = 0.0;
-  for (int s = 0; s < 3; ++s) {
+  for (int s = 0; s < 4; ++s) {
     const TileShape& t = kTileShapes[s];
     const int64_t tiles = ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n);
     for (int64_t k = 1; k <= 16 && (k == 1 || (k * 4 <= slabs && tiles * k <= 8 * kCus)); ++k) {

@@ -43,7 +43,7 @@ struct Side {
     lane = lane_;
     if constexpr (TURNED) {
       const int i = lane & 15, k = 8 * (lane >> 5) + (i >> 2);  // row k of the first read
-      const int x = R >= 128 ? i >> 2 : i >> 3;                 // exchange of the slots, in fours
+      const int x = exchange(k);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const int slot = (((first / 32 + b) ^ x) << 2) | (((lane >> 4) & 1) << 1) | ((i & 3) >> 1);
@@ -57,17 +57,19 @@ struct Side {
     }
   }
 
+  // How many fours of slots row k's are exchanged by.  Rows of 256 or 512 bytes begin at the same bank, those of 128 or 384
+  // at two in turn.
+  static __device__ __forceinline__ int exchange(int k) { return R % 128 == 0 ? k & 3 : (k >> 1) & 1; }
+
   // Slab k0 .. k0 + 63 into LDS at byte address `at`.
   __device__ __forceinline__ void issue(uint32_t at, int k0) const {
     if constexpr (TURNED) {
       const int left = min(64, K - k0);
       const g_u32x4 rs = buffer_rsrc(base + (int64_t)k0 * ld, (uint32_t)(((int64_t)(left - 1) * ld + rows) * 2));
-      constexpr int RPI = 64 / SLOTS;  // rows k to an instruction
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        const int i = q * NW + wave, k = i * RPI + lane / SLOTS, s = lane % SLOTS;
-        const int x = R >= 128 ? k & 3 : (k >> 1) & 1;
-        const int col = (s ^ (x << 2)) * 8;
+        const int i = q * NW + wave, v = i * 64 + lane, k = v / SLOTS, s = v % SLOTS;
+        const int col = (s ^ (exchange(k) << 2)) * 8;
         dma16(at + (uint32_t)i * 1024u, col < rows ? (uint32_t)(k * ld + col) * 2u : kOobOffset, rs);
       }
     } else {
@@ -289,7 +291,8 @@ void launch_tiles(const TileArgs& t, int shape, hipStream_t s) {
   switch (shape) {
     case 0: return launch_shape<GemmCfg<256, 256, 2, 4>>(t, s);
     case 1: return launch_shape<GemmCfg<128, 128, 2, 2>>(t, s);
-    default: return launch_shape<GemmCfg<64, 128, 1, 2>>(t, s);
+    case 2: return launch_shape<GemmCfg<64, 128, 1, 2>>(t, s);
+    default: return launch_shape<GemmCfg<192, 256, 2, 4>>(t, s);
   }
 }
 
