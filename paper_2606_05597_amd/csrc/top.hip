@@ -25,7 +25,8 @@
 namespace grpo {
 
 constexpr int kMostGroups = 256;  // chunks of four lanes that are read again
-constexpr int kTopCap = 1024;     // words the list holds
+constexpr int kTopCap = 1024;     // words the list holds (a quarter of them for rows of one wave)
+constexpr int kShort = 128;       // words that are ranked against one another at once
 constexpr uint32_t kNothing = 0;  // the key of no word (a word's is larger)
 
 // A row's part of a workgroup: its sums relative to max, in units of log 2.
@@ -125,6 +126,10 @@ __device__ __forceinline__ float scale_of(float tau) {
 
 constexpr int kSlices = 32;  // chunks, or runs of chunks, of a lane that have a maximum of their own
 
+// The thread that finishes a row: of the second wave, beside the first one's search for the bound.
+template <int NT>
+constexpr int kFinisher = NT > 64 ? 64 : 0;
+
 template <int NT>
 struct TopSmem {
   float m[NT / 64];
@@ -136,7 +141,10 @@ struct TopSmem {
   int n_groups, count;
   int wave_count[NT / 64];
   uint16_t groups[kMostGroups];
-  uint64_t list[kTopCap];
+  static constexpr int kCap = NT > 64 ? kTopCap : kTopCap / 4;
+  uint64_t list[kCap];
+  uint64_t first[kShort];
+  int n_first;
 };
 
 // All threads' sums joined in fp64 at the shift of the row's maximum M, in every thread.
@@ -220,19 +228,6 @@ struct TopOut {
   }
 };
 
-// The list's first n words in order; the rest of the n places empty.  Every thread of the workgroup.
-template <int NT, class Smem>
-__device__ __forceinline__ void rank_list(const Smem& sm, int c, int n, const TopOut& out) {
-  const int tid = threadIdx.x;
-  for (int i = tid; i < c; i += NT) {
-    const uint64_t key = sm.list[i];
-    int rank = 0;
-    for (int j = 0; j < c; ++j) rank += sm.list[j] > key;
-    if (rank < n) out.put(rank, key);
-  }
-  for (int j = c + tid; j < n; j += NT) out.none(j, false);
-}
-
 // The n-th largest of 64 `per` 16-bit keys, those of a lane the first `per` in k: one wave.
 template <int PER>
 __device__ __forceinline__ uint32_t nth_largest(const uint32_t (&k)[PER], int per, int n) {
@@ -247,6 +242,51 @@ __device__ __forceinline__ uint32_t nth_largest(const uint32_t (&k)[PER], int pe
     if (cnt >= n) p = c;
   }
   return p;
+}
+
+// The list's first n words in order; the rest of the n places empty.  Every thread of the workgroup.  Of a long list the
+// words below the n-th largest (by the upper 16 bits of their order) are left out before they are ranked.
+template <int NT, class Smem>
+__device__ __forceinline__ void rank_list(Smem& sm, int c, int n, const TopOut& out) {
+  const int tid = threadIdx.x;
+  const uint64_t* list = sm.list;
+  int k = c;
+  if (c > kShort) {
+    constexpr int PER = Smem::kCap / 64;
+    if (tid < 64) {
+      uint32_t key[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) key[i] = tid + 64 * i < c ? (uint32_t)(sm.list[tid + 64 * i] >> 48) : 0u;
+      const uint32_t b = nth_largest(key, (c + 63) / 64, n);
+      if (tid == 0) {
+        sm.bound = b;
+        sm.n_first = 0;
+      }
+    }
+    __syncthreads();
+    const uint32_t b = sm.bound;
+    for (int i = tid; i < c; i += NT) {
+      const uint64_t key = sm.list[i];
+      if ((uint32_t)(key >> 48) < b) continue;
+      const int at = atomicAdd(&sm.n_first, 1);
+      if (at < kShort) sm.first[at] = key;
+    }
+    __syncthreads();
+    if (sm.n_first <= kShort) {
+      list = sm.first;
+      k = sm.n_first;
+    }
+  }
+  for (int i = tid; i < k; i += NT) {
+    const uint64_t key = list[i];
+    int rank = 0;
+    for (int j0 = 0; j0 < k; j0 += 8) {  // eight reads of the LDS at a time
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rank += j0 + j < k && list[min(j0 + j, k - 1)] > key;
+    }
+    if (rank < n) out.put(rank, key);
+  }
+  for (int j = c + tid; j < n; j += NT) out.none(j, false);
 }
 
 // The sum of v over the workgroup, in every thread.
@@ -367,7 +407,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
   const float ez = tid < n_edge ? load_elem(row + nvec * EPV + tid) : -INFINITY;
   int act = -1;
   float za = -INFINITY;  // the action's logit, for the thread that finishes the row
-  if (!PART && tid == 64) {
+  if (!PART && tid == kFinisher<NT>) {
     act = a.actions[t];
     if (act >= 0 && act < a.V) za = load_elem(row + act);
   }
@@ -434,8 +474,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
   join_threads<NT>(sum, sc, sm, M, S, Tsum);
   const bool bad = isnan(S) || isnan(M) || M == INFINITY || isnan(sc), some = !bad && S > 0.0;
   if (PART) {
-    if (tid == 64) a.part[(int64_t)t * a.parts + part] = TopPart{bad ? (double)NAN : S, Tsum, some ? M : kShiftMin, 0.f};
-  } else if (tid == 64) {
+    if (tid == kFinisher<NT>) a.part[(int64_t)t * a.parts + part] = TopPart{bad ? (double)NAN : S, Tsum, some ? M : kShiftMin, 0.f};
+  } else if (tid == kFinisher<NT>) {
     const grpo_top_row r = finish_row(a, t, act, za, tau, M, S, Tsum);
     sm.log_sum = r.log_sum;
   }
@@ -466,7 +506,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
   auto take = [&](float z, int idx) {
     if (z >= least && is_word(z)) {
       const int i = atomicAdd(&sm.count, 1);
-      if (i < kTopCap) sm.list[i] = key_of(z, c0 + idx);
+      if (i < sm.kCap) sm.list[i] = key_of(z, c0 + idx);
     }
   };
   if (tid < n_edge) take(ez, nvec * EPV + tid);
@@ -491,7 +531,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
       for (int e = 0; e < EPV; ++e) take(elem<Tin>(x, e), vi * EPV + e);
     }
     __syncthreads();
-    fits = sm.count <= kTopCap;
+    fits = sm.count <= sm.kCap;
   }
   if (fits) rank_list<NT>(sm, sm.count, n, out);
   else top_by_counts<Tin, NT>(row, cols, n, M, sm, out);
@@ -500,10 +540,12 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
 // A row's parts joined: one workgroup to a row.
 constexpr int kJoinNT = 256;
 struct JoinSmem {
-  uint64_t list[kTopCap];
+  static constexpr int kCap = kTopCap;
+  uint64_t list[kCap];
+  uint64_t first[kShort];
   double log_sum;
   uint32_t bound;
-  int count;
+  int count, n_first;
 };
 template <typename Tin>
 __global__ __launch_bounds__(kJoinNT) void k_top_join(const TopArgs a) {
@@ -580,26 +622,24 @@ struct TopBwdArgs {
   const float* dtop;
 };
 
-constexpr int kTopBwdNT = 256, kTopBwdCols = 8192;
+constexpr int kTopBwdCols = 8192;
 
-// One workgroup to kTopBwdCols columns of a row.  A word's log2 p is formed from z - max, which keeps the exponent's
+// One workgroup to COLS columns of a row.  A word's log2 p is formed from z - max, which keeps the exponent's
 // rounding small whatever max and tau are.
-template <typename Tin>
-__global__ __launch_bounds__(kTopBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_top_bwd(const TopBwdArgs a,
-                                                                                                int row0) {
-  constexpr int NT = kTopBwdNT, EPV = 16 / (int)sizeof(Tin), U = kTopBwdCols / NT / EPV;
+template <typename Tin, int NT, int COLS>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 8))) void k_top_bwd(const TopBwdArgs a, int row0) {
+  constexpr int EPV = 16 / (int)sizeof(Tin), U = COLS / NT / EPV;
   typedef typename VecAt<Tin>::type u32x4_any;
-  __shared__ int sh_id[GRPO_TOP_MAX];
-  __shared__ float sh_c[GRPO_TOP_MAX];
   __shared__ double sh_sum;
-  __shared__ int sh_col[GRPO_TOP_MAX + 1];  // this workgroup's words with a coefficient, and their gradients
-  __shared__ float sh_d[GRPO_TOP_MAX + 1];
+  // this workgroup's words with a coefficient: their columns, gradients and the threads that store their vectors
+  __shared__ int sh_col[GRPO_TOP_MAX + 8], sh_owner[GRPO_TOP_MAX + 8];
+  __shared__ float sh_d[GRPO_TOP_MAX + 8];
   __shared__ int sh_count;
   const int t = row0 + (int)(blockIdx.x / (unsigned)a.blocks), b = (int)(blockIdx.x % (unsigned)a.blocks);
   const int tid = threadIdx.x, n = a.n;
   const Tin* row = static_cast<const Tin*>(a.logits) + (int64_t)t * a.ld;
   Tin* drow = static_cast<Tin*>(a.dlogits) + (int64_t)t * a.ld;
-  const int c0 = b * kTopBwdCols, edge = a.V / EPV * EPV;
+  const int c0 = b * COLS, c1 = min(c0 + COLS, a.V), edge = a.V / EPV * EPV;
   const int n_edge = b == a.blocks - 1 ? a.V - edge : 0;
   u32x4 x[U];
 #pragma unroll
@@ -609,56 +649,55 @@ __global__ __launch_bounds__(kTopBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8)
   }
   const float ez = tid < n_edge ? load_elem(row + edge + tid) : 0.f;
   const grpo_top_row r = a.rows[t];
-  const int act = a.actions[t];
   const bool nan = isnan(r.log_sum), none = r.max == -INFINITY;
-  const bool act_on = a.dlogp && act >= 0 && act < a.V && r.logp > -INFINITY;
-  const float d_act = act_on ? a.dlogp[t] : 0.f;
+  const double g = a.dent ? (double)a.dent[t] : 0.0, inv = 1.0 / (double)r.temperature;
   if (tid < 64) {
+    const int act = a.actions[t];
+    const bool act_on = a.dlogp && act >= 0 && act < a.V && r.logp > -INFINITY;
+    const float d_act = act_on ? a.dlogp[t] : 0.f;
     int id = -1;
-    float c = 0.f;
+    float up = 0.f;
     if (tid < n) {
       id = a.ids[(int64_t)t * n + tid];
-      if (id >= 0 && id < a.V) c = a.dtop ? a.dtop[(int64_t)t * n + tid] : 0.f;
+      if (id >= 0 && id < a.V) up = a.dtop[(int64_t)t * n + tid];
       else id = -1;
     }
-    sh_id[tid] = id;
-    sh_c[tid] = c;
-    const double sum = wave_sum_dpp((double)c);
-    if (tid == 0) {
-      sh_sum = sum + (double)d_act;
-      sh_count = 0;
-    }
-  }
-  __syncthreads();
-  const double C = sh_sum, g = a.dent ? (double)a.dent[t] : 0.0, inv = 1.0 / (double)r.temperature;
-  // the words with a coefficient of their own in these columns, each once, in fp64
-  if (tid <= n && !nan && !none) {
-    int id = -1;
-    double c = 0.0;
-    if (tid < n) {
-      id = sh_id[tid];
-      for (int j = 0; j < n; ++j) {
-        if (sh_id[j] != id) continue;
-        if (j < tid) id = -2;  // an earlier one of the same word does it
-        c += (double)sh_c[j];
-      }
-      if (act_on && id == act) c += (double)d_act;
-    } else if (act_on) {
-      id = act;
-      c = (double)d_act;
-      for (int j = 0; j < n; ++j)
-        if (sh_id[j] == act) id = -1;
-    }
-    if (id >= c0 && id < min(c0 + kTopBwdCols, a.V)) {
-      const float z = load_elem(row + id);
+    const double C = wave_sum_dpp((double)up) + (double)d_act;
+    // the words with a coefficient of their own in these columns, each once, in fp64
+    auto special = [&](int col, double c) {
+      if (col < c0 || col >= c1) return;
+      const float z = load_elem(row + col);
       double d = 0.0;
       if (is_word(z)) {
         const double lp = ((double)z - (double)r.max) * inv - r.log_sum;
         d = (c - exp(lp) * (C + g * (lp + (double)r.entropy))) * inv;
       }
       const int i = atomicAdd(&sh_count, 1);
-      sh_col[i] = id;
+      sh_col[i] = col;
       sh_d[i] = (float)d;
+      sh_owner[i] = col >= edge ? col - edge : (col - c0) / EPV % NT;
+    };
+    if (tid == 0) {
+      sh_sum = C;
+      sh_count = 0;
+    }
+    if (!nan && !none) {
+      double c = (double)up + (act_on && id == act ? (double)d_act : 0.0);
+      bool twice = false, again = false;  // a word that is listed more than once; an earlier one of it does it
+      for (int j0 = 0; j0 < n; j0 += 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) twice |= __builtin_amdgcn_readlane(id, j0 + j) == id && j0 + j != tid;
+      }
+      if (__ballot(twice && id >= 0)) {
+        for (int j = 0; j < n; ++j) {
+          const bool same = __builtin_amdgcn_readlane(id, j) == id && j != tid;
+          c += same ? (double)__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, up), j)) : 0.0;
+          again |= same && j < tid;
+        }
+      }
+      const bool listed = __ballot(id == act) != 0;
+      if (id >= 0 && !again) special(id, c);
+      if (tid == 0 && act_on && !listed) special(act, (double)d_act);
     }
   }
   __syncthreads();
@@ -685,6 +724,7 @@ __global__ __launch_bounds__(kTopBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8)
     return;
   }
   // p (A log2 p + B)
+  const double C = sh_sum;
   const float sc = kLog2e / r.temperature, l2 = (float)(r.log_sum / kLn2), top = r.max;
   const float A = (float)(-g * kLn2 * inv), B = (float)(-(C + g * (double)r.entropy) * inv);
   store([&](float z) {
@@ -693,9 +733,14 @@ __global__ __launch_bounds__(kTopBwdNT) __attribute__((amdgpu_waves_per_eu(4, 8)
   });
   // by the thread that stored the word's place, after that store
   const int count = sh_count;
-  for (int i = 0; i < count; ++i) {
-    const int col = sh_col[i];
-    if (tid == (col >= edge ? col - edge : (col - c0) / EPV % NT)) store_elem(drow + col, sh_d[i]);
+  for (int i0 = 0; i0 < count; i0 += 8) {
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine |= (i0 + i < count && sh_owner[i0 + i] == tid) << i;
+    for (; mine; mine &= mine - 1) {
+      const int i = i0 + __ffs(mine) - 1;
+      store_elem(drow + sh_col[i], sh_d[i]);
+    }
   }
 }
 
@@ -713,6 +758,11 @@ static bool bad_top_shape(int64_t T, int64_t V, int64_t ld, int32_t n) {
 // 1,024 threads 21.7, with 256 31.7; T = 16: 22.3, 19.4, 17.6, 18.4, 18.7, 22.2, 32.2; T = 64: 23.8, 21.1, 21.2, 24.7, 29.5,
 // 22.8, 31.8; T = 256 whole 27.9 and 34.2, T = 512 48.3 and 39.3, T = 1,024 82.6 and 60.4).
 constexpr int64_t kFewTopRows = 48, kSomeTopRows = 400;
+// Short rows of which there are many go to one wave each (us, one wave and 256 threads, bf16: V = 1,000 T = 1,024 without
+// alternatives 7.5 and 7.2, with 8 11.2 and 10.5, T = 4,096 9.5 and 13.1, 14 and 21, T = 20,000 23 and 42, 38 and 77, with 33
+// 55 and 99; the gradient at T = 20,000 22 and 37, 31 and 60, with 64 49 and 110), but for more than 48 alternatives, which
+// the 64 lanes' maxima bound badly (with 64 at V = 4,000 T = 20,000 294 and 157).
+constexpr int64_t kOneWaveTopBytes = 8192, kManyTopRows = 2048;
 struct TopPlan {
   int parts, cols;
 };
@@ -744,7 +794,8 @@ static void launch_top(const TopArgs& a, int64_t T, hipStream_t s) {
     hipLaunchKernelGGL(k_top_join<Tin>, dim3((unsigned)T), dim3(kJoinNT), 0, s, a);
     return;
   }
-  if (T > kSomeTopRows || a.V <= 16384) launch_top_rows<Tin, 256>(a, T, s);
+  if (a.V * (int64_t)sizeof(Tin) <= kOneWaveTopBytes && T >= kManyTopRows && a.n <= 48) launch_top_rows<Tin, 64>(a, T, s);
+  else if (T > kSomeTopRows || a.V <= 16384) launch_top_rows<Tin, 256>(a, T, s);
   else launch_top_rows<Tin, 1024>(a, T, s);
 }
 
@@ -802,13 +853,21 @@ extern "C" int grpo_token_logp_top_bwd(const void* logits, int32_t dtype, int64_
       !aligned(rows, 8) || !aligned(dlogp, 4) || !aligned(dentropy, 4) || !aligned(dtop, 4))
     return GRPO_ERR_ALIGN;
   if (T > 0 && rows_overlap(logits, dlogits, T, V, ld, esz)) return GRPO_ERR_ARG;
-  const int blocks = (int)((V + kTopBwdCols - 1) / kTopBwdCols);
+  // Rows of one wave's reach go to one wave each.
+  const bool one_wave = V * (int64_t)esz <= kOneWaveTopBytes && T >= kManyTopRows;
+  const int blocks = one_wave ? 1 : (int)((V + kTopBwdCols - 1) / kTopBwdCols);
   const int64_t per = std::max<int64_t>(1, ((int64_t)1 << 23) / blocks);  // a launch's threads stay below 2^32
   for (int64_t r = 0; r < T; r += per) {
     const TopBwdArgs a{logits, dlogits, ld, (int)V, blocks, dtop ? n : 0, actions, top_ids, rows, dlogp, dentropy, dtop};
     const unsigned grid = (unsigned)(std::min(per, T - r) * blocks);
-    if (dtype == GRPO_BF16) hipLaunchKernelGGL(k_top_bwd<uint16_t>, dim3(grid), dim3(kTopBwdNT), 0, s, a, (int)r);
-    else hipLaunchKernelGGL(k_top_bwd<float>, dim3(grid), dim3(kTopBwdNT), 0, s, a, (int)r);
+    auto go = [&](auto kernel, int nt) { hipLaunchKernelGGL(kernel, dim3(grid), dim3((unsigned)nt), 0, s, a, (int)r); };
+    if (dtype == GRPO_BF16) {
+      if (one_wave) go(k_top_bwd<uint16_t, 64, 4096>, 64);
+      else go(k_top_bwd<uint16_t, 256, kTopBwdCols>, 256);
+    } else {
+      if (one_wave) go(k_top_bwd<float, 64, 2048>, 64);
+      else go(k_top_bwd<float, 256, kTopBwdCols>, 256);
+    }
   }
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
 }
