@@ -18,14 +18,17 @@
 namespace grpo {
 
 // ---- few rows ---------------------------------------------------------------------
-// Up to 32 rows: a product is then as long as reading W once takes.  A wave goes down its part of the summed dimension, 32
-// at a time, over 128 outputs, W's vectors from memory straight into the operands of v_mfma_f32_16x16x32_bf16 (a lane: 8
-// consecutive k of one column):
-//   rows of W along the outputs (KN): a lane reads 8 columns of 8 rows and turns them in its registers (v_perm), so that
-//     fragment c holds its column c;
-//   rows along the summed dimension: a lane reads 8 k of a row, fragment c of row 8 (lane % 16) + c.
+// Up to 16 rows, or 32 where W's rows run along the outputs (KN): a product is then as long as reading W once takes.  A wave
+// goes down its part of the summed dimension over 128 outputs, W's vectors from memory straight into the operands of
+// v_mfma_f32_16x16x32_bf16 (a lane: 8 consecutive k of one column):
+//   KN: a lane reads 8 columns of 8 rows of W and turns them in its registers (v_perm), so that fragment c holds its
+//     column c;
+//   rows of W along the sum: fragment c is of row 8 (lane % 16) + c, of which four lanes read 128 bytes (64 bytes at a time,
+//     the other half of each line came from memory again: 271 us instead of 186 at 3,584 x 151,936).
 // Either way a lane ends with 8 consecutive outputs.  The waves of a workgroup, each with its part of the sum, are added
 // through the LDS in their order.  W's rows may start at any element.
+// us by rows (1, 16, 32; 6 TB/s of W: 182 and 38): 3,584 x 151,936 KN 180, 187, 200, else 186, 194; 3,584 x 32,000 41, 41, 43
+// and 42, 43.  Tiles take 196 and 45 for 33 rows.
 typedef float lin_acc4 __attribute__((ext_vector_type(4)));
 
 struct FewArgs {
@@ -35,12 +38,12 @@ struct FewArgs {
   int M, K, N;
   int strips;     // of 128 outputs
   int splits;     // workgroups that share a strip's sum; > 1: their sums go to part [splits][M][N]
-  int wave_k;     // summed over by a wave, a multiple of 32
+  int wave_k;     // summed over by a wave, a multiple of 64
   float* part;
   Epilogue e;
 };
 
-constexpr int kFewWaves = 8, kFewCols = 128, kFewRows = 32;
+constexpr int kFewWaves = 8, kFewCols = 128;
 
 template <int ACT, bool PART>
 __device__ __forceinline__ void few_out(const FewArgs& a, int split, int m, int n, float (&v)[8]) {
@@ -72,7 +75,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_lin_few(const FewArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int strip = blockIdx.x % a.strips, split = blockIdx.x / a.strips;
   const int n = strip * kFewCols + 8 * (lane & 15);  // the lane's 8 outputs
-  const int kl = 8 * (lane >> 4);                    // and its place in a step
+  const int kl = (KN ? 8 : 16) * (lane >> 4);        // and its place in a step
   const int k0 = (split * kFewWaves + wave) * a.wave_k, k1 = min(k0 + a.wave_k, a.K);
   lin_acc4 acc[MB][8];
 #pragma unroll
@@ -116,38 +119,51 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_lin_few(const FewArgs a) {
                                                             __builtin_bit_cast(g_bf16x8, f), acc[b][c], 0, 0, 0);
     }
   };
-  u32x4 w0[8], w1[8], x0[MB], x1[MB];
-  auto load = [&](u32x4 (&wv)[8], u32x4 (&xv)[MB], int k) {
+  // A step's vectors, H for each output and row: 8 of 32 k (KN) or, so that four lanes read 128 bytes of a row of W, 16 of 64.
+  // Two steps are in flight.
+  constexpr int H = KN ? 1 : 2, STEP = 32 * H;
+  u32x4 w0[H][8], w1[H][8], x0[H][MB], x1[H][MB];
+  auto load = [&](u32x4 (&wv)[H][8], u32x4 (&xv)[H][MB], int k) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) wv[c] = *reinterpret_cast<const u32x4_a2*>(w_at(c, k));
+    for (int c = 0; c < 8; ++c)
 #pragma unroll
-    for (int b = 0; b < MB; ++b) xv[b] = *reinterpret_cast<const u32x4_a2*>(x_at(b, k));
+      for (int h = 0; h < H; ++h) wv[h][c] = *reinterpret_cast<const u32x4_a2*>(w_at(c, k + 8 * h));
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+      for (int h = 0; h < H; ++h) xv[h][b] = *reinterpret_cast<const u32x4_a2*>(x_at(b, k + 8 * h));
   };
-  const int steps = max(0, k1 - k0) / 32;
-  int k = k0, left = steps;
+  auto step = [&](const u32x4 (&wv)[H][8], const u32x4 (&xv)[H][MB]) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) multiply(wv[h], xv[h]);
+  };
+  int k = k0, left = max(0, k1 - k0) / STEP;
   if (left > 0) load(w0, x0, k);
   while (left >= 2) {
-    load(w1, x1, k + 32);
-    multiply(w0, x0);
-    if (left > 2) load(w0, x0, k + 64);
-    multiply(w1, x1);
-    k += 64;
+    load(w1, x1, k + STEP);
+    step(w0, x0);
+    if (left > 2) load(w0, x0, k + 2 * STEP);
+    step(w1, x1);
+    k += 2 * STEP;
     left -= 2;
   }
   if (left) {
-    multiply(w0, x0);
-    k += 32;
+    step(w0, x0);
+    k += STEP;
   }
   if (k < k1) {  // the last, shorter step
-    const int rest = k1 - k - kl;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      if constexpr (KN) w0[c] = c < rest ? *reinterpret_cast<const u32x4_a2*>(w_at(c, k)) : u32x4{0u, 0u, 0u, 0u};
-      else w0[c] = load_vec(w_at(c, k), rest);
+    for (int h = 0; h < H; ++h) {
+      const int rest = k1 - k - kl - 8 * h;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        if constexpr (KN) w0[h][c] = c < rest ? *reinterpret_cast<const u32x4_a2*>(w_at(c, k)) : u32x4{0u, 0u, 0u, 0u};
+        else w0[h][c] = load_vec(w_at(c, k + 8 * h), rest);
+      }
+#pragma unroll
+      for (int b = 0; b < MB; ++b) x0[h][b] = load_vec(x_at(b, k + 8 * h), rest);
     }
-#pragma unroll
-    for (int b = 0; b < MB; ++b) x0[b] = load_vec(x_at(b, k), rest);
-    multiply(w0, x0);
+    step(w0, x0);
   }
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
@@ -395,14 +411,14 @@ static ProductPlan product_plan(const Operand& a, const Operand& b) {
   ProductPlan p{};
   p.splits = 1;
   const int64_t K = a.cols;
-  p.few = a.rows <= kFewRows && !a.turned && K >= 8 && (!b.turned || b.rows >= 8) && a.ld <= kMostLin && b.ld <= kMostLin;
+  p.few = a.rows <= (b.turned ? 32 : 16) && !a.turned && K >= 8 && (!b.turned || b.rows >= 8) && a.ld <= kMostLin && b.ld <= kMostLin;
   if (p.few) {
-    const int64_t strips = (b.rows + kFewCols - 1) / kFewCols, steps = (K + 31) / 32;
-    // workgroups for the whole chip, of waves that have at least 4 steps each
-    const int64_t most = std::max<int64_t>(1, steps / (4 * kFewWaves));
+    const int64_t strips = (b.rows + kFewCols - 1) / kFewCols, steps = (K + 63) / 64;
+    // workgroups for the whole chip, of waves that have at least 2 steps each
+    const int64_t most = std::max<int64_t>(1, steps / (2 * kFewWaves));
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, kCus / strips, 16}));
     const int64_t waves = (int64_t)p.splits * kFewWaves;
-    p.range = (int)((steps + waves - 1) / waves * 32);
+    p.range = (int)((steps + waves - 1) / waves * 64);
   } else {
     plan_tiles(a.rows, b.rows, K, p.shape, p.splits, p.range);
   }
@@ -436,12 +452,10 @@ static void launch_few(const FewArgs& f, bool kn, hipStream_t s) {
     if (f.splits > 1) hipLaunchKernelGGL((k_lin_few<MB, KN, GRPO_ACT_NONE, true>), grid, block, 0, s, f);
     else hipLaunchKernelGGL((k_lin_few<MB, KN, ACT, false>), grid, block, 0, s, f);
   };
-  auto rows = [&](auto mb) {
-    if (kn) go(mb, std::true_type());
-    else go(mb, std::false_type());
-  };
-  if (f.M <= 16) rows(std::integral_constant<int, 1>());
-  else rows(std::integral_constant<int, 2>());
+  const std::integral_constant<int, 1> one;
+  if (!kn) go(one, std::false_type());
+  else if (f.M <= 16) go(one, std::true_type());
+  else go(std::integral_constant<int, 2>(), std::true_type());
 }
 
 static void join_splits(const float* part, int splits, int M, int N, const Epilogue& e, hipStream_t s) {
