@@ -4,8 +4,8 @@
 // Forward.  Each thread walks its vectors, U of them (a chunk) at a time, and keeps, relative to its running maximum m and in
 // units of log 2,
 //   s = sum 2^w, t = sum 2^w w, w = (z - m) log2(e) / tau,
-// over the words (z > -1e8).  m also bounds the alternatives: the n-th largest of the threads' maxima is a lower bound L of
-// the n-th largest word.  The maximum of each chunk of four neighbouring lanes is kept in LDS, and only the chunks whose
+// over the words (z > -1e8).  m also bounds the alternatives: the n-th largest of the threads' maxima (of 1,024 threads, of
+// four lanes') is a lower bound L of the n-th largest word.  The maximum of each chunk of four neighbouring lanes is kept in LDS, and only the chunks whose
 // maximum is >= L, n of them unless words repeat, are read a second time; their words >= L (n and a few) go to a list in
 // LDS, and a word's place is the number of list words in front of it.  Where words repeat so often that the list or the
 // number of chunks is too small, the n-th largest word is found by bisection with counts over the row.
@@ -135,7 +135,8 @@ struct TopSmem {
   float m[NT / 64];
   double s[NT / 64], t[NT / 64];
   double log_sum;
-  uint16_t top[NT];                   // upper 16 bits of the order of each thread's maximum
+  static constexpr int kTops = NT < 256 ? NT : 256;
+  uint16_t top[kTops];                // upper 16 bits of the order of each thread's (1,024 threads: four's) maximum
   uint16_t group[kSlices * NT / 4];   // and of four lanes' chunk
   uint32_t bound;                     // and of L
   int n_groups, count;
@@ -468,7 +469,14 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
       }
     }
   }
-  sm.top[tid] = (uint16_t)(order_of(sum.m) >> 16);
+  constexpr int PER = NT / TopSmem<NT>::kTops;
+  static_assert(PER == 1 || PER == 4, "a thread, or four lanes");
+  float tm = sum.m;
+  if constexpr (PER == 4) {
+    tm = fmaxf(tm, dpp_f32v<0xB1>(tm));
+    tm = fmaxf(tm, dpp_f32v<0x4E>(tm));
+  }
+  if (tid % PER == 0) sm.top[tid / PER] = (uint16_t)(order_of(tm) >> 16);
   float M;
   double S, Tsum;
   join_threads<NT>(sum, sc, sm, M, S, Tsum);
@@ -481,10 +489,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
   }
   if (n == 0) return;
   if (tid < 64 && some) {
-    uint32_t k[NT / 64];
+    constexpr int K = TopSmem<NT>::kTops / 64;
+    uint32_t k[K];
 #pragma unroll
-    for (int i = 0; i < NT / 64; ++i) k[i] = sm.top[tid + 64 * i];
-    const uint32_t p = nth_largest(k, NT / 64, n);
+    for (int i = 0; i < K; ++i) k[i] = sm.top[tid + 64 * i];
+    const uint32_t p = nth_largest(k, K, n);
     if (tid == 0) sm.bound = p;
   }
   __syncthreads();
