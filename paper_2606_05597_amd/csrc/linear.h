@@ -57,7 +57,8 @@ __device__ __forceinline__ float slope_of(float z) {
   }
   if constexpr (ACT == GRPO_ACT_GELU_TANH) {
     const float t = tanh_of(0.79788456f * fmaf(0.044715f * z * z, z, z));
-    return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.79788456f * fmaf(3.f * 0.044715f * z, z, 1.f);
+    const float q = fminf(fabsf(z), 1e6f);  // beyond, 1 - t^2 is 0 and z^2 may be infinite
+    return 0.5f * (1.f + t) + 0.5f * copysignf(q, z) * (1.f - t * t) * 0.79788456f * fmaf(3.f * 0.044715f * q, q, 1.f);
   }
   if constexpr (ACT == GRPO_ACT_SILU) {
     const float g = sigmoid(z);

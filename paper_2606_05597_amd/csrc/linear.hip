@@ -411,7 +411,8 @@ static ProductPlan product_plan(const Operand& a, const Operand& b) {
   ProductPlan p{};
   p.splits = 1;
   const int64_t K = a.cols;
-  p.few = a.rows <= (b.turned ? 32 : 16) && !a.turned && K >= 8 && (!b.turned || b.rows >= 8) && a.ld <= kMostLin && b.ld <= kMostLin;
+  p.few = a.rows <= (b.turned ? 32 : 16) && !a.turned && K >= 8 && (!b.turned || b.rows >= 8) && a.ld <= kMostLin &&
+          b.ld <= kMostLin;
   if (p.few) {
     const int64_t strips = (b.rows + kFewCols - 1) / kFewCols, steps = (K + 63) / 64;
     // workgroups for the whole chip, of waves that have at least 2 steps each
@@ -645,7 +646,8 @@ extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t
   }
   if (g.dw) {
     const Epilogue e{g.dw, op->w_out_in ? op->K : op->N, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE,
-                     g.dw_dtype == GRPO_BF16, false, g.accumulate_dw == 1, op->K * op->N * (int64_t)size_of(g.dw_dtype) > kPastL2};
+                     g.dw_dtype == GRPO_BF16, false, g.accumulate_dw == 1,
+                     op->K * op->N * (int64_t)size_of(g.dw_dtype) > kPastL2};
     launch_product(op->w_out_in ? p.dz_cols : p.x_cols, op->w_out_in ? p.x_cols : p.dz_cols, e, at, s);
   }
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;

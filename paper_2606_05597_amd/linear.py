@@ -56,10 +56,11 @@ def grpo_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = No
                 residual: torch.Tensor | None = None, *, act: str = "none", out_dtype=torch.bfloat16,
                 out: torch.Tensor | None = None, keep_z: bool = False, workspace: torch.Tensor | None = None,
                 stream=None):
-    """y = act(x w + bias) + residual: x bf16 [M, K] and w bf16 [K, N] with unit stride in either dimension, bias [N] bf16
-    or fp32, residual [M, N] of y's type, act "none", "relu", "gelu", "gelu_tanh" or "silu".  ``out``: y, written in place
-    (it may be ``residual``); without it a tensor of ``out_dtype`` (bf16 or fp32).  Returns (y, z), z = x w + bias in fp32
-    with ``keep_z`` (what ``grpo_linear_bwd`` takes if there is an activation), otherwise None."""
+    """y = act(x w + bias) + residual: x bf16 [M, K] with unit column stride, w bf16 [K, N] with unit stride in either
+    dimension, bias [N] bf16 or fp32, residual [M, N] of y's type, act "none", "relu", "gelu", "gelu_tanh" or "silu".
+    ``out``: y, written in place (it may be ``residual``); without it a tensor of ``out_dtype`` (bf16 or fp32).  Returns
+    (y, z), z = x w + bias in fp32 with ``keep_z`` (what ``grpo_linear_bwd`` takes if there is an activation), otherwise
+    None."""
     op = _op(x, w, act)
     M, N, dev = op.M, op.N, x.device
     if bias is not None:

@@ -87,7 +87,7 @@ def test_workspace(lib):
         for V in (16385, 151936, 1 << 22):
             for n in (0, 1, 64):
                 b = f(T, V, n)
-                assert b % 256 == 0 and b <= 256 * (24 + 8 * 64) * 2
+                assert b % 256 == 0 and b <= T * 16 * (24 + 8 * n) + 512  # at most 16 parts to a row
 
 
 def test_binding_refusals():
