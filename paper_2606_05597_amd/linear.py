@@ -27,29 +27,37 @@ def _code(dtype, name):
 def _rows(t, name, dtype, shape=None):
     """Row stride of a 2-D tensor with unit column stride (that of a single row or column says nothing)."""
     _meta(t, name, dtype, shape=shape)
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+    if t.dim() != 2:
         raise ValueError(f"{name} must be 2-D with unit column stride")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    return _row_stride(t.shape, t.stride(), name)
+
+
+def _row_stride(shape, strides, name):
+    (rows, cols), (ld, step) = shape, strides
+    if step != 1 and cols != 1:
+        raise ValueError(f"{name} must be 2-D with unit column stride")
+    if rows <= 1:
+        return cols
+    if ld < cols:
         raise ValueError(f"{name}'s rows overlap")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    return ld
 
 
 def _op(x, w, act):
     """The operator's struct without its bias."""
-    op = _lib.LinearOp()
     if act not in ACTIVATIONS:
         raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
-    op.ldx = _rows(x, "x", torch.bfloat16)
+    ldx = _rows(x, "x", torch.bfloat16)
     _meta(w, "w", torch.bfloat16)
     if w.dim() != 2:
         raise ValueError("w must be 2-D")
-    out_in = w.stride(1) != 1 and w.stride(0) == 1
-    op.ldw = _rows(w.t() if out_in else w, "w.t()" if out_in else "w", torch.bfloat16)
-    if x.shape[1] != w.shape[0]:
-        raise ValueError(f"x and w disagree on K: {x.shape[1]} and {w.shape[0]}")
-    op.M, op.K, op.N = x.shape[0], x.shape[1], w.shape[1]
-    op.x, op.w, op.w_out_in, op.act = x.data_ptr(), w.data_ptr(), out_in, ACTIVATIONS[act]
-    return op
+    (K, N), (s0, s1) = w.shape, w.stride()
+    out_in = s1 != 1 and s0 == 1
+    ldw = _row_stride((N, K), (s1, s0), "w.t()") if out_in else _row_stride((K, N), (s0, s1), "w")
+    M, Kx = x.shape
+    if Kx != K:
+        raise ValueError(f"x and w disagree on K: {Kx} and {K}")
+    return _lib.LinearOp(M, K, N, x.data_ptr(), ldx, w.data_ptr(), ldw, out_in, ACTIVATIONS[act], None, 0)
 
 
 def grpo_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
