@@ -234,12 +234,35 @@ __global__ __launch_bounds__(256) void k_lin_join(const float* __restrict__ part
 }
 
 // ---- operands laid out anew -----------------------------------------------------
-// dst [R, ldd] = src [R, C] (rows lds_ apart), zeros in columns C .. ldd - 1.
-__global__ __launch_bounds__(256) void k_lin_copy(const uint16_t* __restrict__ src, int64_t lds_, int R, int C,
-                                                  uint16_t* __restrict__ dst, int64_t ldd) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= ldd) return;
-  for (int r = blockIdx.y; r < R; r += gridDim.y) dst[r * ldd + c] = c < C ? src[r * lds_ + c] : (uint16_t)0;
+// dst = src [lines, length] (lines ld apart) in lines of `vecs` whole vectors, ending in zeros.
+struct LayOut {
+  const uint16_t* src;
+  int64_t ld;
+  uint16_t* dst;
+  int length, vecs;
+  uint32_t total;  // vectors of all lines
+};
+
+// Both operands of a product in one launch, a thread to a vector: a streaming pass, 322 us for 687 MB of rows of 3,259
+// elements (an element to a thread, 485).
+__global__ __launch_bounds__(256) void k_lin_copy(const LayOut a, const LayOut b) {
+  uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  const bool first = i < a.total;
+  const LayOut& o = first ? a : b;
+  if (!first) i -= a.total;
+  if (i >= o.total) return;
+  const uint32_t line = i / (uint32_t)o.vecs, c = (i - line * (uint32_t)o.vecs) * 8;
+  const uint16_t* p = o.src + line * o.ld + c;
+  const int left = o.length - (int)c;
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (left >= 8) {
+    v = *reinterpret_cast<const u32x4_a2*>(p);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 7; ++q)
+      if (q < left) v[q >> 1] |= (uint32_t)p[q] << (16 * (q & 1));
+  }
+  reinterpret_cast<u32x4*>(o.dst)[i] = v;
 }
 
 // ---- dz -------------------------------------------------------------------------
@@ -357,14 +380,35 @@ struct Operand {
   size_t bytes() const { return copied() ? align_up(2 * (size_t)lines() * (size_t)up8(length())) : 0; }
 };
 
-static TileOperand lay_out(const Operand& o, char*& ws, hipStream_t s) {
-  if (!o.copied()) return TileOperand{o.src, o.ld, o.turned};
-  uint16_t* dst = reinterpret_cast<uint16_t*>(ws);
-  ws += o.bytes();
-  const int64_t ld = up8(o.length());
-  hipLaunchKernelGGL(k_lin_copy, dim3((unsigned)((ld + 255) / 256), (unsigned)std::min<int64_t>(16384, o.lines())), dim3(256),
-                     0, s, o.src, o.ld, (int)o.lines(), (int)o.length(), dst, ld);
-  return TileOperand{dst, ld, o.turned};
+// The operands as tiles read them, from ws on where they are copied.
+static void lay_out(const Operand& a, const Operand& b, char*& ws, TileArgs& t, hipStream_t s) {
+  LayOut l[2];
+  int64_t lines[2], most[2];
+  const Operand* o[2] = {&a, &b};
+  TileOperand* to[2] = {&t.a, &t.b};
+  for (int i = 0; i < 2; ++i) {
+    const bool copied = o[i]->copied();
+    uint16_t* dst = reinterpret_cast<uint16_t*>(ws);
+    if (copied) ws += o[i]->bytes();
+    const int64_t length = o[i]->length(), vecs = up8(length) / 8;
+    *to[i] = copied ? TileOperand{dst, vecs * 8, o[i]->turned} : TileOperand{o[i]->src, o[i]->ld, o[i]->turned};
+    l[i] = LayOut{o[i]->src, o[i]->ld, dst, (int)length, (int)vecs, 0u};
+    lines[i] = copied ? o[i]->lines() : 0;
+    most[i] = std::max<int64_t>(1, ((int64_t)1 << 30) / vecs);  // lines of a launch, whose threads stay below 2^32
+  }
+  while (lines[0] > 0 || lines[1] > 0) {
+    int64_t n[2];
+    for (int i = 0; i < 2; ++i) {
+      n[i] = std::min(lines[i], most[i]);
+      l[i].total = (uint32_t)(n[i] * l[i].vecs);
+    }
+    hipLaunchKernelGGL(k_lin_copy, dim3((l[0].total + l[1].total + 255u) / 256u), dim3(256), 0, s, l[0], l[1]);
+    for (int i = 0; i < 2; ++i) {
+      lines[i] -= n[i];
+      l[i].src += n[i] * l[i].ld;
+      l[i].dst += n[i] * l[i].vecs * 8;
+    }
+  }
 }
 
 // Tile shape and splits of the shortest launch, by what a CU was seen to take (us): for 64 summed over of a tile, with as
@@ -417,7 +461,7 @@ static ProductPlan product_plan(const Operand& a, const Operand& b) {
     const int64_t strips = (b.rows + kFewCols - 1) / kFewCols, steps = (K + 63) / 64;
     // workgroups for the whole chip, of waves that have at least 2 steps each
     const int64_t most = std::max<int64_t>(1, steps / (2 * kFewWaves));
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, kCus / strips, 16}));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({most, kCus / strips, 32}));
     const int64_t waves = (int64_t)p.splits * kFewWaves;
     p.range = (int)((steps + waves - 1) / waves * 64);
   } else {
@@ -476,8 +520,7 @@ static void launch_product(const Operand& a, const Operand& b, const Epilogue& e
     with_act(e.act, [&](auto act) { launch_few<decltype(act)::value>(f, b.turned, s); });
   } else {
     TileArgs t;
-    t.a = lay_out(a, ws, s);
-    t.b = lay_out(b, ws, s);
+    lay_out(a, b, ws, t, s);
     t.M = M;
     t.N = N;
     t.K = K;
