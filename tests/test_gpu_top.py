@@ -103,8 +103,10 @@ def check(logits, z, act, n, tau=1.0, grad=True, in_place=False, flags_want=0, u
             assert not grad or not d[t].any()
             continue
         s, he, x, ls = bounds(z[t], every, tau[t])
-        for got, want in [(logp[t], lp)] + list(zip(tlp[t], want_top)):
-            if np.isinf(want) or not 0 <= act[t] < V and want == 0:
+        assert 0 <= act[t] < V or logp[t] == 0
+        own = [(logp[t], lp)] if 0 <= act[t] < V else []
+        for got, want in own + list(zip(tlp[t], want_top)):
+            if np.isinf(want):
                 assert got == want, (t, got, want)
             else:
                 assert abs(got - want) <= s + 1.01 * E * abs(want), (t, got, want, s)
