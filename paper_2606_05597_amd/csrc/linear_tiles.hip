@@ -15,7 +15,6 @@
 namespace grpo {
 
 typedef short lin_s16x4 __attribute__((ext_vector_type(4)));
-typedef short lin_s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) lin_s16x4 lin_lds_s16x4;
 
 // One operand's part of a tile: R rows (m or n), W of them a wave's, in blocks of 32; NW waves load it.
