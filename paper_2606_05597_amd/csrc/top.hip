@@ -94,9 +94,10 @@ struct Sums {
     s += e;
     t = fmaf(e, w, t);
   }
-  // Any element: a masked word adds 2^-200 = 0, a NaN is not masked.
+  // Any element: a masked word, and one so far below the shift that w may pass fp32's range, adds 2^-200 = 0; a NaN is neither.
   __device__ __forceinline__ void fold(float z, float sc) {
-    const float w = z <= kShiftMin ? -200.f : fmaf(z - m, sc, rest);
+    float w = fmaf(z - m, sc, rest);
+    w = z <= kShiftMin || w < -200.f ? -200.f : w;
     const float e = __builtin_amdgcn_exp2f(w);
     s += e;
     t = fmaf(e, w, t);
@@ -739,7 +740,8 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4, 8))) void
   const float sc = kLog2e / r.temperature, l2 = (float)(r.log_sum / kLn2), top = r.max;
   const float A = (float)(-g * kLn2 * inv), B = (float)(-(C + g * (double)r.entropy) * inv);
   store([&](float z) {
-    const float w = z <= kShiftMin ? -200.f : fmaf(z - top, sc, -l2);
+    // a masked word's, and any so small that A times it may pass fp32's range, weigh nothing
+    const float w = z <= kShiftMin ? -200.f : fmaxf(fmaf(z - top, sc, -l2), -200.f);
     return __builtin_amdgcn_exp2f(w) * fmaf(w, A, B);
   });
   // by the thread that stored the word's place, after that store
