@@ -150,16 +150,19 @@ struct TopSmem {
   int n_first;
 };
 
-// All threads' sums joined in fp64 at the shift of the row's maximum M, in every thread.
+// All threads' sums joined in fp64 at the shift of the row's maximum M, in every thread.  A thread's are divided by the weight
+// that its own maximum was added with (2^rest, as the hardware rounds it), so that the row's maximum weighs 1, S is at
+// least 1 and no log-prob is above 0.
 template <int NT>
 __device__ __forceinline__ void join_threads(const Sums& a, float sc, TopSmem<NT>& sm, float& M, double& S, double& T) {
   constexpr int NW = NT / 64;
   static_assert(NW <= 16, "one wave to a lane of 16");
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const float mw = wave_max_dpp(a.m);
-  const float dl = fmaf(a.m - mw, sc, -a.rest), f = __builtin_amdgcn_exp2f(dl);
-  const double sw = wave_sum_dpp((double)f * (double)a.s);
-  const double tw = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * ((double)a.t + (double)dl * (double)a.s));
+  const float dl = (a.m - mw) * sc, f = __builtin_amdgcn_exp2f(dl);
+  const double own = (double)__builtin_amdgcn_exp2f(a.rest), s = (double)a.s;
+  const double sw = wave_sum_dpp((double)f * (s / own));
+  const double tw = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * (((double)a.t + ((double)dl - (double)a.rest) * s) / own));
   if (lane == 0) {
     sm.m[wv] = mw;
     sm.s[wv] = sw;
@@ -198,7 +201,7 @@ __device__ inline grpo_top_row finish_row(const TopArgs& a, int t, int act, floa
   } else {
     r.log_sum = log(S);
     r.max = M;
-    r.entropy = (float)(r.log_sum - Tsum / S * kLn2);  // both terms >= 0
+    r.entropy = fmaxf((float)(r.log_sum - Tsum / S * kLn2), 0.f);  // S >= 1, T <= 0 but for rounding
     r.logp = !act_ok ? 0.f : is_word(za) ? (float)(((double)za - (double)M) / (double)tau - r.log_sum) : -INFINITY;
   }
   if (flags && a.flags) atomicOr(a.flags, flags);
