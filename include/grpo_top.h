@@ -29,7 +29,7 @@ typedef struct {
   float max;         /* max z over the words, -inf without any                       */
   float entropy;     /* H                                                            */
   float temperature; /* tau                                                          */
-  float logp;        /* the action's log-prob                                        */
+  float logp;        /* the action's log-prob, a word's no lower than -FLT_MAX       */
 } grpo_top_row;
 
 /* Bytes of device workspace grpo_token_logp_top needs: 0 for many or short rows (ws may then be NULL), and for invalid
@@ -42,8 +42,8 @@ size_t grpo_token_logp_top_workspace_bytes(int64_t T, int64_t V, int32_t n);
  *   0 <= T < 2^31, 1 <= V <= GRPO_TOP_MAX_V, V <= ld, 0 <= n <= GRPO_TOP_MAX
  *   temperature  device fp32 [T], a value for each row, or NULL and temperature_all for all: 1e-6 .. 1e6
  *   actions      device int32 [T]
- *   logp         device fp32 [T] or NULL: log p of the action; -inf for a masked word; 0 where it is outside [0, V)
- *                (GRPO_FLAG_ACTION)
+ *   logp         device fp32 [T] or NULL: log p of the action; -inf for a masked word and below fp32's range; 0 where the
+ *                action is outside [0, V) (GRPO_FLAG_ACTION)
  *   entropy      device fp32 [T] or NULL
  *   top_ids      device int32 [T, n] or NULL, -1 past a row's last word
  *   top_logp     device fp32 [T, n] or NULL, -inf past a row's last word

@@ -14,6 +14,7 @@
 //
 // Backward.  A streaming pass: dlogits_v = p_v (A log2 p_v + B) with A, B of the row; the words with a coefficient of their
 // own (the action, the alternatives) are formed apart in fp64 and stored over it by the thread that stored their vector.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -207,6 +208,8 @@ __device__ inline grpo_top_row finish_row(const TopArgs& a, int t, int act, floa
   if (flags && a.flags) atomicOr(a.flags, flags);
   if (a.logp) a.logp[t] = r.logp;
   if (a.entropy) a.entropy[t] = r.entropy;
+  // Below fp32's range it is -inf, by which the backward call knows a masked word.
+  if (act_ok && is_word(za) && !bad) r.logp = fmaxf(r.logp, -FLT_MAX);
   if (a.rows) a.rows[t] = r;
   return r;
 }

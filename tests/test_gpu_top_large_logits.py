@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2606_05597_amd as grpo
 from tests.test_gpu_top import BF16, F32, check, make
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +41,25 @@ def test_words_far_below_the_maximum(T, V, big, tau, dtype):
     act = np.where(np.arange(T) % 2 == 0, at, np.argmax(z == 0.0, axis=1))
     for n, ups in ((9, (True, True, True)), (9, (True, False, True)), (0, (True, True, False))):
         check(logits, z, act, n, tau, ups=ups)
+
+
+@pytest.mark.parametrize("T,V", [(2100, 500), (7, 3000), (7, 40000), (60, 20003)])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_an_action_whose_log_prob_passes_fp32_is_no_masked_word(T, V, dtype):
+    """Its log-prob is -inf; the gradient is that of a word of weight 0, d / tau, against the largest word's -d / tau (one
+    rounding of each to the type, two of fp32 before it); a masked action's is 0."""
+    tau, big = float(np.float32(1e-6)), 1e38
+    x, z, at = large(T, V, dtype, big)
+    act = torch.zeros(T, dtype=torch.int32, device="cuda")
+    some = [t for t in range(T) if t % 6 in (0, 1) and at[t] > 0]
+    x[some[0], 0] = -float("inf")
+    logp, ent, ids, _, rows = grpo.grpo_token_logp_top(x, act, 2, temperature=tau)
+    up = torch.linspace(0.5, 2.0, T, device="cuda")
+    d = grpo.grpo_token_logp_top_bwd(x, act, ids, rows, up, None, None).double().cpu().numpy()
+    half = torch.finfo(dtype).eps / 2
+    for t in some:
+        want = np.zeros(V)
+        if t != some[0]:
+            want[0], want[at[t]] = float(up[t]) / tau, -float(up[t]) / tau
+        assert logp[t] == -float("inf") and ent[t] == 0
+        assert (np.abs(d[t] - want) <= 1.01 * (half + 2 * 2.0**-24) * np.abs(want)).all(), t
