@@ -72,36 +72,50 @@ __device__ __forceinline__ bool is_word(float z) { return z > kShiftMin; }
 
 // A thread's sums relative to the shift m sc - rest: w = z sc - m sc + rest.  Near: m sc is small enough that c = -m sc,
 // rounded, is a shift to half a unit, rest its rounding, and w one fma, whose error is relative to w; otherwise the
-// difference z - m comes first and rest is 0.
+// difference z - m comes first and rest is 0.  A chunk's words are summed in fp32, the chunks in fp64: weights that repeat are
+// all rounded the same way (rows of two values, log S with fp32 throughout: off by 3e-6 over 782 words of a thread, by 3e-5
+// over 5,860), and two additions to 32 words cost no time that could be measured.
+constexpr float kNear = 4194304.f;
+__device__ __forceinline__ float rest_of(float m, float sc) {
+  const float c = -(m * sc);
+  return fabsf(c) < kNear ? fmaf(m, sc, c) : 0.f;
+}
 struct Sums {
-  float m = kShiftMin, s = 0.f, t = 0.f, c = 0.f, rest = 0.f;
+  double s = 0.0, t = 0.0;
+  float m = kShiftMin, c = 0.f, rest = 0.f;
+  float cs = 0.f, ct = 0.f;  // of the chunk
   bool near = false;
 
   __device__ __forceinline__ void raise(float mn, float sc) {
     if (mn > m) {
       c = -(mn * sc);
-      near = fabsf(c) < 4194304.f;
+      near = fabsf(c) < kNear;
       const float r = near ? fmaf(mn, sc, c) : 0.f;
       const float dl = fmaf(m - mn, sc, r - rest), f = __builtin_amdgcn_exp2f(dl);
-      t = f == 0.f ? 0.f : f * fmaf(dl, s, t);
-      s *= f;
+      t = f == 0.f ? 0.0 : (double)f * fma((double)dl, s, t);
+      s *= (double)f;
       m = mn;
       rest = r;
     }
   }
+  __device__ __forceinline__ void join() {
+    s += (double)cs;
+    t += (double)ct;
+    cs = ct = 0.f;
+  }
   // A word at the shift, near and above -1e8; a NaN makes s NaN.
   __device__ __forceinline__ void fold_near(float z, float sc) {
     const float w = fmaf(z, sc, c), e = __builtin_amdgcn_exp2f(w);
-    s += e;
-    t = fmaf(e, w, t);
+    cs += e;
+    ct = fmaf(e, w, ct);
   }
   // Any element: a masked word, and one so far below the shift that w may pass fp32's range, adds 2^-200 = 0; a NaN is neither.
   __device__ __forceinline__ void fold(float z, float sc) {
     float w = fmaf(z - m, sc, rest);
     w = z <= kShiftMin || w < -200.f ? -200.f : w;
     const float e = __builtin_amdgcn_exp2f(w);
-    s += e;
-    t = fmaf(e, w, t);
+    cs += e;
+    ct = fmaf(e, w, ct);
   }
 };
 
@@ -151,37 +165,51 @@ struct TopSmem {
   int n_first;
 };
 
-// All threads' sums joined in fp64 at the shift of the row's maximum M, in every thread.  A thread's are divided by the weight
-// that its own maximum was added with (2^rest, as the hardware rounds it), so that the row's maximum weighs 1, S is at
-// least 1 and no log-prob is above 0.
+// All threads' sums joined in fp64, in every thread: S = sum 2^w and T / S at the shift M sc of the row's maximum M.  The sums stay
+// at the shift of the thread's, the wave's and the row's maximum until they are joined; then they are divided by the weight
+// that the maximum was added with (2^rest, as the hardware rounds it), so that it weighs 1, S is at least 1 and no log-prob is
+// above 0.  One thread needs them: `divide`.
 template <int NT>
-__device__ __forceinline__ void join_threads(const Sums& a, float sc, TopSmem<NT>& sm, float& M, double& S, double& T) {
+__device__ __forceinline__ void join_threads(const Sums& a, float sc, TopSmem<NT>& sm, bool divide, float& M, double& S,
+                                             double& mean) {
   constexpr int NW = NT / 64;
   static_assert(NW <= 16, "one wave to a lane of 16");
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const float mw = wave_max_dpp(a.m);
-  const float dl = (a.m - mw) * sc, f = __builtin_amdgcn_exp2f(dl);
-  const double own = (double)__builtin_amdgcn_exp2f(a.rest), s = (double)a.s;
-  const double sw = wave_sum_dpp((double)f * (s / own));
-  const double tw = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * (((double)a.t + ((double)dl - (double)a.rest) * s) / own));
-  if (lane == 0) {
-    sm.m[wv] = mw;
-    sm.s[wv] = sw;
-    sm.t[wv] = tw;
+  M = wave_max_dpp(a.m);
+  float rest = rest_of(M, sc);
+  const float dl = fmaf(a.m - M, sc, rest - a.rest), f = __builtin_amdgcn_exp2f(dl);
+  S = wave_sum_dpp((double)f * a.s);
+  double T = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * (a.t + (double)dl * a.s));
+  if (NW > 1 && lane == 0) {
+    sm.m[wv] = M;
+    sm.s[wv] = S;
+    sm.t[wv] = T;
   }
   __syncthreads();
-  const int q = lane & 15;
-  const bool in = q < NW;
-  const float mq = in ? sm.m[q] : -INFINITY;
-  M = row16_max(mq);
-  const float dq = (mq - M) * sc, g = in ? __builtin_amdgcn_exp2f(dq) : 0.f;
-  S = row16_sum(in ? (double)g * sm.s[q] : 0.0);
-  T = row16_sum(g == 0.f || !in ? 0.0 : (double)g * (sm.t[q] + (double)dq * sm.s[q]));
+  if constexpr (NW > 1) {
+    const int q = lane & 15;
+    const bool in = q < NW;
+    const float mq = in ? sm.m[q] : -INFINITY;
+    M = row16_max(mq);
+    rest = rest_of(M, sc);
+    const float dq = in ? fmaf(mq - M, sc, rest - rest_of(mq, sc)) : 0.f, g = in ? __builtin_amdgcn_exp2f(dq) : 0.f;
+    S = row16_sum(in ? (double)g * sm.s[q] : 0.0);
+    T = row16_sum(g == 0.f ? 0.0 : (double)g * (sm.t[q] + (double)dq * sm.s[q]));
+  }
+  if (divide) {
+    mean = T / S - (double)rest;
+    // S / own by its residual, twice: exact where they are equal
+    const float own = __builtin_amdgcn_exp2f(rest);
+    const double inv = (double)__builtin_amdgcn_rcpf(own);
+    double s1 = S * inv;
+    s1 = fma(fma(-(double)own, s1, S), inv, s1);
+    S = fma(fma(-(double)own, s1, S), inv, s1);
+  }
 }
 
 // What the row comes to, from the joined sums, and its outputs: one thread.  za: the logit of the action act.
 __device__ inline grpo_top_row finish_row(const TopArgs& a, int t, int act, float za, float tau, float M, double S,
-                                          double Tsum) {
+                                          double mean) {
   grpo_top_row r;
   const bool act_ok = act >= 0 && act < a.V;
   const bool bad_tau = !(tau >= 1e-6f && tau <= 1e6f), bad = isnan(S) || isnan(M) || M == INFINITY || bad_tau;
@@ -202,7 +230,7 @@ __device__ inline grpo_top_row finish_row(const TopArgs& a, int t, int act, floa
   } else {
     r.log_sum = log(S);
     r.max = M;
-    r.entropy = fmaxf((float)(r.log_sum - Tsum / S * kLn2), 0.f);  // S >= 1, T <= 0 but for rounding
+    r.entropy = fmaxf((float)(r.log_sum - mean * kLn2), 0.f);  // S >= 1, mean <= 0 but for rounding
     r.logp = !act_ok ? 0.f : is_word(za) ? (float)(((double)za - (double)M) / (double)tau - r.log_sum) : -INFINITY;
   }
   if (flags && a.flags) atomicOr(a.flags, flags);
@@ -399,7 +427,7 @@ __device__ __forceinline__ void top_by_counts(const Tin* row, int cols, int n, f
 
 // One workgroup to a row, or (PART) to a part of it.
 template <typename Tin, int NT, bool PART>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ? 8 : 4))) void k_top(const TopArgs a,
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ? 8 : 7))) void k_top(const TopArgs a,
                                                                                                   int row0) {
   constexpr int EPV = 16 / (int)sizeof(Tin), U = 4, QUADS = NT / 4;
   typedef typename VecAt<Tin>::type u32x4_any;
@@ -423,6 +451,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
   Sums sum;
   sum.raise(ez, sc);
   sum.fold(ez, sc);
+  sum.join();
   float gm = -INFINITY;
   for (int q = 0; q < chunks; ++q) {
     const int base = q * NT * U + tid;
@@ -458,6 +487,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
 #pragma unroll
           for (int e = 0; e < EPV; ++e) sum.fold(elem<Tin>(x[u], e), sc);
       }
+      sum.join();
     } else {
 #pragma unroll 1
       for (int vi = base; vi < nvec; vi += NT) {
@@ -466,6 +496,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
         cn = vec_min<Tin>(x, cn);
         sum.raise(cm, sc);
         words(x);
+        sum.join();
       }
     }
     if (n > 0) {
@@ -486,14 +517,14 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ?
   }
   if (tid % PER == 0) sm.top[tid / PER] = (uint16_t)(order_of(tm) >> 16);
   float M;
-  double S, Tsum;
-  join_threads<NT>(sum, sc, sm, M, S, Tsum);
+  double S, mean = 0.0;
+  join_threads<NT>(sum, sc, sm, tid == kFinisher<NT>, M, S, mean);
   const bool bad = isnan(S) || isnan(M) || M == INFINITY || isnan(sc), some = !bad && S > 0.0;
   if (PART) {
     if (tid == kFinisher<NT>)
-      a.part[(int64_t)t * a.parts + part] = TopPart{bad ? (double)NAN : S, Tsum, some ? M : kShiftMin, 0.f};
+      a.part[(int64_t)t * a.parts + part] = TopPart{bad ? (double)NAN : S, some ? mean * S : 0.0, some ? M : kShiftMin, 0.f};
   } else if (tid == kFinisher<NT>) {
-    const grpo_top_row r = finish_row(a, t, act, za, tau, M, S, Tsum);
+    const grpo_top_row r = finish_row(a, t, act, za, tau, M, S, mean);
     sm.log_sum = r.log_sum;
   }
   if (n == 0) return;
@@ -593,7 +624,7 @@ __global__ __launch_bounds__(kJoinNT) void k_top_join(const TopArgs a) {
   const double S = wave_sum_dpp((double)f * p.s);
   const double Tsum = wave_sum_dpp(f == 0.f ? 0.0 : (double)f * (p.t + (double)d * p.s));
   const bool bad = isnan(S) || isnan(sc), some = !bad && S > 0.0;
-  if (tid == 64) sm.log_sum = finish_row(a, t, act, za, tau, M, S, Tsum).log_sum;
+  if (tid == 64) sm.log_sum = finish_row(a, t, act, za, tau, M, S, Tsum / S).log_sum;
   if (n == 0) return;
   __syncthreads();
   if (tid < 64 && some) {
