@@ -510,7 +510,7 @@ static void join_splits(const float* part, int splits, int M, int N, const Epilo
 }
 
 // C [a.rows, b.rows] = A B^T with the epilogue e.
-static void launch_product(const Operand& a, const Operand& b, const Epilogue& e, char*& ws, hipStream_t s) {
+static void launch_product(const Operand& a, const Operand& b, const Epilogue& e, char* ws, hipStream_t s) {
   const ProductPlan p = product_plan(a, b);
   const int M = (int)a.rows, N = (int)b.rows, K = (int)a.cols;
   float* part = reinterpret_cast<float*>(ws);
@@ -555,7 +555,8 @@ static Operand w_as_kn(const grpo_linear_op& op) {
   return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.K, op.N, op.w_out_in == 1, false};
 }
 
-// What the backward call does and keeps.
+// What the backward call does and keeps: dz, dbias's partial sums, and what the product at hand needs (dW's comes after dx's on
+// the stream and takes the same place).
 struct BwdPlan {
   bool make_dz;  // dz is not dy as it lies
   size_t dz, part;
@@ -570,15 +571,15 @@ static BwdPlan bwd_plan(const grpo_linear_op& op, const void* dy, int64_t lddy, 
   p.dz = p.make_dz ? align_up(2 * (size_t)op.M * (size_t)up8(op.N)) : 0;
   const int64_t rows = dz_rows(op.M, op.N);
   p.part = g.dbias ? align_up(4 * (size_t)((op.M + rows - 1) / rows) * (size_t)op.N) : 0;
-  const uint16_t* dz = static_cast<const uint16_t*>(dy);
+  const uint16_t* dz = p.make_dz ? nullptr : static_cast<const uint16_t*>(dy);  // its place in the workspace is aligned as NULL is
   const int64_t ld = p.make_dz ? up8(op.N) : lddy;
   p.dz_rows = Operand{dz, ld, op.M, op.N, false, p.make_dz};
   p.dz_cols = Operand{dz, ld, op.N, op.M, true, p.make_dz};
   p.x_cols = Operand{static_cast<const uint16_t*>(op.x), op.ldx, op.K, op.M, true, false};
   p.w = w_as_kn(op);
-  p.total = p.dz + p.part;
-  if (g.dx) p.total += product_bytes(p.dz_rows, p.w);
-  if (g.dw) p.total += product_bytes(op.w_out_in ? p.dz_cols : p.x_cols, op.w_out_in ? p.x_cols : p.dz_cols);
+  const size_t dx = g.dx ? product_bytes(p.dz_rows, p.w) : 0;
+  const size_t dw = g.dw ? product_bytes(op.w_out_in ? p.dz_cols : p.x_cols, op.w_out_in ? p.x_cols : p.dz_cols) : 0;
+  p.total = p.dz + p.part + std::max(dx, dw);
   return p;
 }
 
