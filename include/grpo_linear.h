@@ -46,13 +46,16 @@ size_t grpo_linear_workspace_bytes(const grpo_linear_op* op);
  * y = act(x W + bias) + residual.
  *   op           host struct (above)
  *   residual     device [M, N] of y's type, rows ldr apart, or NULL; may be y itself (ldr = ldy)
- *   y            device [M, N] of y_dtype (GRPO_F32 or GRPO_BF16), rows ldy apart; shares no element with x, w or bias
- *   z            device fp32 [M, N], contiguous, or NULL: z, which the backward call takes unless act is GRPO_ACT_NONE
+ *   y            device [M, N] of y_dtype (GRPO_F32 or GRPO_BF16), rows ldy apart; shares no element with x, w or bias, nor
+ *                with a residual that is not y itself (rows of two operands may lie in turn)
+ *   z            device fp32 [M, N], contiguous, or NULL: z, which the backward call takes unless act is GRPO_ACT_NONE; shares
+ *                no element with another operand
  *   ws, ws_bytes device workspace of at least grpo_linear_workspace_bytes(op), 16-byte aligned; calls that may overlap (on
  *                two streams, in two graphs) need one each
  * The same inputs give the same bits.
- * Errors: GRPO_ERR_ARG (NULL pointer, act or w_out_in unknown), GRPO_ERR_SHAPE (a size outside its range, rows closer than
- *   their length), GRPO_ERR_DTYPE, GRPO_ERR_ALIGN (a pointer not aligned to its element), GRPO_ERR_WORKSPACE, GRPO_ERR_HIP.
+ * Errors: GRPO_ERR_ARG (NULL pointer, act or w_out_in unknown, operands that share elements), GRPO_ERR_SHAPE (a size outside
+ *   its range, rows closer than their length), GRPO_ERR_DTYPE, GRPO_ERR_ALIGN (a pointer not aligned to its element),
+ *   GRPO_ERR_WORKSPACE, GRPO_ERR_HIP.
  */
 int grpo_linear(const grpo_linear_op* op, const void* residual, int64_t ldr, void* y, int64_t ldy, int32_t y_dtype,
                 float* z, void* ws, size_t ws_bytes, hipStream_t s);
@@ -76,7 +79,8 @@ size_t grpo_linear_bwd_workspace_bytes(const grpo_linear_op* op, const void* dy,
  *   op           as the forward call took it
  *   dy           device [M, N] of dy_dtype (GRPO_F32 or GRPO_BF16), rows lddy apart
  *   z            device fp32 [M, N]: what grpo_linear stored; NULL where act is GRPO_ACT_NONE
- *   grads        host struct (above); its arrays share no element with an input or with one another
+ *   grads        host struct (above); its arrays share no element with one another or with an input that the call reads
+ *                (dy; z; x for dw; w for dx)
  *   ws, ws_bytes device workspace of at least grpo_linear_bwd_workspace_bytes(...), as above
  * With M = 0 dw and dbias are zeros (dw as it was with accumulate_dw).
  * Errors: as grpo_linear, and GRPO_ERR_ARG for z NULL with an activation, or accumulate_dw with a bf16 dw.

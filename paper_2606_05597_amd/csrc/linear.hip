@@ -14,6 +14,7 @@
 #include "gemm.h"
 #include "host.h"
 #include "linear.h"
+#include "overlap.h"
 
 namespace grpo {
 
@@ -555,6 +556,11 @@ static Operand w_as_kn(const grpo_linear_op& op) {
   return Operand{static_cast<const uint16_t*>(op.w), op.ldw, op.K, op.N, op.w_out_in == 1, false};
 }
 
+static ByteRows x_bytes(const grpo_linear_op& op) { return ByteRows(op.x, op.M, op.K, op.ldx, 2); }
+static ByteRows w_bytes(const grpo_linear_op& op) {
+  return op.w_out_in ? ByteRows(op.w, op.N, op.K, op.ldw, 2) : ByteRows(op.w, op.K, op.N, op.ldw, 2);
+}
+
 // What the backward call does and keeps: dz, dbias's partial sums, and what the product at hand needs (dW's comes after dx's on
 // the stream and takes the same place).
 struct BwdPlan {
@@ -630,6 +636,12 @@ extern "C" int grpo_linear(const grpo_linear_op* op, const void* residual, int64
     if (!aligned(ws, 16)) return GRPO_ERR_ALIGN;
   }
   if (op->M > 0) {
+    const ByteRows x = x_bytes(*op), w = w_bytes(*op), b(op->bias, 1, op->N, op->N, size_of(op->bias_dtype)),
+                   r(residual, op->M, op->N, ldr, size_of(y_dtype)), out(y, op->M, op->N, ldy, size_of(y_dtype)),
+                   zs(z, op->M, op->N, op->N, 4);
+    if (rows_share(out, x) || rows_share(out, w) || rows_share(out, b) || (residual != y && rows_share(out, r)) ||
+        rows_share(zs, x) || rows_share(zs, w) || rows_share(zs, b) || rows_share(zs, r) || rows_share(zs, out))
+      return GRPO_ERR_ARG;
     char* at = static_cast<char*>(ws);
     const Epilogue e{y, ldy, op->bias, residual, ldr, z, op->act, y_dtype == GRPO_BF16, op->bias_dtype == GRPO_BF16, false,
                      op->M * op->N * (int64_t)size_of(y_dtype) > kPastL2};
@@ -664,6 +676,17 @@ extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t
     if (g.dw && !g.accumulate_dw) zero_fill(g.dw, op->K * op->N, size_of(g.dw_dtype), s);
     if (g.dbias) zero_fill(g.dbias, op->N, size_of(op->bias_dtype), s);
     return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+  }
+  const ByteRows out[3] = {ByteRows(g.dx, op->M, op->K, op->K, 2),
+                           ByteRows(g.dw, op->K, op->N, op->N, size_of(g.dw_dtype)),
+                           ByteRows(g.dbias, 1, op->N, op->N, size_of(op->bias_dtype))};
+  const ByteRows in[4] = {ByteRows(dy, op->M, op->N, lddy, size_of(dy_dtype)), ByteRows(act ? z : nullptr, op->M, op->N, op->N, 4),
+                          x_bytes(*op), w_bytes(*op)};
+  const bool read[4] = {true, true, g.dw != nullptr, g.dx != nullptr};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 4; ++j)
+      if (read[j] && rows_share(out[i], in[j])) return GRPO_ERR_ARG;
+    if (rows_share(out[i], out[(i + 1) % 3])) return GRPO_ERR_ARG;
   }
   BwdPlan p = bwd_plan(*op, dy, lddy, dy_dtype, g);
   char* at = static_cast<char*>(ws);

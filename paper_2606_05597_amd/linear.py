@@ -66,7 +66,8 @@ def grpo_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = No
                 stream=None):
     """y = act(x w + bias) + residual: x bf16 [M, K] with unit column stride, w bf16 [K, N] with unit stride in either
     dimension, bias [N] bf16 or fp32, residual [M, N] of y's type, act "none", "relu", "gelu", "gelu_tanh" or "silu".
-    ``out``: y, written in place (it may be ``residual``); without it a tensor of ``out_dtype`` (bf16 or fp32).  Returns
+    ``out``: y, written in place (it may be ``residual``, and otherwise shares no element with another operand; columns of one
+    buffer are in order); without it a tensor of ``out_dtype`` (bf16 or fp32).  Returns
     (y, z), z = x w + bias in fp32 with ``keep_z`` (what ``grpo_linear_bwd`` takes if there is an activation), otherwise
     None."""
     op = _op(x, w, act)
@@ -101,8 +102,8 @@ def grpo_linear_bwd(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, z: torch
     """The gradients of ``grpo_linear``'s y given that call's x, w and z (fp32 [M, N]; None without an activation) and the
     incoming dy [M, N] (bf16 or fp32); the residual's is dy itself.  ``dx``: True allocates a bf16 [M, K] tensor, False is
     none, a tensor is written.  ``dw``: likewise, laid out as w ([K, N], or the transpose of [N, K]), bf16 or fp32, an fp32
-    one added to with ``accumulate_dw``.  ``dbias``: a tensor [N] of the bias's type to be written, or None.  Returns
-    (dx, dw, dbias), None for those not asked for."""
+    one added to with ``accumulate_dw``.  ``dbias``: a tensor [N] of the bias's type to be written, or None.  What is written
+    shares no element with what is read.  Returns (dx, dw, dbias), None for those not asked for."""
     op = _op(x, w, act)
     M, K, N, dev = op.M, op.K, op.N, x.device
     lddy = _rows(dy, "dy", None, (M, N))
