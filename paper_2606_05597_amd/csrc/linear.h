@@ -16,10 +16,8 @@ __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -kLog2e));
 }
 
-// tanh(u) = 1 - 2 / (1 + e^2u), off by 3e-7 at most.
-__device__ __forceinline__ float tanh_of(float u) {
-  return fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * (2.f * kLog2e))), 1.f);
-}
+// (1 + tanh u) / 2 = sigmoid(2u) of u = sqrt(2 / pi) (z + 0.044715 z^3), which for negative z is small and has no 1 to cancel.
+__device__ __forceinline__ float twice_u(float z) { return (2.f * 0.79788456f) * fmaf(0.044715f * z * z, z, z); }
 
 // The normal distribution's function at z and e^(-z^2 / 2).  For x >= 0, erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 +
 // p x), off by 1.5e-7 at most (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26).
@@ -41,8 +39,7 @@ __device__ __forceinline__ float act_of(float z) {
     float e;
     return z * normal_cdf(z, e);
   }
-  if constexpr (ACT == GRPO_ACT_GELU_TANH)
-    return 0.5f * z * (1.f + tanh_of(0.79788456f * fmaf(0.044715f * z * z, z, z)));
+  if constexpr (ACT == GRPO_ACT_GELU_TANH) return z * sigmoid(twice_u(z));
   if constexpr (ACT == GRPO_ACT_SILU) return z * sigmoid(z);
   return z;
 }
@@ -56,9 +53,10 @@ __device__ __forceinline__ float slope_of(float z) {
     return fmaf(0.39894228f * z, e, c);
   }
   if constexpr (ACT == GRPO_ACT_GELU_TANH) {
-    const float t = tanh_of(0.79788456f * fmaf(0.044715f * z * z, z, z));
-    const float q = fminf(fabsf(z), 1e6f);  // beyond, 1 - t^2 is 0 and z^2 may be infinite
-    return 0.5f * (1.f + t) + 0.5f * copysignf(q, z) * (1.f - t * t) * 0.79788456f * fmaf(3.f * 0.044715f * q, q, 1.f);
+    // s + z s (1 - s) d(2u)/dz, with 1 - s = e s and e held below infinity
+    const float e = __builtin_amdgcn_exp2f(fminf(twice_u(z) * -kLog2e, 127.f)), s = __builtin_amdgcn_rcpf(1.f + e);
+    const float q = fminf(fabsf(z), 1e6f);  // beyond, s (1 - s) is 0 and z^2 may be infinite
+    return fmaf(copysignf(q, z) * (s * (e * s)), (2.f * 0.79788456f) * fmaf(3.f * 0.044715f * q, q, 1.f), s);
   }
   if constexpr (ACT == GRPO_ACT_SILU) {
     const float g = sigmoid(z);
