@@ -19,15 +19,19 @@ __device__ __forceinline__ float sigmoid(float z) {
 // (1 + tanh u) / 2 = sigmoid(2u) of u = sqrt(2 / pi) (z + 0.044715 z^3), which for negative z is small and has no 1 to cancel.
 __device__ __forceinline__ float twice_u(float z) { return (2.f * 0.79788456f) * fmaf(0.044715f * z * z, z, z); }
 
-// The normal distribution's function at z and e^(-z^2 / 2).  For x >= 0, erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 +
-// p x), off by 1.5e-7 at most (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26).
+// The normal distribution's function at z and e^(-z^2 / 2).  For x >= 0, erfc(x) = (a1 t + .. + a8 t^8) e^(-x^2), t = 1 / (1 +
+// 0.33 x): coefficients fitted here for the least largest relative error over 0 <= x <= 9.4 (repeatedly reweighted least
+// squares, Lawson's method), 8.2e-8, so that the tail below zero keeps its bits.  Five terms reach 2.8e-5.
 __device__ __forceinline__ float normal_cdf(float z, float& e) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.33f * 0.70710678f, fabsf(z), 1.f));
   e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f);
+  float p = fmaf(-0.135928795f, t, 0.462688237f);
+  p = fmaf(p, t, -0.355438948f);
+  p = fmaf(p, t, 0.412541598f);
+  p = fmaf(p, t, 0.0450106487f);
+  p = fmaf(p, t, 0.201923817f);
+  p = fmaf(p, t, 0.182837248f);
+  p = fmaf(p, t, 0.186366111f);
   const float half = 0.5f * p * t * e;  // of the tail beyond |z|
   return z >= 0.f ? 1.f - half : half;
 }

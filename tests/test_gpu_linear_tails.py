@@ -4,6 +4,9 @@ z is the bias alone (x = 0), y fp32, and dbias of one row with dy = 1 the slope,
 - gelu_tanh: z sigmoid(a), a = 2 sqrt(2 / pi) (z + 0.044715 z^3), is off by 5 e |a| of the exponent (a's four roundings and the
   factor's), 2 e for exp2, e for the sum, 2 e for the reciprocal and e for the product: (5 |a| + 7) e.  Its slope is s + z s (1 - s) a':
   s as above, the other term by three such factors, (15 |a| + 24) e, and e.
+- gelu: z times half the weight of the tail, p(t) e^(-z^2/2): 1.5 z^2 e of the exponent's three factors and 2 e for exp2, 4 e in
+  t, which count at most twice, 16 e for the eight terms, 1.4 e for the fit, 3 e of products: (1.5 z^2 + 32) e; above zero that of
+  the tail, in 1 - tail, and 2 e.  Its slope adds z e^(-z^2/2) / sqrt(2 pi), off by (1.5 z^2 + 8) e, and e.
 - silu: z sigmoid(z) likewise with 3 e |z| of the exponent: (3 |z| + 7) e.
 """
 import math
@@ -44,6 +47,18 @@ def test_gelu_tanh():
     near(y, zd * s, 1.01 * (5 * a.abs() + 7) * E * (zd * s).abs(), z)
     rest = zd * s * torch.sigmoid(-a) * da
     near(slope, s + rest, 1.01 * E * ((5 * a.abs() + 7) * s + (15 * a.abs() + 24) * rest.abs() + (s + rest).abs()), z)
+
+
+def test_gelu():
+    z = torch.linspace(-12, 12, 6001, device="cuda")
+    y, slope = values("gelu", z)
+    zd = z.double()
+    tail = 0.5 * torch.special.erfc(zd.abs() * math.sqrt(0.5))
+    cdf = torch.where(zd < 0, tail, 1 - tail)
+    off = (1.5 * zd**2 + 32) * E * tail + torch.where(zd < 0, 0.0, 2 * E)
+    near(y, zd * cdf, 1.01 * (zd.abs() * off + E * (zd * cdf).abs()), z)
+    rest = zd * torch.exp(-0.5 * zd**2) / math.sqrt(2 * math.pi)
+    near(slope, cdf + rest, 1.01 * (off + (1.5 * zd**2 + 8) * E * rest.abs() + E * (cdf + rest).abs()), z)
 
 
 def test_silu():
