@@ -359,7 +359,6 @@ __global__ __launch_bounds__(256) void k_lin_dbias(const float* __restrict__ par
 
 // ---- host -----------------------------------------------------------------------
 constexpr int64_t kCus = 256;
-constexpr int64_t kPastL2 = (int64_t)256 << 20;  // bytes of a result that passes the L2
 constexpr int64_t kMostLin = 8388352;  // 2^23 - 256: 256 rows of an operand stay below 4 GB
 
 static int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -643,8 +642,7 @@ extern "C" int grpo_linear(const grpo_linear_op* op, const void* residual, int64
         rows_share(zs, x) || rows_share(zs, w) || rows_share(zs, b) || rows_share(zs, r) || rows_share(zs, out))
       return GRPO_ERR_ARG;
     char* at = static_cast<char*>(ws);
-    const Epilogue e{y, ldy, op->bias, residual, ldr, z, op->act, y_dtype == GRPO_BF16, op->bias_dtype == GRPO_BF16, false,
-                     op->M * op->N * (int64_t)size_of(y_dtype) > kPastL2};
+    const Epilogue e{y, ldy, op->bias, residual, ldr, z, op->act, y_dtype == GRPO_BF16, op->bias_dtype == GRPO_BF16, false};
     launch_product(x_rows(*op), w_as_nk(*op), e, at, s);
   }
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
@@ -707,14 +705,12 @@ extern "C" int grpo_linear_bwd(const grpo_linear_op* op, const void* dy, int64_t
   }
   if (dz) p.dz_rows.src = p.dz_cols.src = dz;
   if (g.dx) {
-    const Epilogue e{g.dx, op->K, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE, true, false, false,
-                     op->M * op->K * 2 > kPastL2};
+    const Epilogue e{g.dx, op->K, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE, true, false, false};
     launch_product(p.dz_rows, p.w, e, at, s);
   }
   if (g.dw) {
     const Epilogue e{g.dw, op->w_out_in ? op->K : op->N, nullptr, nullptr, 0, nullptr, GRPO_ACT_NONE,
-                     g.dw_dtype == GRPO_BF16, false, g.accumulate_dw == 1,
-                     op->K * op->N * (int64_t)size_of(g.dw_dtype) > kPastL2};
+                     g.dw_dtype == GRPO_BF16, false, g.accumulate_dw == 1};
     launch_product(op->w_out_in ? p.dz_cols : p.x_cols, op->w_out_in ? p.x_cols : p.dz_cols, e, at, s);
   }
   return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
