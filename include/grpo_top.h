@@ -54,8 +54,8 @@ size_t grpo_token_logp_top_workspace_bytes(int64_t T, int64_t V, int32_t n);
  * A row with a NaN or +inf (GRPO_FLAG_NONFINITE), or with its own temperature out of range (GRPO_FLAG_SETTING): log-prob,
  * entropy and alternatives' log-probs NaN, alternatives -1.  A row without words (GRPO_FLAG_NONFINITE): entropy 0, no
  * alternatives, the log-prob of an action in [0, V) -inf.
- * Each row is read once, but for the few words that may be alternatives; one in which so many words equal the largest that
- * they overflow the list of these is read 16 (bf16) or 32 (fp32) times more.  Sums run in fp32 over at most 32 words, in fp64
+ * Each row is read once, but for the few words that may be alternatives; a row whose large words repeat more often than a list
+ * of 1,024 holds (256 for rows of one wave) is read up to 16 (bf16) or 32 (fp32) times more.  Sums run in fp32 over at most 32 words, in fp64
  * beyond; the same inputs give the same bits.  Log-probs are at most 0, entropies at least 0.
  * Errors: GRPO_ERR_ARG (a required pointer NULL, temperature_all out of range), GRPO_ERR_SHAPE, GRPO_ERR_DTYPE,
  *   GRPO_ERR_ALIGN (logits and arrays to their element, ws to 16), GRPO_ERR_WORKSPACE, GRPO_ERR_HIP.
