@@ -425,7 +425,8 @@ __device__ __forceinline__ void top_by_counts(const Tin* row, int cols, int n, f
   if (tid >= above && tid < n) out.put(tid, equal[tid - above]);
 }
 
-// One workgroup to a row, or (PART) to a part of it.
+// One workgroup to a row, or (PART) to a part of it.  Seven waves to a SIMD: left to itself the compiler takes the registers of six
+// (20,000 x 1,000 bf16 words with 64 alternatives: 151 us against 132).
 template <typename Tin, int NT, bool PART>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT == 1024 ? 8 : 7))) void k_top(const TopArgs a,
                                                                                                   int row0) {
